@@ -141,13 +141,16 @@ def prepare(case, seed):
     tokens = tokens.masked_fill(padding, -100).to(torch.int32)
     state["tokens"] = tokens[:, 0].contiguous() if n == 1 else tokens
     if case["op"] == "grad":
+        # what the forward pass left: each row's largest logit and log sum relative to it
         _, lse, entropy = _row_statistics(logits)
-        state["lse"], state["entropy"] = lse, entropy
+        highest = logits.float().amax(dim=1)
+        state["stats"] = torch.stack([highest, lse - highest * INV_TEMPERATURE], dim=1)
+        state["entropy"] = entropy
         state["grad_logprobs"] = torch.empty_like(state["tokens"], dtype=torch.float32).normal_(
             0.0, 1.0 / n, generator=g)
         if case["entropy"]:
             state["grad_entropy"] = torch.empty(B, device="cuda").uniform_(-0.02, 0.0, generator=g)
-            state["grad_lse"] = 2e-4 * lse                  # of a penalty on the squared log sum
+            state["grad_lse"] = 2e-4 * lse                 # of a penalty on the squared log sum
     return state
 
 
@@ -204,7 +207,7 @@ def _plain(s):
             out["top_logprobs"] = torch.where(empty[:, None], -math.inf, best)
         return out
     g = torch.where(real, s["grad_logprobs"].view(B, c["n"]), 0.0)
-    logp = s["logits"].float() * INV_TEMPERATURE - s["lse"][:, None]
+    logp = (s["logits"].float() - s["stats"][:, :1]) * INV_TEMPERATURE - s["stats"][:, 1:]
     share = -g.sum(dim=1, keepdim=True)
     if c["entropy"]:
         share = share + s["grad_lse"][:, None] - s["grad_entropy"][:, None] * (logp + s["entropy"][:, None])
@@ -229,8 +232,8 @@ def run(state):
         if c["top"]:
             out["top_ids"], out["top_logprobs"] = r.top_ids, r.top_logprobs
         return out
-    return sbw.token_logprobs_grad(state["logits"], state["tokens"], state["lse"], state["entropy"],
-                                   state["grad_logprobs"], state.get("grad_lse"),
+    return sbw.token_logprobs_grad(state["logits"], state["tokens"], state["stats"],
+                                   state["entropy"], state["grad_logprobs"], state.get("grad_lse"),
                                    state.get("grad_entropy"), INV_TEMPERATURE)
 
 
@@ -248,7 +251,7 @@ def work(case):
     if op == "logprobs":
         # shift, scale, exponential, sum, weighted sum (a multiply and an add)
         return {"bytes": size * B * V + B * (8 * case["n"] + 8 + 8 * case["top"]), "flops": 6 * B * V}
-    rows = B * (8 * case["n"] + (16 if case["entropy"] else 4))
+    rows = B * (8 * case["n"] + (20 if case["entropy"] else 8))
     return {"bytes": 2 * size * B * V + rows, "flops": (6 if case["entropy"] else 4) * B * V}
 
 
@@ -282,13 +285,14 @@ def exact(case, seed):
     B, n = case["B"], case["n"]
     parts = []
     for b in range(B):
-        z = s["logits"][b].double() * INV_TEMPERATURE
+        x = s["logits"][b].double()
+        z = x * INV_TEMPERATURE
         ids = s["tokens"].view(B, n)[b].long()
         real = ids >= 0
         at = ids.clamp(min=0)
         if case["op"] == "grad":
             g = torch.where(real, s["grad_logprobs"].view(B, n)[b].double(), 0.0)
-            logp = z - s["lse"][b].double()
+            logp = (x - s["stats"][b, 0].double()) * INV_TEMPERATURE - s["stats"][b, 1].double()
             p = torch.exp(logp)
             d = p * -g.sum()
             if case["entropy"]:
