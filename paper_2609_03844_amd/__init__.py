@@ -13,6 +13,13 @@ fallback: if the library is missing this module raises on import.
     green_mask(prev_tokens, V, key, gamma, seeding="context") -> int32 [B, ceil(V/32)]
     detect(tokens, key, gamma, seeding="context") -> (counts int32 [N], z float64 [N])
 
+and the operators beside it in a decode or training step (``step.py``):
+
+    head_logits(hidden, codes, scales) -> logits [B, V]
+    top_candidates(logits, k) -> (ids [B, k], values [B, k])
+    token_logprobs(logits, tokens, inv_temperature, top) -> TokenLogprobs
+    token_logprobs_grad(logits, tokens, stats, ...) -> gradient like logits
+
 Tensors are torch tensors on the current HIP device; torch provides the memory
 and the stream, nothing else.
 
@@ -578,3 +585,12 @@ def detect_ex(tokens: torch.Tensor, key: int, gamma: float, seeding="context", w
                               DETECT_IGNORE_REPEATED if ignore_repeated else 0, counts.data_ptr(),
                               scored.data_ptr(), z.data_ptr(), _stream(stream)))
     return counts, scored, z
+
+
+from .step import (EXPORTED_STEP, TokenLogprobs, head_logits, token_logprobs,  # noqa: E402
+                   token_logprobs_grad, token_logprobs_workspace_size, top_candidates,
+                   top_candidates_workspace_size)
+
+__all__ += ["token_logprobs", "token_logprobs_grad", "top_candidates", "head_logits",
+            "TokenLogprobs", "token_logprobs_workspace_size", "top_candidates_workspace_size",
+            "EXPORTED_STEP"]

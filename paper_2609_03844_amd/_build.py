@@ -13,13 +13,14 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIBRARY = os.path.join(PKG, "libsbw.so")
-SOURCES = [os.path.join(CSRC, "sbw_kernels.hip")]
+SOURCES = [os.path.join(CSRC, "sbw_library.hip")]   # includes the other sources
 BINDING = os.path.join(PKG, "_binding.so")
 BINDING_SOURCE = os.path.join(CSRC, "binding.cpp")
 RATE_LIBRARY = os.path.join(PKG, "libsbw_rate.so")
 RATE_SOURCES = [os.path.join(CSRC, "philox_rate.hip")]
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
-HEADERS = [os.path.join(CSRC, "sbw_device.hpp"), os.path.join(INCLUDE, "sbw.h")]
+HEADERS = [os.path.join(CSRC, "sbw_device.hpp"), os.path.join(INCLUDE, "sbw.h"),
+           os.path.join(INCLUDE, "sbw_step.h")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

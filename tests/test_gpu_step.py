@@ -1,0 +1,530 @@
+"""The operators of include/sbw_step.h on the GPU against their 64-bit definitions."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import step_reference as ref
+
+pytestmark = pytest.mark.gpu
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def sbw():
+    import paper_2609_03844_amd as sbw
+    return sbw
+
+
+def say(text):
+    print(text, flush=True)
+
+
+def placed(x, dtype, pad=0, offset=0):
+    """x [B, V] float32 -> (device tensor with padded, possibly unaligned rows, its exact values)."""
+    B, V = x.shape
+    buf = torch.full((B * (V + pad) + offset,), 7.0e4, dtype=DTYPES[dtype], device="cuda")
+    t = buf[offset:].view(B, V + pad)[:, :V]
+    t.copy_(torch.from_numpy(x))
+    return t, t.float().cpu().numpy()
+
+
+def logits(rng, B, V):
+    x = (3.0 * rng.standard_normal((B, V))).astype(np.float32)
+    x[rng.random((B, V)) < 0.05] += 8.0
+    return x
+
+
+def special(rng, B, V):
+    """Rows out of the ordinary, in turn: masks of -inf and of the lowest value, empty rows, NaN, +inf,
+    all equal, few tokens left, sorted, zeros of both signs, one token far above."""
+    x = logits(rng, B, V)
+    low = np.float32(-3.3895314e38)            # bf16's lowest value, a finite float
+    for b in range(B):
+        kind = b % 13
+        if kind == 1:
+            x[b, rng.random(V) < 0.9] = -np.inf
+        elif kind == 2:
+            x[b, rng.random(V) < 0.9] = low
+        elif kind == 3:
+            x[b] = -np.inf
+        elif kind == 4:
+            x[b] = low
+        elif kind == 5:
+            x[b, rng.integers(0, V, 3)] = np.nan
+        elif kind == 6:
+            x[b, rng.integers(0, V, 2)] = np.inf
+        elif kind == 7:
+            x[b] = 1.25
+        elif kind == 8:
+            keep = rng.integers(0, V, 5)
+            kept = x[b, keep]
+            x[b] = -np.inf
+            x[b, keep] = kept
+        elif kind == 9:
+            x[b] = np.sort(x[b])[::-1] if b % 2 else np.sort(x[b])
+        elif kind == 10:
+            x[b] = np.where(rng.random(V) < 0.5, 0.0, -0.0)
+        elif kind == 11:
+            x[b] = np.round(x[b])
+        elif kind == 12:
+            x[b, rng.integers(0, V)] = 300.0
+    return x
+
+
+def given(rng, B, V, n):
+    t = rng.integers(0, V, (B, n))
+    t[rng.random((B, n)) < 0.1] = rng.choice([-1, -100, V, V + 5, 2 ** 31 - 1, -2 ** 31])
+    if n > 2:
+        t[:, 2] = t[:, 0]                      # a token given twice
+    return t.astype(np.int32)
+
+
+def close(got, want, tol, what):
+    got = got.double().cpu().numpy()
+    assert got.shape == want.shape, what
+    assert np.array_equal(np.isnan(got), np.isnan(want)), what
+    inf = np.isinf(want)
+    assert np.array_equal(got[inf], want[inf]), what
+    fine = np.isfinite(want)
+    assert np.isfinite(got[fine]).all(), what
+    bad = np.abs(got - want)[fine] > np.broadcast_to(tol, want.shape)[fine]
+    assert not bad.any(), (what, np.abs(got - want)[fine][bad][:5], np.broadcast_to(tol, want.shape)[fine][bad][:5])
+
+
+def check_forward(sbw, x, tokens, inv_t, top, dtype, pad=0, offset=0, what=""):
+    t, exact = placed(x, dtype, pad, offset)
+    B = x.shape[0]
+    flat = torch.from_numpy(tokens[:, 0].copy() if tokens.shape[1] == 1 else tokens).cuda()
+    r = sbw.token_logprobs(t, flat, inv_t, top=top)
+    want, tol = ref.logprobs(exact, tokens, inv_t, top)
+    close(r.logprobs.view(B, -1), want[0], tol[0], what + " logprobs")
+    close(r.lse, want[1], tol[1], what + " lse")
+    close(r.entropy, want[2], tol[2], what + " entropy")
+    if top:
+        assert np.array_equal(r.top_ids.cpu().numpy(), want[3]), what + " top ids"
+        close(r.top_logprobs, want[4], tol[4], what + " top logprobs")
+    else:
+        assert r.top_ids is None and r.top_logprobs is None
+    return t, flat, r
+
+
+SIZES = [(1, 1), (13, 2), (13, 3), (3, 7), (13, 64), (26, 255), (13, 1000), (26, 2049), (13, 4097),
+         (26, 8192), (13, 20011), (13, 32001), (13, 50257)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,V", SIZES)
+def test_logprobs_special_rows(sbw, dtype, B, V):
+    rng = np.random.default_rng(1000 * B + V)
+    for n, top, inv_t in ((1, 0, 1.0), (4, 5, 0.7), (1, 50, 1.25), (33, 1024, 1.0)):
+        say(f"logprobs {dtype} B={B} V={V} n={n} top={top}")
+        check_forward(sbw, special(rng, B, V), given(rng, B, V, n), inv_t, top, dtype, what=f"n={n} top={top}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pad,offset", [(1, 0), (0, 1), (3, 5), (8, 8)])
+def test_logprobs_layouts(sbw, dtype, pad, offset):
+    rng = np.random.default_rng(pad * 10 + offset)
+    for B, V in ((13, 5003), (300, 777)):
+        say(f"layout {dtype} {B}x{V} pad={pad} offset={offset}")
+        check_forward(sbw, special(rng, B, V), given(rng, B, V, 2), 1.0, 9, dtype, pad, offset)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,V,top", [(1, 152064, 20), (70, 128259, 0), (40, 30000, 7), (1, 1000003, 100),
+                                     (600, 16384, 3), (2, 151936, 1000)])
+def test_logprobs_launch_shapes(sbw, dtype, B, V, top):
+    rng = np.random.default_rng(B + V)
+    say(f"logprobs {dtype} B={B} V={V} top={top}")
+    check_forward(sbw, logits(rng, B, V), given(rng, B, V, 1), 1.25, top, dtype)
+
+
+def test_logprobs_without_tokens_and_outputs_of_the_caller(sbw):
+    rng = np.random.default_rng(5)
+    x = logits(rng, 5, 3000)
+    t, exact = placed(x, "f32")
+    r = sbw.token_logprobs(t, None)
+    want, tol = ref.logprobs(exact, np.zeros((5, 0), np.int64), 1.0)
+    assert r.logprobs is None
+    close(r.entropy, want[2], tol[2], "entropy")
+    ids = torch.from_numpy(given(rng, 5, 3000, 1)[:, 0].copy()).cuda()
+    full = sbw.token_logprobs(t, ids, top=4)
+    out = sbw.TokenLogprobs(*(torch.full_like(v, 3) for v in full))
+    again = sbw.token_logprobs(t, ids, top=4, out=out,
+                               workspace=torch.empty(max(1, sbw.token_logprobs_workspace_size(5, 3000, 4)),
+                                                     dtype=torch.int64, device="cuda"))
+    for a, b, c in zip(full, again, out):
+        assert b is c and torch.equal(a, b)
+
+
+def test_masked_value_range(sbw):
+    """fp32's lowest value, infinite differences and subnormal logits."""
+    x = np.zeros((4, 700), np.float32)
+    x[0, 1:] = np.finfo(np.float32).min
+    x[1, :350], x[1, 350:] = np.finfo(np.float32).min, np.finfo(np.float32).max
+    x[2] = np.linspace(-1e-40, 1e-40, 700)
+    x[3, ::2] = -3e38
+    tokens = np.tile(np.array([[0, 1, 699]], np.int32), (4, 1))
+    for inv_t in (0.5, 1.0):
+        check_forward(sbw, x, tokens, inv_t, 3, "f32")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,V", SIZES)
+def test_candidates_special_rows(sbw, dtype, B, V):
+    rng = np.random.default_rng(77 * B + V)
+    x = special(rng, B, V)
+    t, exact = placed(x, dtype, pad=V % 3, offset=V % 2)
+    for k in (1, 2, 40, 100, 1000, 1024):
+        say(f"candidates {dtype} B={B} V={V} k={k}")
+        ids, values = sbw.top_candidates(t, k, v_offset=0 if k > 1 else 11)
+        for b in range(B):
+            want = ref.order(exact[b])[:k]
+            got = ids[b].cpu().numpy()
+            kept = min(k, V)
+            assert np.array_equal(got[:kept], want + (0 if k > 1 else 11)), (k, b)
+            assert (got[kept:] == -1).all()
+            assert np.array_equal(values[b, :kept].cpu().numpy(), exact[b][want], equal_nan=True), (k, b)
+            assert (values[b, kept:] == -np.inf).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,V,k", [(1, 152064, 40), (300, 32000, 40), (2, 1000003, 300), (70, 128259, 1024),
+                                   (520, 4099, 64)])
+def test_candidates_launch_shapes(sbw, dtype, B, V, k):
+    rng = np.random.default_rng(B + V + k)
+    t, exact = placed(logits(rng, B, V), dtype)
+    ids, values = sbw.top_candidates(t, k)
+    got, val = ids.cpu().numpy(), values.cpu().numpy()
+    for b in range(0, B, max(1, B // 20)):
+        want = ref.order(exact[b])[:k]
+        assert np.array_equal(got[b], want), b
+        assert np.array_equal(val[b], exact[b][want]), b
+    assert torch.equal(sbw.top_candidates(t, k, with_values=False)[0], ids)
+
+
+def test_candidates_where_the_largest_stand_together(sbw):
+    """The largest logits side by side, or a fixed distance apart: wherever a split of the row puts them."""
+    rng = np.random.default_rng(6)
+    V = 60000
+    rows = []
+    for step in (1, 2, 4, 8, 32, 64, 256, 1024, 2048, 4096):
+        x = rng.standard_normal(V).astype(np.float32)
+        at = (np.arange(2000) * step + 17) % V
+        x[at] = 50 + rng.random(2000).astype(np.float32)
+        rows.append(x)
+    x = np.stack(rows + [np.sort(rows[0]), np.sort(rows[0])[::-1].copy()])
+    for dtype in ("f32", "bf16"):
+        t, exact = placed(x, dtype)
+        for k in (1, 64, 500, 1024):
+            say(f"together {dtype} k={k}")
+            ids = sbw.top_candidates(t, k)[0].cpu().numpy()
+            for b in range(x.shape[0]):
+                assert np.array_equal(ids[b], ref.order(exact[b])[:k]), (dtype, k, b)
+
+
+def upstream(rng, B, n, which):
+    def f(shape, scale):
+        return (scale * rng.standard_normal(shape)).astype(np.float32)
+    return (f((B, n), 1.0) if "p" in which else None, f(B, 0.3) if "l" in which else None,
+            f(B, 0.1) if "h" in which else None)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,V", SIZES)
+def test_gradient(sbw, dtype, B, V):
+    rng = np.random.default_rng(31 * B + V)
+    for n, which, inv_t in ((1, "p", 1.0), (1, "plh", 1.25), (5, "ph", 0.7), (64, "p", 1.0), (1024, "pl", 1.0),
+                            (3, "h", 1.0), (2, "l", 1.0)):
+        say(f"gradient {dtype} B={B} V={V} n={n} {which}")
+        x, tokens = special(rng, B, V), given(rng, B, V, n)
+        t, exact = placed(x, dtype, pad=n % 3, offset=n % 2)
+        flat = torch.from_numpy(tokens[:, 0].copy() if n == 1 else tokens).cuda()
+        r = sbw.token_logprobs(t, flat, inv_t)
+        stats, H = r.stats.cpu().numpy(), r.entropy.cpu().numpy()
+        up = upstream(rng, B, n, which)
+        dev = [torch.from_numpy(u).cuda() if u is not None else None for u in up]
+        if dev[0] is not None:
+            dev[0] = dev[0].view(flat.shape)
+        zero = (np.zeros((B, n)), np.zeros(B), np.zeros(B))
+        want, tol = ref.gradient(exact, tokens, inv_t, stats, H, *(u if u is not None else z for u, z in zip(up, zero)),
+                                 bf16=dtype == "bf16")
+        d = sbw.token_logprobs_grad(t, flat, r.stats, r.entropy, *dev, inv_t)
+        assert d.dtype == DTYPES[dtype]
+        close(d, want, tol, f"n={n} {which}")
+        # into padded rows, then in place: the same bits
+        wide = torch.full((B, V + 3), 5.0, dtype=d.dtype, device="cuda")
+        sbw.token_logprobs_grad(t, flat, r.stats, r.entropy, *dev, inv_t, out=wide[:, :V])
+        assert torch.equal(wide[:, :V].contiguous().view(torch.uint8), d.contiguous().view(torch.uint8))
+        assert (wide[:, V:] == 5.0).all()
+        assert sbw.token_logprobs_grad(t, flat, r.stats, r.entropy, *dev, inv_t, out=t) is t
+        assert torch.equal(t.contiguous().view(torch.uint8), d.contiguous().view(torch.uint8))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,V,n", [(1, 152064, 1), (70, 128259, 2), (600, 16384, 1), (1, 1000003, 32)])
+def test_gradient_launch_shapes(sbw, dtype, B, V, n):
+    rng = np.random.default_rng(B + V)
+    x, tokens = logits(rng, B, V), given(rng, B, V, n)
+    t, exact = placed(x, dtype)
+    flat = torch.from_numpy(tokens[:, 0].copy() if n == 1 else tokens).cuda()
+    r = sbw.token_logprobs(t, flat)
+    g, gl, gh = upstream(rng, B, n, "plh")
+    d = sbw.token_logprobs_grad(t, flat, r.stats, r.entropy, torch.from_numpy(g).cuda().view(flat.shape),
+                                torch.from_numpy(gl).cuda(), torch.from_numpy(gh).cuda())
+    want, tol = ref.gradient(exact, tokens, 1.0, r.stats.cpu().numpy(), r.entropy.cpu().numpy(), g, gl, gh,
+                             bf16=dtype == "bf16")
+    close(d, want, tol, "gradient")
+
+
+def test_gradient_against_differences(sbw):
+    """Central differences of the 64-bit loss, at every column of small rows."""
+    rng = np.random.default_rng(8)
+    B, V, n, inv_t = 3, 37, 4, 1.25
+    x, tokens = (2 * rng.standard_normal((B, V))).astype(np.float32), given(rng, B, V, n)
+    g, gl, gh = upstream(rng, B, n, "plh")
+
+    def loss(z):
+        (lp, lse, H, _, _), _ = ref.logprobs(z, tokens, inv_t)
+        return (lp * g).sum() + (lse * gl).sum() + (H * gh).sum()
+    t = torch.from_numpy(x).cuda()
+    ids = torch.from_numpy(tokens).cuda()
+    r = sbw.token_logprobs(t, ids, inv_t)
+    d = sbw.token_logprobs_grad(t, ids, r.stats, r.entropy, *(torch.from_numpy(u).cuda() for u in (g, gl, gh)),
+                                inv_t).cpu().numpy()
+    for b in range(B):
+        for v in range(V):
+            step = np.zeros((B, V))
+            step[b, v] = 1e-5
+            quotient = (loss(x + step) - loss(x - step)) / 2e-5
+            # the quotient's own error is about 1e-10 (third derivatives) + 1e-15 * loss / 1e-5
+            assert abs(quotient - d[b, v]) < 2e-5, (b, v)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_autograd(sbw, dtype):
+    rng = np.random.default_rng(9)
+    B, V = 6, 3001
+    t, _ = placed(logits(rng, B, V), dtype)
+    ids = torch.from_numpy(given(rng, B, V, 3)).cuda()
+    x = t.clone().requires_grad_()
+    r = sbw.token_logprobs(x, ids, 0.8, top=4)
+    assert r.logprobs.requires_grad and r.lse.requires_grad and r.entropy.requires_grad
+    assert not r.top_ids.requires_grad and not r.top_logprobs.requires_grad
+    (-r.logprobs.mean() + 1e-3 * r.lse.square().mean() - 0.01 * r.entropy.mean()).backward()
+    g = torch.full((B, 3), -1.0 / (3 * B), device="cuda")
+    want = sbw.token_logprobs_grad(t, ids, r.stats, r.entropy.detach(), g, 2e-3 * r.lse.detach() / B,
+                                   torch.full((B,), -0.01 / B, device="cuda"), 0.8)
+    torch.testing.assert_close(x.grad, want, rtol=1e-5 if dtype == "f32" else 1e-2, atol=1e-8)
+    # one output alone, from a non-contiguous upstream gradient
+    x = t.clone().requires_grad_()
+    sbw.token_logprobs(x, ids[:, 0].contiguous(), 0.8).logprobs[::2].sum().backward()
+    g = torch.zeros(B, device="cuda")
+    g[::2] = 1.0
+    assert torch.equal(x.grad, sbw.token_logprobs_grad(t, ids[:, 0].contiguous(), r.stats, None, g,
+                                                       inv_temperature=0.8))
+    with torch.no_grad():
+        assert not sbw.token_logprobs(x, ids).logprobs.requires_grad
+    with pytest.raises(ValueError):
+        sbw.token_logprobs(x, ids, out=r)
+
+
+def packed(rng, V, K, group, scale_dtype, whole=False):
+    codes = rng.integers(0, 256, (V, K // 2)).astype(np.uint8)
+    s = np.ones((V, K // group), np.float32) if whole else rng.uniform(0.5, 1.5, (V, K // group)).astype(np.float32)
+    if whole:
+        s *= 2.0 ** rng.integers(-2, 3, s.shape)
+    s = torch.from_numpy(s).to(DTYPES[scale_dtype])
+    return codes, s.cuda(), s.float().numpy()
+
+
+HEADS = [(1, 1, 32), (1, 33, 32), (2, 16, 64), (3, 17, 96), (1, 1000, 128), (16, 257, 1024), (5, 100, 1152),
+         (17, 70, 2048), (1, 4096, 2048), (33, 40, 4096), (11, 300, 4096), (4, 130, 5120), (16, 65, 8192),
+         (2, 31, 7168), (1, 20000, 256)]
+
+
+@pytest.mark.parametrize("B,V,K", HEADS)
+def test_head(sbw, B, V, K):
+    rng = np.random.default_rng(B + V + K)
+    for group in (32, 64, 128):
+        if K % group:
+            continue
+        for scale_dtype, out_dtype in (("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16")):
+            say(f"head B={B} V={V} K={K} group={group} {scale_dtype} {out_dtype}")
+            codes, s, exact_s = packed(rng, V, K, group, scale_dtype)
+            h = torch.from_numpy(rng.standard_normal((B, K + 3)).astype(np.float32)).to(torch.bfloat16)
+            hidden = h.cuda()[:, 1:K + 1] if B % 2 else h.cuda()[:, :K]
+            exact_h = hidden.float().cpu().numpy()
+            out = sbw.head_logits(hidden, torch.from_numpy(codes).cuda(), s, dtype=DTYPES[out_dtype])
+            want, tol = ref.head(exact_h, codes, exact_s, out_dtype == "bf16")
+            close(out, want, tol, f"group={group}")
+
+
+@pytest.mark.parametrize("B,V,K", HEADS)
+def test_head_whole_numbers(sbw, B, V, K):
+    """Small whole hidden states and scales that are powers of two: every sum is exact."""
+    rng = np.random.default_rng(2 * B + V + K)
+    for group in (32, 64, 128):
+        if K % group:
+            continue
+        codes, s, exact_s = packed(rng, V, K, group, "f32", whole=True)
+        h = rng.integers(-3, 4, (B, K)).astype(np.float32)
+        wide = torch.full((B, V + 5), 9.0, device="cuda")
+        sbw.head_logits(torch.from_numpy(h).to(torch.bfloat16).cuda(), torch.from_numpy(codes).cuda(), s,
+                        out=wide[:, :V])
+        want, _ = ref.head(h, codes, exact_s)
+        assert np.array_equal(wide[:, :V].cpu().numpy(), want.astype(np.float32)), group
+        assert (wide[:, V:] == 9.0).all()
+
+
+def test_head_one_weight_at_a_time(sbw):
+    """A hidden state with a single 1 reads out one column's weights exactly."""
+    rng = np.random.default_rng(4)
+    V, K = 48, 384
+    for group in (32, 64, 128):
+        codes, s, exact_s = packed(rng, V, K, group, "bf16")
+        w = ref.weights(codes, exact_s)
+        eye = torch.eye(K, device="cuda").to(torch.bfloat16)
+        out = sbw.head_logits(eye, torch.from_numpy(codes).cuda(), s)
+        assert np.array_equal(out.cpu().numpy(), w.T.astype(np.float32)), group
+
+
+def test_head_infinite_and_nan_states(sbw):
+    rng = np.random.default_rng(10)
+    B, V, K = 4, 100, 512
+    codes, s, exact_s = packed(rng, V, K, 64, "f32")
+    h = rng.standard_normal((B, K)).astype(np.float32)
+    h[1, 77], h[2, 500] = np.nan, np.inf
+    hidden = torch.from_numpy(h).to(torch.bfloat16).cuda()
+    out = sbw.head_logits(hidden, torch.from_numpy(codes).cuda(), s)
+    want, tol = ref.head(hidden.float().cpu().numpy()[[0, 3]], codes, exact_s)
+    close(out[[0, 3]], want, tol, "finite rows")
+    assert torch.isnan(out[1]).all() and not torch.isfinite(out[2]).any()
+
+
+def test_far_rows(sbw):
+    """Rows more than 2^31 elements apart."""
+    rng = np.random.default_rng(12)
+    V, stride = 5001, (1 << 31) + 3
+    x = logits(rng, 2, V)
+    buf = torch.empty(stride + V, dtype=torch.bfloat16, device="cuda")
+    t = buf.as_strided((2, V), (stride, 1))
+    t.copy_(torch.from_numpy(x))
+    exact = t.float().cpu().numpy()
+    tokens = given(rng, 2, V, 3)
+    ids = torch.from_numpy(tokens).cuda()
+    r = sbw.token_logprobs(t, ids, top=6)
+    want, tol = ref.logprobs(exact, tokens, 1.0, 6)
+    close(r.logprobs, want[0], tol[0], "logprobs")
+    assert np.array_equal(r.top_ids.cpu().numpy(), want[3])
+    assert np.array_equal(sbw.top_candidates(t, 6)[0].cpu().numpy(), want[3])
+    g = np.ones((2, 3), np.float32)
+    d = sbw.token_logprobs_grad(t, ids, r.stats, None, torch.from_numpy(g).cuda(), out=t)
+    want, tol = ref.gradient(exact, tokens, 1.0, r.stats.cpu().numpy(), r.entropy.cpu().numpy(), g, np.zeros(2),
+                             np.zeros(2), bf16=True)
+    close(d, want, tol, "gradient")
+
+
+def test_streams_graphs_and_repeats(sbw):
+    """Another stream, a captured step replayed with other work between, and the same bits every time."""
+    rng = np.random.default_rng(13)
+    B, V, K = 5, 20011, 1024
+    codes, s, _ = packed(rng, V, K, 128, "bf16")
+    codes = torch.from_numpy(codes).cuda()
+    hidden = torch.from_numpy(rng.standard_normal((B, K)).astype(np.float32)).to(torch.bfloat16).cuda() * 0.05
+    prev = torch.from_numpy(rng.integers(0, V, B).astype(np.int32)).cuda()
+    g = torch.full((B,), -0.2, device="cuda")
+
+    def step():
+        x = sbw.head_logits(hidden, codes, s)
+        ids, values = sbw.top_candidates(x, 40)
+        sbw.watermark_candidates(x, prev, ids, 15485863, 0.25, 2.0)
+        tokens, _ = sbw.watermark_argmax(x, prev, 15485863, 0.25, 0.0)
+        r = sbw.token_logprobs(x, tokens, 1.25, top=20)
+        d = sbw.token_logprobs_grad(x, tokens, r.stats, r.entropy, g, inv_temperature=1.25)
+        return [x, ids, values, tokens, *r, d]
+    first = [t.clone() for t in step()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = step()
+    side.synchronize()
+    explicit = sbw.token_logprobs(first[0], first[3], 1.25, top=20, stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(first, other))
+    assert all(torch.equal(a, b) for a, b in zip(first[4:10], explicit))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    noise = torch.randn(1 << 20, device="cuda")
+    for replay in range(4):
+        for t in held:
+            t.zero_()
+        noise.mul_(1.0001)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(first, held)), replay
+
+
+def test_candidates_feed_the_watermark(sbw):
+    """The top-k scheme from logits alone equals the oracle's on the same candidates."""
+    rng = np.random.default_rng(14)
+    B, V, k = 9, 30011, 40
+    x = logits(rng, B, V)
+    ctx = rng.integers(0, V, (B, 4)).astype(np.int32)
+    t = torch.from_numpy(x).cuda()
+    ids, _ = sbw.top_candidates(t, k)
+    sbw.watermark_candidates(t, torch.from_numpy(ctx).cuda(), ids, 15485863, 0.25, 2.0)
+    want = oracle.watermark_candidates(x, ids.cpu().numpy(), ctx, 15485863, 0.25, 2.0, "self_salt")
+    assert np.array_equal(t.cpu().numpy().view(np.uint32), want.view(np.uint32))
+
+
+def test_argument_errors(sbw):
+    x = torch.zeros((2, 300), device="cuda")
+    ids = torch.zeros(2, dtype=torch.int32, device="cuda")
+    lse = torch.zeros(2, device="cuda")
+    stats = torch.zeros((2, 2), device="cuda")
+    for bad in (lambda: sbw.token_logprobs(x[0], ids), lambda: sbw.token_logprobs(x.t(), ids),
+                lambda: sbw.token_logprobs(x, ids.long()), lambda: sbw.token_logprobs(x, ids[:1]),
+                lambda: sbw.token_logprobs(x, ids.cpu()), lambda: sbw.token_logprobs(x.cpu(), ids),
+                lambda: sbw.token_logprobs(x, ids, workspace=torch.zeros(0, dtype=torch.int32, device="cuda")),
+                lambda: sbw.token_logprobs_grad(x, ids, stats[:1], None, lse),
+                lambda: sbw.token_logprobs_grad(x, None, stats, None, lse), lambda: sbw.token_logprobs_grad(x, ids, None, None, lse),
+                lambda: sbw.token_logprobs_grad(x, ids, stats, None, lse, None, lse),
+                lambda: sbw.token_logprobs_grad(x, ids, stats, None, lse, out=x[:, :200]),
+                lambda: sbw.token_logprobs_grad(x, ids, stats, None, lse, out=x.to(torch.bfloat16)),
+                lambda: sbw.top_candidates(x, 4, ids=ids),
+                lambda: sbw.head_logits(x, ids, lse),
+                lambda: sbw.head_logits(x.to(torch.bfloat16), torch.zeros((3, 149), dtype=torch.uint8, device="cuda"),
+                                        torch.zeros((3, 2), device="cuda")),
+                lambda: sbw.head_logits(x[:, :256].to(torch.bfloat16),
+                                        torch.zeros((3, 128), dtype=torch.uint8, device="cuda"),
+                                        torch.zeros((3, 2), device="cpu"))):
+        with pytest.raises((ValueError, TypeError)):
+            bad()
+    with pytest.raises(TypeError):
+        sbw.token_logprobs(x.half(), ids)
+    for bad in (lambda: sbw.token_logprobs(x, ids, 0.0), lambda: sbw.token_logprobs(x, ids, top=1025),
+                lambda: sbw.token_logprobs(x, ids, top=-1),
+                lambda: sbw.top_candidates(x, 0), lambda: sbw.top_candidates(x, 1025),
+                lambda: sbw.top_candidates(x, 3, v_offset=-1), lambda: sbw.token_logprobs(x[:, :0], ids),
+                lambda: sbw.head_logits(x[:, :256].to(torch.bfloat16),
+                                        torch.zeros((3, 128), dtype=torch.uint8, device="cuda"),
+                                        torch.zeros((3, 1), device="cuda"))):
+        with pytest.raises(sbw.SbwError):
+            bad()
+
+
+def test_empty_batches(sbw):
+    x = torch.zeros((0, 300), device="cuda")
+    ids = torch.zeros(0, dtype=torch.int32, device="cuda")
+    r = sbw.token_logprobs(x, ids, top=3)
+    assert r.logprobs.shape == (0,) and r.top_ids.shape == (0, 3)
+    assert sbw.token_logprobs_grad(x, ids, r.stats, None, r.logprobs).shape == (0, 300)
+    assert sbw.top_candidates(x, 3)[0].shape == (0, 3)
+    codes, s = torch.zeros((7, 64), dtype=torch.uint8, device="cuda"), torch.zeros((7, 1), device="cuda")
+    assert sbw.head_logits(torch.zeros((0, 128), dtype=torch.bfloat16, device="cuda"), codes, s).shape == (0, 7)
+    assert sbw.head_logits(torch.zeros((2, 128), dtype=torch.bfloat16, device="cuda"), codes[:0], s[:0]).shape == (2, 0)
+    torch.cuda.synchronize()
