@@ -25,7 +25,7 @@ head_logits_kernel(const uint16_t* __restrict__ hidden, int64_t B, uint32_t K, i
       d = __builtin_fmaf(logit_of(h[1]), static_cast<float>(q >> 4) - 8.0f, d);
       total = __builtin_fmaf(d, logit_of(scales[v * (K / group) + 2 * c / group]), total);
     }
-    total = wave_reduce(total, sum);
+    total = wave_sum(total);
     if (lane == 0) put_logit(logits + b * row_stride + v, total);
   }
 }

@@ -11,11 +11,12 @@
 namespace sbw {
 namespace {
 
-constexpr int kRowThreads = 1024;
-constexpr int kRowWaves = kRowThreads / kWave;
 constexpr int kMostTokens = SBW_STEP_MAX_TOKENS;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.693147180559945309417f;
+// A score's floor inside the weighted sums: its exponential is 0, and 0 times it is 0 where 0
+// times -inf would be NaN (2^32 of them together still fit fp32).
+constexpr float kScoreFloor = -1e20f;
 
 __device__ __forceinline__ float logit_of(float x) { return x; }
 __device__ __forceinline__ float logit_of(uint16_t x) {
@@ -32,168 +33,512 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 __device__ __forceinline__ float logit_of_key(uint32_t key) {
   return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
 }
+constexpr uint32_t kLowestKey = 0x007FFFFFu;   // of -inf
 
 // (x - m) * inv_t - ln_s; halved on the way, so that only a result beyond fp32 is infinite.
 __device__ __forceinline__ float logprob_of(float x, float m, float inv_t, float ln_s) {
   return __builtin_fmaf((0.5f * x - 0.5f * m) * inv_t, 2.0f, -ln_s);
 }
 
+// Wave reductions by DPP moves: within rows of 16 lanes, then row broadcasts that carry the
+// result to lane 63, from where every lane gets it.  Lanes a move does not reach see the identity.
+template <int kCtrl, int kRowMask>
+__device__ __forceinline__ float dpp_moved(float v, float identity) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(identity), __float_as_int(v), kCtrl, kRowMask,
+                                                    0xF, false));
+}
 template <typename F>
-__device__ __forceinline__ float wave_reduce(float v, F f) {
+__device__ __forceinline__ float wave_reduce(float v, float identity, F f) {
+  v = f(v, dpp_moved<0xB1, 0xF>(v, identity));    // quad_perm [1,0,3,2]
+  v = f(v, dpp_moved<0x4E, 0xF>(v, identity));    // quad_perm [2,3,0,1]
+  v = f(v, dpp_moved<0x141, 0xF>(v, identity));   // row_half_mirror
+  v = f(v, dpp_moved<0x140, 0xF>(v, identity));   // row_mirror
+  v = f(v, dpp_moved<0x142, 0xA>(v, identity));   // row_bcast:15 into rows 1 and 3
+  v = f(v, dpp_moved<0x143, 0xC>(v, identity));   // row_bcast:31 into rows 2 and 3
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+// The larger of two, NaN if either is.
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float wave_largest(float v) {
+  return wave_reduce(v, -INFINITY, [](float a, float b) { return larger(a, b); });
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  return wave_reduce(v, 0.0f, [](float a, float b) { return a + b; });
+}
+
+// ---------------------------------------------------------------------------
+// Vectors of a row.  Vector j holds columns j * kPer .. j * kPer + kPer - 1; the row's last
+// one may be partial (its other places read as -inf and are not written).
+// ---------------------------------------------------------------------------
+template <typename T>
+constexpr uint32_t kPerOf = 16 / sizeof(T);
+
+__device__ __forceinline__ void set_elem(f32x4& v, int e, float x) { v[e] = x; }
+__device__ __forceinline__ void set_elem(u32x4& v, int e, uint16_t x) {
+  const uint32_t shift = (e & 1) * 16;
+  v[e >> 1] = (v[e >> 1] & ~(0xFFFFu << shift)) | static_cast<uint32_t>(x) << shift;
+}
+
+template <typename T>
+__device__ __forceinline__ typename VecOf<T>::Value load_whole(const T* row, uint32_t j) {
+  return *reinterpret_cast<const typename VecOf<T>::Memory*>(row + j * kPerOf<T>);
+}
+template <typename T>
+__device__ __forceinline__ typename VecOf<T>::Value load_any(const T* row, uint32_t V, uint32_t j) {
+  const uint32_t at = j * kPerOf<T>;
+  if (at + kPerOf<T> <= V) return load_whole(row, j);
+  typename VecOf<T>::Value v = lowest_vec(typename VecOf<T>::Value{});
 #pragma unroll
-  for (int d = kWave / 2; d > 0; d /= 2) v = f(v, __shfl_xor(v, d));
+  for (uint32_t e = 0; e < kPerOf<T>; ++e)
+    if (at + e < V) set_elem(v, e, row[at + e]);
   return v;
 }
 
-// The reduction of one value a thread over the workgroup, the same in every thread.
-template <typename F>
-__device__ __forceinline__ float row_reduce(float v, F f, float* slots) {
-  v = wave_reduce(v, f);
-  __syncthreads();
-  if (threadIdx.x % kWave == 0) slots[threadIdx.x / kWave] = v;
-  __syncthreads();
-  v = slots[0];
-  for (int w = 1; w < kRowWaves; ++w) v = f(v, slots[w]);
-  return v;
-}
-__device__ __forceinline__ uint32_t row_count(uint32_t v, uint32_t* slots) {
-#pragma unroll
-  for (int d = kWave / 2; d > 0; d /= 2) v += __shfl_xor(v, d);
-  __syncthreads();
-  if (threadIdx.x % kWave == 0) slots[threadIdx.x / kWave] = v;
-  __syncthreads();
-  v = 0;
-  for (int w = 0; w < kRowWaves; ++w) v += slots[w];
-  return v;
-}
-
-__device__ __forceinline__ float larger(float a, float b) { return a > b || a != a ? a : b; }
-__device__ __forceinline__ float sum(float a, float b) { return a + b; }
-
-// The k first logits of a row in order, as (key << 32 | ~column), in best[0 .. found).
-// Bisection over the keys for the k-th largest, then the larger logits and as many equal
-// ones, by column, as there is room for.
-struct Selection {
-  uint64_t raw[kMostTokens], best[kMostTokens];
-  uint32_t slots[kRowWaves], taken;
+// ---------------------------------------------------------------------------
+// Row statistics: the largest logit m, S and A of a part of a row (0 of each where m is
+// -inf), and their join.
+// ---------------------------------------------------------------------------
+struct Stats {
+  float m, S, A;
 };
-template <typename T>
-__device__ uint32_t select_row(const T* row, uint32_t V, uint32_t k, Selection& s) {
-  k = k < V ? k : V;
-  const uint32_t tid = threadIdx.x;
-  uint32_t at = 0;      // the largest key with k logits at or above it
-  for (uint32_t bit = 0x80000000u; bit != 0; bit >>= 1) {
-    uint32_t c = 0;
-    for (uint32_t v = tid; v < V; v += kRowThreads) c += order_key(logit_of(row[v])) >= (at | bit);
-    if (row_count(c, s.slots) >= k) at |= bit;
-  }
-  if (tid == 0) s.taken = 0;
-  __syncthreads();
-  for (uint32_t v = tid; v < V; v += kRowThreads) {
-    const uint32_t key = order_key(logit_of(row[v]));
-    if (key > at) s.raw[atomicAdd(&s.taken, 1u)] = static_cast<uint64_t>(key) << 32 | ~v;
-  }
-  __syncthreads();
-  uint32_t taken = s.taken;
-  for (uint32_t v0 = 0; v0 < V && taken < k; v0 += kRowThreads) {
-    const bool equal = v0 + tid < V && order_key(logit_of(row[v0 + tid])) == at;
-    const uint64_t mask = __ballot(equal);
-    __syncthreads();
-    if (tid % kWave == 0) s.slots[tid / kWave] = __popcll(mask);
-    __syncthreads();
-    uint32_t before = taken;
-    for (uint32_t w = 0; w < kRowWaves; ++w) {
-      if (w < tid / kWave) before += s.slots[w];
-      taken += s.slots[w];
-    }
-    before += __popcll(mask & ((uint64_t{1} << (tid % kWave)) - 1u));
-    if (equal && before < k) s.raw[before] = static_cast<uint64_t>(at) << 32 | ~(v0 + tid);
-  }
-  __syncthreads();
-  if (tid < k) {
-    const uint64_t mine = s.raw[tid];
-    uint32_t rank = 0;
-    for (uint32_t i = 0; i < k; ++i) rank += s.raw[i] > mine;
-    s.best[rank] = mine;
-  }
-  __syncthreads();
-  return k;
+__device__ __forceinline__ Stats join(Stats a, Stats b, float c) {
+  const float m = larger(a.m, b.m);
+  if (m == -INFINITY) return Stats{m, 0.0f, 0.0f};
+  const float da = (a.m - m) * c, db = (b.m - m) * c;
+  const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
+  return Stats{m, fa * a.S + fb * b.S,
+               fa * __builtin_fmaf(a.S, fmaxf(da, kScoreFloor), a.A) +
+                   fb * __builtin_fmaf(b.S, fmaxf(db, kScoreFloor), b.A)};
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads)
-token_logprobs_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride,
-                      const int32_t* __restrict__ tokens, uint32_t n, float inv_t, uint32_t top,
-                      float* __restrict__ logprobs, float* __restrict__ lse,
-                      float* __restrict__ entropy, float* __restrict__ stats,
-                      int32_t* __restrict__ top_ids, float* __restrict__ top_logprobs) {
-  __shared__ float slots[kRowWaves];
-  __shared__ Selection s;
+// The row's statistics from its parts, the same in every lane of the wave.
+__device__ __forceinline__ Stats join_parts(const Stats* parts, uint32_t count, float c) {
+  Stats s{-INFINITY, 0.0f, 0.0f};
+  for (uint32_t i = threadIdx.x % kWave; i < count; i += kWave) s = join(s, parts[i], c);
+  const float m = wave_largest(s.m);
+  const float d = s.m == -INFINITY ? kScoreFloor : (s.m - m) * c;
+  const float f = __builtin_amdgcn_exp2f(d);
+  s.A = wave_sum(f * __builtin_fmaf(s.S, fmaxf(d, kScoreFloor), s.A));
+  s.S = wave_sum(f * s.S);
+  s.m = m;
+  return s;
+}
+
+// The streaming pass: one read of every logit.  A workgroup takes a segment of kThreads * kVecs
+// vectors of a row, a lane kVecs of them, kThreads vectors apart.  A wave writes the statistics
+// of its part; with kTop a lane also writes the key of its largest logit (its group's maximum),
+// from which the selection finds the few groups that can hold one of the k largest.
+template <typename T, int kVecs, bool kStats, bool kTop>
+__global__ void __launch_bounds__(kThreads)
+row_pass_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride, float c,
+                Stats* __restrict__ parts, uint32_t* __restrict__ maxima) {
+  constexpr uint32_t kPer = kPerOf<T>;
+  const uint32_t j0 = blockIdx.x * (kThreads * kVecs) + threadIdx.x;
+  const bool whole = (blockIdx.x + 1) * (kThreads * kVecs) <= V / kPer;
+  for (int64_t b = blockIdx.y; b < B; b += gridDim.y) {
+    const T* row = logits + b * row_stride;
+    typename VecOf<T>::Value x[kVecs];
+    if (whole) {
+#pragma unroll
+      for (int u = 0; u < kVecs; ++u) x[u] = load_whole(row, j0 + u * kThreads);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kVecs; ++u) x[u] = load_any(row, V, j0 + u * kThreads);
+    }
+    float m = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u)
+#pragma unroll
+      for (uint32_t e = 0; e < kPer; ++e) m = larger(m, elem(x[u], e));
+    const int64_t segment = b * gridDim.x + blockIdx.x;
+    if (kTop) maxima[segment * kThreads + threadIdx.x] = order_key(m);
+    if (kStats) {
+      m = wave_largest(m);
+      const float base = m == -INFINITY ? 0.0f : m;
+      float S = 0.0f, A = 0.0f;
+#pragma unroll
+      for (int u = 0; u < kVecs; ++u)
+#pragma unroll
+        for (uint32_t e = 0; e < kPer; ++e) {
+          const float y = (elem(x[u], e) - base) * c;
+          const float p = __builtin_amdgcn_exp2f(y);
+          S += p;
+          A = __builtin_fmaf(p, fmaxf(y, kScoreFloor), A);
+        }
+      S = wave_sum(S);
+      A = wave_sum(A);
+      if (threadIdx.x % kWave == 0)
+        parts[segment * (kThreads / kWave) + threadIdx.x / kWave] = Stats{m, S, A};
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The k first logits of a row in order, by one workgroup, from the maxima of its groups.
+//
+// A threshold t with at least k group maxima at or above it has at least k logits there, all in
+// those groups; bisection stops at a t that leaves not many more than k groups.  Their logits
+// from t on are gathered as (key << 32 | ~column), which no two logits share, and sorted.
+// Where too many groups tie at t (a mask, equal logits), only what lies above t is gathered,
+// fewer than k groups, and the rest are the first columns that equal t.
+// ---------------------------------------------------------------------------
+constexpr uint32_t kListMost = 4096;     // gathered logits
+constexpr uint32_t kGroupsMost = 2048;   // listed groups
+constexpr uint32_t kRankMost = 256;      // gathered logits that are ordered by counting
+
+template <int kT>
+struct Selection {
+  uint64_t list[kListMost], best[kRankMost];
+  uint32_t groups[kGroupsMost], slots[2][kT / kWave];
+  uint32_t taken, listed;
+};
+
+// The sum over the workgroup of one number a wave; `turn` alternates.
+template <int kT>
+__device__ __forceinline__ uint32_t group_sum(uint32_t of_wave, Selection<kT>& s, uint32_t turn) {
+  if (threadIdx.x % kWave == 0) s.slots[turn & 1][threadIdx.x / kWave] = of_wave;
+  __syncthreads();
+  uint32_t n = 0;
+#pragma unroll
+  for (int w = 0; w < kT / kWave; ++w) n += s.slots[turn & 1][w];
+  return n;
+}
+
+// Bisection between two keys: lo has at least k at or above it, hi fewer.  In the logits' own
+// scale first, which is where they spread evenly, then bit by bit.
+struct Bisection {
+  uint32_t lo, hi, step = 0;
+  float reach = 1.0f;
+  __device__ __forceinline__ uint32_t middle() {
+    uint32_t mid = lo;
+    if (step < 16) {
+      const float a = logit_of_key(lo), z = logit_of_key(hi);
+      const float t = lo == kLowestKey ? z - __builtin_fmaf(0.5f, fabsf(z), 1.0f) * reach : 0.5f * a + 0.5f * z;
+      mid = order_key(t);
+      reach *= 4.0f;
+    }
+    ++step;
+    return mid > lo && mid < hi ? mid : lo + (hi - lo) / 2;
+  }
+};
+
+template <typename T, int kVecs, int kT>
+__device__ const uint64_t* select_row(const T* row, uint32_t V, const uint32_t* __restrict__ maxima,
+                                      uint32_t groups, uint32_t k, Selection<kT>& s) {
+  constexpr uint32_t kPer = kPerOf<T>;
+  constexpr int kHeld = 8192 / kT;
+  const uint32_t tid = threadIdx.x;
+  uint32_t turn = 0;
+  uint32_t held[kHeld];
+  uint32_t highest = 0;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    held[i] = tid + i * kT < groups ? maxima[tid + i * kT] : 0u;   // 0 is below every key
+    highest = max(highest, held[i]);
+  }
+  for (uint32_t g = tid + kHeld * kT; g < groups; g += kT) highest = max(highest, maxima[g]);
+#pragma unroll
+  for (int d = kWave / 2; d > 0; d /= 2) highest = max(highest, __shfl_xor(highest, d));
+  if (tid % kWave == 0) s.slots[turn & 1][tid / kWave] = highest;
+  if (tid == 0) s.taken = s.listed = 0;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kT / kWave; ++w) highest = max(highest, s.slots[turn & 1][w]);
+  ++turn;
+
+  const auto groups_from = [&](uint32_t t) {
+    uint32_t n = 0;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) n += __popcll(__ballot(held[i] >= t));
+    for (uint32_t g0 = kHeld * kT; g0 < groups; g0 += kT)
+      n += __popcll(__ballot(g0 + tid < groups && maxima[g0 + tid] >= t));
+    return group_sum(n, s, turn++);
+  };
+  k = min(k, V);
+  Bisection at{kLowestKey, highest};
+  uint32_t from = groups;                       // group maxima at or above at.lo
+  if (from > k) {
+    const uint32_t most = k + k / 4 + 16;
+    const uint32_t at_highest = groups_from(highest);
+    if (at_highest >= k) {
+      at.lo = highest;
+      from = at_highest;
+    }
+    while (from > most && at.hi - at.lo > 1) {
+      const uint32_t mid = at.middle();
+      const uint32_t n = groups_from(mid);
+      if (n >= k) {
+        at.lo = mid;
+        from = n;
+      } else {
+        at.hi = mid;
+      }
+    }
+  }
+  // `above`: what lies above at.lo only
+  bool above = from > kGroupsMost;
+  const auto wanted = [&](uint32_t key) { return above ? key > at.lo : key >= at.lo; };
+  const auto list_group = [&](uint32_t g, uint32_t key) {
+    if (wanted(key)) s.groups[atomicAdd(&s.listed, 1u)] = g;
+  };
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i)
+    if (tid + i * kT < groups) list_group(tid + i * kT, held[i]);
+  for (uint32_t g = tid + kHeld * kT; g < groups; g += kT) list_group(g, maxima[g]);
+  __syncthreads();
+
+  // every logit of the listed groups
+  const uint32_t items = s.listed * kVecs;
+  const auto each_listed = [&](auto&& f) {
+    for (uint32_t i = tid; i < items; i += kT) {
+      const uint32_t g = s.groups[i / kVecs];
+      const uint32_t j = g / kThreads * (kThreads * kVecs) + i % kVecs * kThreads + g % kThreads;
+      const auto x = load_any(row, V, j);
+#pragma unroll
+      for (uint32_t e = 0; e < kPer; ++e)
+        if (j * kPer + e < V) f(order_key(elem(x, e)), j * kPer + e);
+    }
+  };
+  const auto gather = [&] {
+    each_listed([&](uint32_t key, uint32_t column) {
+      if (!wanted(key)) return;
+      const uint32_t n = atomicAdd(&s.taken, 1u);
+      if (n < kListMost) s.list[n] = static_cast<uint64_t>(key) << 32 | ~column;
+    });
+    __syncthreads();
+  };
+  gather();
+  uint32_t taken = s.taken;
+  if (taken > kListMost) {
+    // the largest stand together in few groups: bisection over their logits
+    if (above) ++at.lo;
+    above = false;
+    at.hi = highest;
+    at.step = 0;
+    const auto logits_from = [&](uint32_t t) {
+      uint32_t n = 0;
+      each_listed([&](uint32_t key, uint32_t) { n += key >= t; });
+#pragma unroll
+      for (int d = kWave / 2; d > 0; d /= 2) n += __shfl_xor(n, d);
+      return group_sum(n, s, turn++);
+    };
+    const uint32_t at_highest = logits_from(highest);
+    if (at_highest >= k) {
+      at.lo = highest;
+      taken = at_highest;
+    }
+    while (taken > kListMost && at.hi - at.lo > 1) {
+      const uint32_t mid = at.middle();
+      const uint32_t n = logits_from(mid);
+      if (n >= k) {
+        at.lo = mid;
+        taken = n;
+      } else {
+        at.hi = mid;
+      }
+    }
+    above = taken > kListMost;
+    __syncthreads();
+    if (tid == 0) s.taken = 0;
+    __syncthreads();
+    gather();
+    taken = s.taken;
+  }
+  if (above) {
+    // the first columns that equal at.lo
+    for (uint32_t j0 = 0; taken < k && j0 * kPer < V; j0 += kT) {
+      const uint32_t j = j0 + tid;
+      uint32_t equal = 0;
+      if (j * kPer < V) {
+        const auto x = load_any(row, V, j);
+#pragma unroll
+        for (uint32_t e = 0; e < kPer; ++e)
+          equal |= static_cast<uint32_t>(j * kPer + e < V && order_key(elem(x, e)) == at.lo) << e;
+      }
+      uint32_t before = __popc(equal);
+#pragma unroll
+      for (int d = 1; d < kWave; d *= 2) {
+        const uint32_t n = __shfl_up(before, d);
+        if (tid % kWave >= static_cast<uint32_t>(d)) before += n;
+      }
+      const uint32_t of_wave = __shfl(before, kWave - 1);
+      if (tid % kWave == 0) s.slots[turn & 1][tid / kWave] = of_wave;
+      __syncthreads();
+      before += taken - __popc(equal);
+      for (uint32_t w = 0; w < kT / kWave; ++w) {
+        if (w < tid / kWave) before += s.slots[turn & 1][w];
+        taken += s.slots[turn & 1][w];
+      }
+      ++turn;
+      for (uint32_t e = 0; e < kPer; ++e)
+        if (equal >> e & 1u) {
+          if (before < k) s.list[before] = static_cast<uint64_t>(at.lo) << 32 | ~(j * kPer + e);
+          ++before;
+        }
+    }
+    taken = k;
+    __syncthreads();
+  }
+
+  if (taken <= kRankMost) {
+    for (uint32_t i = tid; i < taken; i += kT) {
+      const uint64_t mine = s.list[i];
+      uint32_t rank = 0;
+      for (uint32_t n = 0; n < taken; ++n) rank += s.list[n] > mine;
+      s.best[rank] = mine;
+    }
+    __syncthreads();
+    return s.best;
+  }
+  uint32_t size = 2 * kRankMost;
+  while (size < taken) size *= 2;
+  for (uint32_t i = taken + tid; i < size; i += kT) s.list[i] = 0;
+  for (uint32_t run = 2; run <= size; run *= 2)
+    for (uint32_t d = run / 2; d > 0; d /= 2) {
+      __syncthreads();
+      for (uint32_t i = tid; i < size / 2; i += kT) {
+        const uint32_t a = 2 * i - (i & (d - 1)), z = a + d;
+        const uint64_t p = s.list[a], q = s.list[z];
+        if ((p < q) == ((a & run) == 0)) {
+          s.list[a] = q;
+          s.list[z] = p;
+        }
+      }
+    }
+  __syncthreads();
+  return s.list;
+}
+
+constexpr int kFinishThreads = 1024;
+
+// After the pass: one workgroup a row joins the statistics, looks up the given tokens and
+// selects the alternatives.
+template <typename T, int kVecs>
+__global__ void __launch_bounds__(kFinishThreads)
+token_logprobs_top_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride,
+                          const int32_t* __restrict__ tokens, uint32_t n, float inv_t, uint32_t top,
+                          uint32_t segments, const Stats* __restrict__ parts,
+                          const uint32_t* __restrict__ maxima, float* __restrict__ logprobs,
+                          float* __restrict__ lse, float* __restrict__ entropy,
+                          float* __restrict__ stats, int32_t* __restrict__ top_ids,
+                          float* __restrict__ top_logprobs) {
+  __shared__ Selection<kFinishThreads> s;
   const uint32_t tid = threadIdx.x;
   for (int64_t b = blockIdx.x; b < B; b += gridDim.x) {
     const T* row = logits + b * row_stride;
-    float m = -INFINITY;
-    for (uint32_t v = tid; v < V; v += kRowThreads) m = larger(logit_of(row[v]), m);
-    m = row_reduce(m, larger, slots);
-    const bool empty = m == -INFINITY;
-    const float c = inv_t * kLog2e;
-    float S = 0.0f, A = 0.0f;
-    for (uint32_t v = tid; v < V; v += kRowThreads) {
-      const float y = empty ? -INFINITY : (logit_of(row[v]) - m) * c;
-      const float e = __builtin_amdgcn_exp2f(y);
-      S += e;
-      A = __builtin_fmaf(e, fmaxf(y, -1e30f), A);   // 0 * -inf is no part of the sum
-    }
-    S = row_reduce(S, sum, slots);
-    A = row_reduce(A, sum, slots);
-    const float ln_s = logf(S);
+    const uint32_t count = segments * (kThreads / kWave);
+    const Stats r = join_parts(parts + b * count, count, inv_t * kLog2e);
+    const float ln_s = logf(r.S);
+    const bool empty = r.m == -INFINITY;
     if (tid == 0) {
-      if (lse != nullptr) lse[b] = empty ? -INFINITY : __builtin_fmaf(m, inv_t, ln_s);
-      if (entropy != nullptr) entropy[b] = empty ? 0.0f : ln_s - kLn2 * (A / S);
-      if (stats != nullptr) stats[2 * b] = m, stats[2 * b + 1] = ln_s;
+      if (lse != nullptr) lse[b] = empty ? -INFINITY : __builtin_fmaf(r.m, inv_t, ln_s);
+      if (entropy != nullptr) entropy[b] = empty ? 0.0f : ln_s - kLn2 * (r.A / r.S);
+      if (stats != nullptr) stats[2 * b] = r.m, stats[2 * b + 1] = ln_s;
     }
-    for (uint32_t j = tid; j < n; j += kRowThreads) {
+    for (uint32_t j = tid; j < n; j += kFinishThreads) {
       const int32_t t = tokens[b * n + j];
       const bool token = t >= 0 && static_cast<uint32_t>(t) < V;
-      logprobs[b * n + j] = !token ? 0.0f : empty ? -INFINITY : logprob_of(logit_of(row[t]), m, inv_t, ln_s);
+      logprobs[b * n + j] = !token ? 0.0f : empty ? -INFINITY : logprob_of(logit_of(row[t]), r.m, inv_t, ln_s);
     }
-    if (top == 0) continue;
-    const uint32_t found = select_row(row, V, top, s);
-    for (uint32_t j = tid; j < top; j += kRowThreads) {
-      top_ids[b * top + j] = j < found ? static_cast<int32_t>(~static_cast<uint32_t>(s.best[j])) : -1;
-      if (top_logprobs != nullptr) {
-        const float x = j < found ? logit_of_key(static_cast<uint32_t>(s.best[j] >> 32)) : 0.0f;
-        top_logprobs[b * top + j] = j >= found || empty ? -INFINITY : logprob_of(x, m, inv_t, ln_s);
-      }
+    const uint64_t* best = select_row<T, kVecs>(row, V, maxima + b * segments * kThreads, segments * kThreads,
+                                                top, s);
+    for (uint32_t j = tid; j < top; j += kFinishThreads) {
+      const bool some = j < V;
+      top_ids[b * top + j] = some ? static_cast<int32_t>(~static_cast<uint32_t>(best[j])) : -1;
+      if (top_logprobs != nullptr)
+        top_logprobs[b * top + j] =
+            !some || empty ? -INFINITY
+                           : logprob_of(logit_of_key(static_cast<uint32_t>(best[j] >> 32)), r.m, inv_t, ln_s);
     }
     __syncthreads();
   }
 }
 
+// The same without alternatives: one wave a row.
 template <typename T>
-__global__ void __launch_bounds__(kRowThreads)
+__global__ void __launch_bounds__(kThreads)
+token_logprobs_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride,
+                      const int32_t* __restrict__ tokens, uint32_t n, float inv_t, uint32_t segments,
+                      const Stats* __restrict__ parts, float* __restrict__ logprobs,
+                      float* __restrict__ lse, float* __restrict__ entropy, float* __restrict__ stats) {
+  const uint32_t lane = threadIdx.x % kWave;
+  for (int64_t b = static_cast<int64_t>(blockIdx.x) * (kThreads / kWave) + threadIdx.x / kWave; b < B;
+       b += static_cast<int64_t>(gridDim.x) * (kThreads / kWave)) {
+    const uint32_t count = segments * (kThreads / kWave);
+    const Stats r = join_parts(parts + b * count, count, inv_t * kLog2e);
+    const float ln_s = logf(r.S);
+    const bool empty = r.m == -INFINITY;
+    if (lane == 0) {
+      if (lse != nullptr) lse[b] = empty ? -INFINITY : __builtin_fmaf(r.m, inv_t, ln_s);
+      if (entropy != nullptr) entropy[b] = empty ? 0.0f : ln_s - kLn2 * (r.A / r.S);
+      if (stats != nullptr) stats[2 * b] = r.m, stats[2 * b + 1] = ln_s;
+    }
+    for (uint32_t j = lane; j < n; j += kWave) {
+      const int32_t t = tokens[b * n + j];
+      const bool token = t >= 0 && static_cast<uint32_t>(t) < V;
+      logprobs[b * n + j] = !token ? 0.0f
+                            : empty ? -INFINITY
+                                    : logprob_of(logit_of(logits[b * row_stride + t]), r.m, inv_t, ln_s);
+    }
+  }
+}
+
+template <typename T, int kVecs>
+__global__ void __launch_bounds__(kFinishThreads)
 top_candidates_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride,
-                      uint32_t vbase, uint32_t k, int32_t* __restrict__ ids,
+                      uint32_t vbase, uint32_t k, uint32_t segments,
+                      const uint32_t* __restrict__ maxima, int32_t* __restrict__ ids,
                       float* __restrict__ values) {
-  __shared__ Selection s;
+  __shared__ Selection<kFinishThreads> s;
   for (int64_t b = blockIdx.x; b < B; b += gridDim.x) {
-    const uint32_t found = select_row(logits + b * row_stride, V, k, s);
-    for (uint32_t j = threadIdx.x; j < k; j += kRowThreads) {
-      ids[b * k + j] = j < found ? static_cast<int32_t>(vbase + ~static_cast<uint32_t>(s.best[j])) : -1;
+    const uint64_t* best = select_row<T, kVecs>(logits + b * row_stride, V, maxima + b * segments * kThreads,
+                                                segments * kThreads, k, s);
+    for (uint32_t j = threadIdx.x; j < k; j += kFinishThreads) {
+      ids[b * k + j] = j < V ? static_cast<int32_t>(vbase + ~static_cast<uint32_t>(best[j])) : -1;
       if (values != nullptr)
-        values[b * k + j] = j < found ? logit_of_key(static_cast<uint32_t>(s.best[j] >> 32)) : -INFINITY;
+        values[b * k + j] = j < V ? logit_of_key(static_cast<uint32_t>(best[j] >> 32)) : -INFINITY;
     }
     __syncthreads();
   }
 }
 
+// ---------------------------------------------------------------------------
+// Gradient: one read and one write of every logit.
+// ---------------------------------------------------------------------------
 __device__ __forceinline__ void put_logit(float* p, float x) { *p = x; }
 __device__ __forceinline__ void put_logit(uint16_t* p, float x) {
   *p = static_cast<uint16_t>(to_bf16x2(x, 0.0f));
 }
-
+__device__ __forceinline__ f32x4 packed(const float (&d)[4]) { return f32x4{d[0], d[1], d[2], d[3]}; }
+__device__ __forceinline__ u32x4 packed(const float (&d)[8]) {
+  return u32x4{to_bf16x2(d[0], d[1]), to_bf16x2(d[2], d[3]), to_bf16x2(d[4], d[5]), to_bf16x2(d[6], d[7])};
+}
 template <typename T>
-__global__ void __launch_bounds__(kRowThreads)
+__device__ __forceinline__ void store_any(T* row, uint32_t V, uint32_t j, typename VecOf<T>::Value v) {
+  const uint32_t at = j * kPerOf<T>;
+  if (at + kPerOf<T> <= V) {
+    *reinterpret_cast<typename VecOf<T>::Memory*>(row + at) = v;
+    return;
+  }
+#pragma unroll
+  for (uint32_t e = 0; e < kPerOf<T>; ++e)
+    if (at + e < V) put_logit(row + at + e, elem(v, e));
+}
+
+// What a row's gradient is made of.  For column v with score y = (x_v - m) inv_t and
+// log p = y - ln S:  d_v = p (share - slope log p) + inv_t * (the gradients of the tokens v),
+// share = inv_t (g_lse - sum_j g_j - g_H H), slope = inv_t g_H.
+struct RowGradient {
+  float m, ln_s, inv_t, share, slope;
+  __device__ __forceinline__ float operator()(float x) const {
+    const float y = __builtin_fmaf(x - m, inv_t, -ln_s);
+    const float p = __builtin_amdgcn_exp2f(y * kLog2e);
+    return p * __builtin_fmaf(-slope, fmaxf(y, kScoreFloor), share);
+  }
+};
+
+template <typename T, int kVecs, bool kOne>
+__global__ void __launch_bounds__(kThreads)
 token_logprobs_grad_kernel(const T* logits, int64_t B, uint32_t V, int64_t row_stride,
                            const int32_t* __restrict__ tokens, uint32_t n,
                            const float* __restrict__ stats, const float* __restrict__ entropy,
@@ -201,28 +546,185 @@ token_logprobs_grad_kernel(const T* logits, int64_t B, uint32_t V, int64_t row_s
                            const float* __restrict__ grad_lse,
                            const float* __restrict__ grad_entropy, float inv_t, T* grad,
                            int64_t grad_stride) {
-  for (int64_t b = blockIdx.x; b < B; b += gridDim.x) {
+  constexpr uint32_t kPer = kPerOf<T>;
+  constexpr int kOwn = kOne ? 1 : kMostTokens / kThreads;   // tokens a lane looks after
+  __shared__ int32_t ids[kOne ? 1 : kMostTokens];
+  __shared__ float gs[kOne ? 1 : kMostTokens];
+  const uint32_t j0 = blockIdx.x * (kThreads * kVecs) + threadIdx.x;
+  const bool whole = (blockIdx.x + 1) * (kThreads * kVecs) <= V / kPer;
+  const uint32_t first = blockIdx.x * (kThreads * kVecs * kPer);   // the segment's columns
+  for (int64_t b = blockIdx.y; b < B; b += gridDim.y) {
     const T* row = logits + b * row_stride;
     T* out = grad + b * grad_stride;
-    const float m = stats[2 * b], ln_s = stats[2 * b + 1];
-    const float gh = grad_entropy != nullptr ? grad_entropy[b] : 0.0f;
-    float share = grad_lse != nullptr ? grad_lse[b] : 0.0f;
-    if (grad_entropy != nullptr) share -= gh * entropy[b];
-    const int32_t* ids = tokens + b * n;
-    const float* g = grad_logprobs + b * n;
-    if (grad_logprobs != nullptr)
-      for (uint32_t j = 0; j < n; ++j)
-        if (ids[j] >= 0 && static_cast<uint32_t>(ids[j]) < V) share -= g[j];
-    for (uint32_t v = threadIdx.x; v < V; v += kRowThreads) {
-      const float y = __builtin_fmaf(logit_of(row[v]) - m, inv_t, -ln_s);
-      const float p = __builtin_amdgcn_exp2f(y * kLog2e);
-      float d = p * __builtin_fmaf(-gh, fmaxf(y, -1e30f), share);
-      if (grad_logprobs != nullptr)
-        for (uint32_t j = 0; j < n; ++j)
-          if (static_cast<uint32_t>(ids[j]) == v) d += g[j];
-      put_logit(out + v, m == -INFINITY ? 0.0f : d * inv_t);
+    typename VecOf<T>::Value x[kVecs];
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u)
+      x[u] = whole ? load_whole(row, j0 + u * kThreads) : load_any(row, V, j0 + u * kThreads);
+
+    RowGradient r{stats[2 * b], stats[2 * b + 1], inv_t, 0.0f, 0.0f};
+    if (grad_lse != nullptr) r.share = grad_lse[b];
+    if (grad_entropy != nullptr) {
+      r.slope = grad_entropy[b];
+      r.share = __builtin_fmaf(-r.slope, entropy[b], r.share);
+      r.slope *= inv_t;
+    }
+    uint32_t token = 0xFFFFFFFFu;
+    float g = 0.0f;
+    float own[kOwn];
+    if (kOne) {
+      token = static_cast<uint32_t>(tokens[b]);
+      g = token < V ? grad_logprobs[b] : 0.0f;
+      r.share = (r.share - g) * inv_t;
+    } else {
+      float total = 0.0f;
+      for (uint32_t i = threadIdx.x % kWave; i < n; i += kWave)
+        if (static_cast<uint32_t>(tokens[b * n + i]) < V) total += grad_logprobs[b * n + i];
+      r.share = (r.share - wave_sum(total)) * inv_t;
+      __syncthreads();     // the last row's tokens are done with
+      for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
+        ids[i] = tokens[b * n + i];
+        gs[i] = grad_logprobs[b * n + i];
+      }
+      __syncthreads();
+      // The segment's tokens, each with all its gradients at its first place, before anything is
+      // written (the gradient may replace the logits).
+#pragma unroll
+      for (int q = 0; q < kOwn; ++q) {
+        const uint32_t i = threadIdx.x + q * kThreads;
+        own[q] = NAN;
+        if (i >= n) continue;
+        const uint32_t t = static_cast<uint32_t>(ids[i]);
+        if (t >= V || t - first >= kThreads * kVecs * kPer) continue;
+        own[q] = r(logit_of(row[t]));
+      }
+      __syncthreads();
+    }
+    const bool empty = r.m == -INFINITY;
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) {
+      const uint32_t j = j0 + u * kThreads;
+      float d[kPer];
+#pragma unroll
+      for (uint32_t e = 0; e < kPer; ++e) {
+        d[e] = r(elem(x[u], e));
+        if (kOne && j * kPer + e == token) d[e] = __builtin_fmaf(g, inv_t, d[e]);
+        if (empty) d[e] = 0.0f;
+      }
+      store_any(out, V, j, packed(d));
+    }
+    if (kOne || empty) continue;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kOwn; ++q) {
+      const uint32_t i = threadIdx.x + q * kThreads;
+      if (i >= n) continue;
+      const int32_t t = ids[i];
+      if (static_cast<uint32_t>(t) >= V || static_cast<uint32_t>(t) - first >= kThreads * kVecs * kPer) continue;
+      bool again = false;
+      for (uint32_t o = 0; o < i && !again; ++o) again = ids[o] == t;
+      if (again) continue;
+      float of_token = 0.0f;
+      for (uint32_t o = i; o < n; ++o)
+        if (ids[o] == t) of_token += gs[o];
+      put_logit(out + t, __builtin_fmaf(of_token, inv_t, own[q]));
     }
   }
+}
+
+// ---------------------------------------------------------------------------
+// Launch shapes.
+// ---------------------------------------------------------------------------
+// Vectors of a lane in the pass: the long form reads 32 logits, the short one 8.
+template <typename T>
+constexpr int kLongVecs = sizeof(T) == 4 ? 8 : 4;
+template <typename T>
+constexpr int kShortVecs = sizeof(T) == 4 ? 2 : 1;
+constexpr int64_t kLongSegment = kThreads * 32, kShortSegment = kThreads * 8;
+
+// Whether the pass takes the long form: rows that make enough workgroups of it, and enough
+// groups for the selection to leave few.
+bool long_segments(int64_t B, int64_t V, int64_t top) {
+  return B * ((V + kLongSegment - 1) / kLongSegment) >= 512 && V / 32 >= 4 * top;
+}
+int64_t segments_of(int64_t B, int64_t V, int64_t top) {
+  const int64_t size = long_segments(B, V, top) ? kLongSegment : kShortSegment;
+  return (V + size - 1) / size;
+}
+// uint64 elements of the workspace a segment takes: the statistics of its waves, a key a lane
+constexpr int64_t kPartElems = sizeof(Stats) * (kThreads / kWave) / 8;
+constexpr int64_t kMaximaElems = kThreads / 2;
+
+template <typename T, bool kStats, bool kTop>
+void launch_pass(const T* logits, int64_t B, uint32_t V, int64_t row_stride, float c, int64_t top, uint64_t* parts,
+                 uint64_t* maxima, hipStream_t stream) {
+  const dim3 grid(static_cast<uint32_t>(segments_of(B, V, top)),
+                  static_cast<uint32_t>(B < kMaxGridY ? B : kMaxGridY));
+  auto* p = reinterpret_cast<Stats*>(parts);
+  auto* m = reinterpret_cast<uint32_t*>(maxima);
+  if (long_segments(B, V, top))
+    row_pass_kernel<T, kLongVecs<T>, kStats, kTop><<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, c, p, m);
+  else
+    row_pass_kernel<T, kShortVecs<T>, kStats, kTop><<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, c, p, m);
+}
+
+template <typename T>
+void launch_logprobs(const void* logits_, int64_t B, uint32_t V, int64_t row_stride, const int32_t* tokens,
+                     uint32_t n, float inv_t, uint32_t top, float* logprobs, float* lse, float* entropy,
+                     float* stats, int32_t* top_ids, float* top_logprobs, uint64_t* workspace, hipStream_t stream) {
+  const T* logits = static_cast<const T*>(logits_);
+  const auto segments = static_cast<uint32_t>(segments_of(B, V, top));
+  uint64_t* maxima = workspace + B * segments * kPartElems;
+  const auto* parts = reinterpret_cast<const Stats*>(workspace);
+  const float c = inv_t * kLog2e;
+  if (top == 0) {
+    launch_pass<T, true, false>(logits, B, V, row_stride, c, top, workspace, nullptr, stream);
+    const dim3 grid(static_cast<uint32_t>(grid_for((B + 3) / 4)));
+    token_logprobs_kernel<T><<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, tokens, n, inv_t, segments,
+                                                             parts, logprobs, lse, entropy, stats);
+    return;
+  }
+  launch_pass<T, true, true>(logits, B, V, row_stride, c, top, workspace, maxima, stream);
+  const dim3 grid(static_cast<uint32_t>(grid_for(B)));
+  const auto launch = [&](auto* kernel) {
+    kernel<<<grid, kFinishThreads, 0, stream>>>(logits, B, V, row_stride, tokens, n, inv_t, top, segments, parts,
+                                                 reinterpret_cast<const uint32_t*>(maxima), logprobs, lse, entropy,
+                                                 stats, top_ids, top_logprobs);
+  };
+  if (long_segments(B, V, top)) launch(token_logprobs_top_kernel<T, kLongVecs<T>>);
+  else launch(token_logprobs_top_kernel<T, kShortVecs<T>>);
+}
+
+template <typename T>
+void launch_candidates(const void* logits_, int64_t B, uint32_t V, int64_t row_stride, uint32_t vbase, uint32_t k,
+                       int32_t* ids, float* values, uint64_t* workspace, hipStream_t stream) {
+  const T* logits = static_cast<const T*>(logits_);
+  const auto segments = static_cast<uint32_t>(segments_of(B, V, k));
+  launch_pass<T, false, true>(logits, B, V, row_stride, 1.0f, k, nullptr, workspace, stream);
+  const dim3 grid(static_cast<uint32_t>(grid_for(B)));
+  const auto launch = [&](auto* kernel) {
+    kernel<<<grid, kFinishThreads, 0, stream>>>(logits, B, V, row_stride, vbase, k, segments,
+                                                 reinterpret_cast<const uint32_t*>(workspace), ids, values);
+  };
+  if (long_segments(B, V, k)) launch(top_candidates_kernel<T, kLongVecs<T>>);
+  else launch(top_candidates_kernel<T, kShortVecs<T>>);
+}
+
+template <typename T>
+void launch_grad(const void* logits, int64_t B, uint32_t V, int64_t row_stride, const int32_t* tokens, uint32_t n,
+                 const float* stats, const float* entropy, const float* grad_logprobs, const float* grad_lse,
+                 const float* grad_entropy, float inv_t, void* grad, int64_t grad_stride, hipStream_t stream) {
+  constexpr int kVecs = sizeof(T) == 4 ? 4 : 2;
+  constexpr int64_t kSegment = kThreads * kVecs * kPerOf<T>;
+  const dim3 grid(static_cast<uint32_t>((V + kSegment - 1) / kSegment),
+                  static_cast<uint32_t>(B < kMaxGridY ? B : kMaxGridY));
+  if (grad_logprobs == nullptr) n = 0;
+  const auto launch = [&](auto* kernel) {
+    kernel<<<grid, kThreads, 0, stream>>>(static_cast<const T*>(logits), B, V, row_stride, tokens, n, stats, entropy,
+                                           grad_logprobs, grad_lse, grad_entropy, inv_t, static_cast<T*>(grad),
+                                           grad_stride);
+  };
+  if (n == 1) launch(token_logprobs_grad_kernel<T, kVecs, true>);
+  else launch(token_logprobs_grad_kernel<T, kVecs, false>);
 }
 
 constexpr int64_t kMostColumns = kMaxTokenIds - 65536;   // column + a workgroup's stride fits 32 bits
@@ -247,13 +749,13 @@ sbw_status_t check_most(int64_t count, int64_t least) {
 extern "C" {
 
 int64_t sbw_token_logprobs_workspace(int64_t B, int64_t V, int64_t top) {
-  (void)B, (void)V, (void)top;
-  return 0;
+  if (B <= 0 || V <= 0 || V > kMostColumns || top < 0 || top > kMostTokens) return 0;
+  return B * segments_of(B, V, top) * (kPartElems + (top > 0 ? kMaximaElems : 0));
 }
 
 int64_t sbw_top_candidates_workspace(int64_t B, int64_t V, int64_t k) {
-  (void)B, (void)V, (void)k;
-  return 0;
+  if (B <= 0 || V <= 0 || V > kMostColumns || k < 1 || k > kMostTokens) return 0;
+  return B * segments_of(B, V, k) * kMaximaElems;
 }
 
 sbw_status_t sbw_token_logprobs(const void* logits, sbw_dtype_t dtype, int64_t B, int64_t V,
@@ -273,17 +775,9 @@ sbw_status_t sbw_token_logprobs(const void* logits, sbw_dtype_t dtype, int64_t B
   s = check_device();
   if (s != SBW_OK) return s;
   const auto st = static_cast<hipStream_t>(stream);
-  const dim3 grid(static_cast<uint32_t>(grid_for(B)));
-  if (dtype == SBW_F32)
-    token_logprobs_kernel<float><<<grid, kRowThreads, 0, st>>>(
-        static_cast<const float*>(logits), B, static_cast<uint32_t>(V), row_stride, tokens,
-        static_cast<uint32_t>(n), inv_temperature, static_cast<uint32_t>(top), logprobs, lse, entropy,
-        stats, top_ids, top_logprobs);
-  else
-    token_logprobs_kernel<uint16_t><<<grid, kRowThreads, 0, st>>>(
-        static_cast<const uint16_t*>(logits), B, static_cast<uint32_t>(V), row_stride, tokens,
-        static_cast<uint32_t>(n), inv_temperature, static_cast<uint32_t>(top), logprobs, lse, entropy,
-        stats, top_ids, top_logprobs);
+  auto* launch = dtype == SBW_F32 ? launch_logprobs<float> : launch_logprobs<uint16_t>;
+  launch(logits, B, static_cast<uint32_t>(V), row_stride, tokens, static_cast<uint32_t>(n), inv_temperature,
+         static_cast<uint32_t>(top), logprobs, lse, entropy, stats, top_ids, top_logprobs, workspace, st);
   return after_launch();
 }
 
@@ -306,17 +800,9 @@ sbw_status_t sbw_token_logprobs_grad(const void* logits, sbw_dtype_t dtype, int6
   s = check_device();
   if (s != SBW_OK) return s;
   const auto st = static_cast<hipStream_t>(stream);
-  const dim3 grid(static_cast<uint32_t>(grid_for(B)));
-  if (dtype == SBW_F32)
-    token_logprobs_grad_kernel<float><<<grid, kRowThreads, 0, st>>>(
-        static_cast<const float*>(logits), B, static_cast<uint32_t>(V), row_stride, tokens,
-        static_cast<uint32_t>(n), stats, entropy, grad_logprobs, grad_lse, grad_entropy, inv_temperature,
-        static_cast<float*>(grad), grad_stride);
-  else
-    token_logprobs_grad_kernel<uint16_t><<<grid, kRowThreads, 0, st>>>(
-        static_cast<const uint16_t*>(logits), B, static_cast<uint32_t>(V), row_stride, tokens,
-        static_cast<uint32_t>(n), stats, entropy, grad_logprobs, grad_lse, grad_entropy, inv_temperature,
-        static_cast<uint16_t*>(grad), grad_stride);
+  auto* launch = dtype == SBW_F32 ? launch_grad<float> : launch_grad<uint16_t>;
+  launch(logits, B, static_cast<uint32_t>(V), row_stride, tokens, static_cast<uint32_t>(n), stats, entropy,
+         grad_logprobs, grad_lse, grad_entropy, inv_temperature, grad, grad_stride, st);
   return after_launch();
 }
 
@@ -334,16 +820,9 @@ sbw_status_t sbw_top_candidates(const void* logits, sbw_dtype_t dtype, int64_t B
   s = check_device();
   if (s != SBW_OK) return s;
   const auto st = static_cast<hipStream_t>(stream);
-  const dim3 grid(static_cast<uint32_t>(grid_for(B)));
-  const auto vbase = static_cast<uint32_t>(v_offset);
-  if (dtype == SBW_F32)
-    top_candidates_kernel<float><<<grid, kRowThreads, 0, st>>>(
-        static_cast<const float*>(logits), B, static_cast<uint32_t>(V), row_stride, vbase,
-        static_cast<uint32_t>(k), ids, values);
-  else
-    top_candidates_kernel<uint16_t><<<grid, kRowThreads, 0, st>>>(
-        static_cast<const uint16_t*>(logits), B, static_cast<uint32_t>(V), row_stride, vbase,
-        static_cast<uint32_t>(k), ids, values);
+  auto* launch = dtype == SBW_F32 ? launch_candidates<float> : launch_candidates<uint16_t>;
+  launch(logits, B, static_cast<uint32_t>(V), row_stride, static_cast<uint32_t>(v_offset), static_cast<uint32_t>(k),
+         ids, values, workspace, st);
   return after_launch();
 }
 
