@@ -20,6 +20,7 @@
 #include <exception>
 
 #include "sbw.h"
+#include "sbw_step.h"
 
 namespace {
 
@@ -318,6 +319,186 @@ PyObject* detect(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- the operators of sbw_step.h ---------------------------------------------------------
+
+// A tuple of `count` new objects (an array whose unset places are None); all or nothing.
+template <size_t count>
+PyObject* tuple_of(PyObject* (&objects)[count]) {
+  PyObject* t = PyTuple_New(count);
+  for (size_t i = 0; i < count; ++i) {
+    if (objects[i] == nullptr) {
+      Py_INCREF(Py_None);
+      objects[i] = Py_None;
+    }
+    if (t != nullptr) PyTuple_SET_ITEM(t, i, objects[i]);
+    else Py_DECREF(objects[i]);
+  }
+  return t;
+}
+
+// logits and, unless None, tokens [rows] or [rows, n]
+bool tokens_call(PyObject* logits, PyObject* tokens, Call* c, const Tensor** ids, int64_t* n) {
+  if (!matrix_of(logits, c) || (c->rows > 1 && c->row_stride < c->columns)) return false;
+  if (c->matrix->scalar_type() == at::kBFloat16) c->dtype = SBW_BF16;
+  else if (c->matrix->scalar_type() != at::kFloat) return false;
+  *ids = nullptr;
+  *n = 0;
+  if (tokens == Py_None) return true;
+  const Tensor* t = packed_of(tokens, at::kInt, c->device);
+  if (t == nullptr || t->dim() < 1 || t->dim() > 2 || t->size(0) != c->rows) return false;
+  *ids = t;
+  *n = t->dim() == 2 ? t->size(1) : 1;
+  return true;
+}
+
+// None (a null pointer), or a packed float tensor of this shape.
+bool floats_of(PyObject* o, at::IntArrayRef shape, const Call& c, const float** out) {
+  *out = nullptr;
+  if (o == Py_None) return true;
+  const Tensor* t = packed_of(o, at::kFloat, c.device);
+  if (t == nullptr || t->sizes() != shape) return false;
+  *out = static_cast<const float*>(t->data_ptr());
+  return true;
+}
+
+// token_logprobs(logits, tokens or None, inv_temperature, top): the six outputs
+PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  return guarded([&]() -> PyObject* {
+    Call c;
+    const Tensor* ids;
+    int64_t n, top;
+    double inv_t;
+    if (count != 4 || !tokens_call(a[0], a[1], &c, &ids, &n) || !number(a[2], &inv_t) || !integer(a[3], &top) ||
+        top < 0)
+      Py_RETURN_NONE;
+    const auto floats = c.matrix->options().dtype(at::kFloat).requires_grad(false);
+    const auto ints = floats.dtype(at::kInt);
+    const int64_t need = sbw_token_logprobs_workspace(c.rows, c.columns, top);
+    Tensor workspace = at::empty({need}, floats.dtype(at::kLong));
+    Tensor logprobs, top_ids, top_logprobs;
+    if (ids != nullptr) logprobs = at::empty(ids->sizes(), floats);
+    Tensor lse = at::empty({c.rows}, floats), entropy = at::empty({c.rows}, floats);
+    Tensor stats = at::empty({c.rows, 2}, floats);
+    if (top > 0) {
+      top_ids = at::empty({c.rows, top}, ints);
+      top_logprobs = at::empty({c.rows, top}, floats);
+    }
+    const void* logits = c.matrix->data_ptr();
+    const auto* token = ids != nullptr ? static_cast<const int32_t*>(ids->data_ptr()) : nullptr;
+    const auto address = [](const Tensor& t) { return t.defined() ? static_cast<float*>(t.data_ptr()) : nullptr; };
+    float *lp = address(logprobs), *l = address(lse), *h = address(entropy), *st = address(stats);
+    float* tl = address(top_logprobs);
+    auto* ti = top > 0 ? static_cast<int32_t*>(top_ids.data_ptr()) : nullptr;
+    auto* scratch = static_cast<uint64_t*>(workspace.data_ptr());
+    void* stream = stream_of(c);
+    PyObject* objects[6] = {};
+    const Tensor* outputs[6] = {&logprobs, &lse, &entropy, &stats, &top_ids, &top_logprobs};
+    for (int i = 0; i < 6; ++i)
+      if (outputs[i]->defined()) objects[i] = THPVariable_Wrap(*outputs[i]);
+    PyObject* result = tuple_of(objects);
+    if (result == nullptr) return nullptr;
+    return outputs_or_status(result, unlocked([&] {
+      return sbw_token_logprobs(logits, c.dtype, c.rows, c.columns, c.row_stride, token, n,
+                                static_cast<float>(inv_t), top, lp, l, h, st, ti, tl, scratch, stream);
+    }));
+  });
+}
+
+// token_logprobs_grad(logits, tokens or None, stats, entropy, grad_logprobs, grad_lse, grad_entropy (each or
+//                     None), inv_temperature): the gradient
+PyObject* token_logprobs_grad(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  return guarded([&]() -> PyObject* {
+    Call c;
+    const Tensor* ids;
+    int64_t n;
+    double inv_t;
+    const float *stats, *entropy, *g, *g_lse, *g_entropy;
+    if (count != 8 || !tokens_call(a[0], a[1], &c, &ids, &n) || a[2] == Py_None ||
+        (a[4] != Py_None && ids == nullptr) || !floats_of(a[2], {c.rows, 2}, c, &stats) ||
+        !floats_of(a[3], {c.rows}, c, &entropy) ||
+        !floats_of(a[4], ids != nullptr ? ids->sizes() : at::IntArrayRef(), c, &g) ||
+        !floats_of(a[5], {c.rows}, c, &g_lse) || !floats_of(a[6], {c.rows}, c, &g_entropy) || !number(a[7], &inv_t) ||
+        (g_entropy != nullptr && entropy == nullptr))
+      Py_RETURN_NONE;
+    Tensor grad = at::empty({c.rows, c.columns}, c.matrix->options().requires_grad(false));
+    const void* logits = c.matrix->data_ptr();
+    const auto* token = ids != nullptr ? static_cast<const int32_t*>(ids->data_ptr()) : nullptr;
+    void* out = grad.data_ptr();
+    void* stream = stream_of(c);
+    PyObject* result = THPVariable_Wrap(grad);
+    if (result == nullptr) return nullptr;
+    return outputs_or_status(result, unlocked([&] {
+      return sbw_token_logprobs_grad(logits, c.dtype, c.rows, c.columns, c.row_stride, token, n, stats, entropy, g,
+                                     g_lse, g_entropy, static_cast<float>(inv_t), out, c.columns, stream);
+    }));
+  });
+}
+
+// top_candidates(logits, k, v_offset): ids and values
+PyObject* top_candidates(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  return guarded([&]() -> PyObject* {
+    Call c;
+    const Tensor* none;
+    int64_t n, k, v_offset;
+    if (count != 3 || !tokens_call(a[0], Py_None, &c, &none, &n) || !integer(a[1], &k) || k < 1 ||
+        !integer(a[2], &v_offset))
+      Py_RETURN_NONE;
+    const int64_t need = sbw_top_candidates_workspace(c.rows, c.columns, k);
+    const auto floats = c.matrix->options().dtype(at::kFloat).requires_grad(false);
+    Tensor workspace = at::empty({need}, floats.dtype(at::kLong));
+    Tensor ids = at::empty({c.rows, k}, floats.dtype(at::kInt)), values = at::empty({c.rows, k}, floats);
+    const void* logits = c.matrix->data_ptr();
+    auto* id = static_cast<int32_t*>(ids.data_ptr());
+    auto* value = static_cast<float*>(values.data_ptr());
+    auto* scratch = static_cast<uint64_t*>(workspace.data_ptr());
+    void* stream = stream_of(c);
+    PyObject* result = tuple_of(THPVariable_Wrap(ids), THPVariable_Wrap(values), nullptr);
+    if (result == nullptr) return nullptr;
+    return outputs_or_status(result, unlocked([&] {
+      return sbw_top_candidates(logits, c.dtype, c.rows, c.columns, c.row_stride, v_offset, k, id, value, scratch,
+                                stream);
+    }));
+  });
+}
+
+// head_logits(hidden, codes, scales, whether the logits are bfloat16): the logits
+PyObject* head_logits(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  return guarded([&]() -> PyObject* {
+    Call c;
+    if (count != 4 || !matrix_of(a[0], &c) || c.matrix->scalar_type() != at::kBFloat16 || !PyBool_Check(a[3]) ||
+        (c.rows > 1 && c.row_stride < c.columns))
+      Py_RETURN_NONE;
+    const Tensor* codes = packed_of(a[1], at::kByte, c.device);
+    if (codes == nullptr || codes->dim() != 2 || 2 * codes->size(1) != c.columns || codes->size(0) == 0)
+      Py_RETURN_NONE;
+    const int64_t V = codes->size(0);
+    const Tensor* scales = packed_of(a[2], at::kFloat, c.device);
+    sbw_dtype_t scale_dtype = SBW_F32;
+    if (scales == nullptr) {
+      scales = packed_of(a[2], at::kBFloat16, c.device);
+      scale_dtype = SBW_BF16;
+    }
+    if (scales == nullptr || scales->dim() != 2 || scales->size(0) != V || scales->size(1) == 0 ||
+        c.columns % scales->size(1) != 0)
+      Py_RETURN_NONE;
+    const bool bf16 = a[3] == Py_True;
+    Tensor logits = at::empty({c.rows, V}, c.matrix->options().dtype(bf16 ? at::kBFloat16 : at::kFloat)
+                                               .requires_grad(false));
+    const void* hidden = c.matrix->data_ptr();
+    const auto* code = static_cast<const uint8_t*>(codes->data_ptr());
+    const void* scale = scales->data_ptr();
+    const int64_t group = c.columns / scales->size(1);
+    void* out = logits.data_ptr();
+    void* stream = stream_of(c);
+    PyObject* result = THPVariable_Wrap(logits);
+    if (result == nullptr) return nullptr;
+    return outputs_or_status(result, unlocked([&] {
+      return sbw_head_logits(hidden, c.rows, c.columns, c.row_stride, code, scale, scale_dtype, group, V, out,
+                             bf16 ? SBW_BF16 : SBW_F32, V, stream);
+    }));
+  });
+}
+
 PyCFunction fast(PyObject* (*f)(PyObject*, PyObject* const*, Py_ssize_t)) {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f));
 }
@@ -327,6 +508,10 @@ PyMethodDef methods[] = {
     {"watermark_candidates", fast(watermark_candidates), METH_FASTCALL, nullptr},
     {"decode", fast(decode), METH_FASTCALL, nullptr},
     {"detect", fast(detect), METH_FASTCALL, nullptr},
+    {"token_logprobs", fast(token_logprobs), METH_FASTCALL, nullptr},
+    {"token_logprobs_grad", fast(token_logprobs_grad), METH_FASTCALL, nullptr},
+    {"top_candidates", fast(top_candidates), METH_FASTCALL, nullptr},
+    {"head_logits", fast(head_logits), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods,

@@ -6,38 +6,241 @@ namespace {
 
 constexpr int64_t kMostHidden = 8192;
 
-// One wave a logit: its lanes share the columns, eight weights a 32-bit word.
-template <typename S, typename T>
-__global__ void __launch_bounds__(kThreads)
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kChunk = 128;              // columns of a wave's 16-byte loads: 16 rows x 64 bytes
+constexpr int kTileRows = 16;            // head rows of a matrix instruction
+constexpr int kHeadWaves = 16;           // most waves of a workgroup
+constexpr uint32_t kSixteens = 0x41804180u;   // two bf16 16.0: or a 4-bit q into bits 3-6 for 16 + q
+constexpr uint32_t kCodeBits = 0x00780078u;
+
+__device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
+                                                 0, 0);
+}
+
+// Eight 4-bit codes as bf16 16 + q, in the order 0 4 1 5 2 6 3 7.
+__device__ __forceinline__ u32x4 widened(uint32_t w) {
+  return u32x4{((w << 3) & kCodeBits) | kSixteens, ((w >> 1) & kCodeBits) | kSixteens,
+               ((w >> 5) & kCodeBits) | kSixteens, ((w >> 9) & kCodeBits) | kSixteens};
+}
+// Eight hidden values in the same order.
+__device__ __forceinline__ u32x4 in_code_order(u32x4 h) {
+  return u32x4{(h.x & 0xFFFFu) | h.z << 16, h.x >> 16 | (h.z & 0xFFFF0000u), (h.y & 0xFFFFu) | h.w << 16,
+               h.y >> 16 | (h.w & 0xFFFF0000u)};
+}
+
+// A lane's 16 bytes hold 32 columns of one row, a quarter (lane / 16) of a chunk; word d its columns
+// 8 d .. 8 d + 7.  A matrix instruction sums over the four quarters' words, so for groups smaller
+// than a chunk the words are exchanged between quarters until each instruction's lie in one group.
+// Instruction i then takes, in this quarter, word `d` of quarter `q`:
+struct Source {
+  uint32_t q, d;
+};
+template <int kGroup>
+__device__ __forceinline__ Source source_of(uint32_t i, uint32_t quarter) {
+  if (kGroup == 128) return Source{quarter, i};
+  if (kGroup == 32) return Source{i, quarter};
+  const bool upper = quarter >= 2;
+  if (i < 2) return Source{upper ? quarter - 2 : quarter, upper ? i + 2 : i};
+  return Source{upper ? quarter : quarter + 2, upper ? i : i - 2};
+}
+// Swap a's upper half (lanes 32-63) with b's lower half; a's odd quarters with b's even ones.
+__device__ __forceinline__ void swap32(uint32_t& a, uint32_t& b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  a = r[0];
+  b = r[1];
+}
+__device__ __forceinline__ void swap16(uint32_t& a, uint32_t& b) {
+  const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+  a = r[0];
+  b = r[1];
+}
+template <int kGroup>
+__device__ __forceinline__ void exchange(u32x4& w) {
+  if (kGroup == 128) return;
+  uint32_t w0 = w.x, w1 = w.y, w2 = w.z, w3 = w.w;
+  swap32(w0, w2);
+  swap32(w1, w3);
+  if (kGroup == 32) {
+    swap16(w0, w1);
+    swap16(w2, w3);
+  }
+  w = u32x4{w0, w1, w2, w3};
+}
+
+// The scales of a chunk's groups in every lane, from the one that each lane loaded (that of the group
+// quarter * 32 / kGroup of its row).
+template <int kGroup>
+__device__ __forceinline__ void spread(uint32_t own, float (&scale)[kChunk / kGroup]) {
+  uint32_t a = own, b = own;
+  if (kGroup < 128) swap32(a, b);               // a: quarters 0 1 0 1, b: 2 3 2 3
+  if (kGroup == 32) {
+    uint32_t c = a, d = b;
+    swap16(a, c);                               // a: 0 0 0 0, c: 1 1 1 1
+    swap16(b, d);
+    scale[1 % (kChunk / kGroup)] = __uint_as_float(c);
+    scale[3 % (kChunk / kGroup)] = __uint_as_float(d);
+  }
+  scale[0] = __uint_as_float(a);
+  if (kGroup == 64) scale[1 % (kChunk / kGroup)] = __uint_as_float(b);
+  if (kGroup == 32) scale[2 % (kChunk / kGroup)] = __uint_as_float(b);
+}
+
+// Logits of up to 16 hidden states (grid y) by tiles of kTiles * 16 head rows (grid x, in turn).
+//
+// The waves of a workgroup share the columns, kChunks chunks each, and keep their part of the hidden
+// states in registers, so a head row streams through once: 16 bytes a lane, widened to 16 + q by one
+// shift and one and-or for two codes, straight into the matrix instructions (hidden states as rows,
+// head rows as columns).  Each group's sum starts at -24 times the sum of its hidden values, which leaves
+// sum (q - 8) h: every product is exact and all sums are fp32.  A lane then holds four hidden states'
+// sums for one head row, so a group's scale is one value a lane.  The waves' sums meet in LDS.
+template <typename S, typename T, int kGroup, int kChunks, int kTiles>
+__global__ void __launch_bounds__(kHeadWaves * kWave)
 head_logits_kernel(const uint16_t* __restrict__ hidden, int64_t B, uint32_t K, int64_t hidden_stride,
-                   const uint8_t* __restrict__ codes, const S* __restrict__ scales, uint32_t group,
-                   int64_t V, T* __restrict__ logits, int64_t row_stride) {
-  const int64_t waves = static_cast<int64_t>(gridDim.x) * (kThreads / kWave);
-  const uint32_t lane = threadIdx.x % kWave;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * (kThreads / kWave) + threadIdx.x / kWave; i < B * V;
-       i += waves) {
-    const int64_t b = i % B, v = i / B;
-    float total = 0.0f;
-    for (uint32_t c = lane; c < K / 2; c += kWave) {
-      const uint32_t q = codes[v * (K / 2) + c];
-      const uint16_t* h = hidden + b * hidden_stride + 2 * c;
-      float d = logit_of(h[0]) * (static_cast<float>(q & 15u) - 8.0f);
-      d = __builtin_fmaf(logit_of(h[1]), static_cast<float>(q >> 4) - 8.0f, d);
-      total = __builtin_fmaf(d, logit_of(scales[v * (K / group) + 2 * c / group]), total);
+                   const uint8_t* __restrict__ codes, const S* __restrict__ scales, uint32_t V,
+                   T* __restrict__ logits, int64_t row_stride) {
+  constexpr int kGroups = kChunk / kGroup;           // groups of a chunk
+  constexpr int kPerGroup = 4 / kGroups;             // matrix instructions of a group
+  constexpr uint32_t kRows = kTiles * kTileRows;
+  __shared__ float sums[2][kHeadWaves][kTiles * kWave * 4];
+  const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
+  const uint32_t r = lane % 16, quarter = lane / 16;
+  const int64_t b0 = static_cast<int64_t>(blockIdx.y) * 16;
+  const uint32_t batch = static_cast<uint32_t>(B - b0 < 16 ? B - b0 : 16);
+
+  u32x4 h[kChunks][4];
+  // held where there are few groups; else it is summed again by a second matrix instruction
+  constexpr bool kHold = kChunks * kGroups <= 4 && kChunks <= 2;
+  f32x4 base[kChunks][kGroups];
+  const u32x4 minus24 = {0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u};
+#pragma unroll
+  for (int q = 0; q < kChunks; ++q) {
+    const uint32_t k0 = (wave * kChunks + q) * kChunk;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const Source at = source_of<kGroup>(i, quarter);
+      const uint32_t k = k0 + at.q * 32 + at.d * 8;
+      h[q][i] = u32x4{0u, 0u, 0u, 0u};
+      if (r < batch && k < K)
+        h[q][i] = in_code_order(*reinterpret_cast<const u32x4_memory*>(hidden + (b0 + r) * hidden_stride + k));
     }
-    total = wave_sum(total);
-    if (lane == 0) put_logit(logits + b * row_stride + v, total);
+    if (!kHold) continue;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      base[q][g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int i = 0; i < kPerGroup; ++i) base[q][g] = mfma(h[q][g * kPerGroup + i], minus24, base[q][g]);
+    }
+  }
+
+  const uint32_t groups = K / kGroup;
+  u32x4 next[kTiles][kChunks];
+  float next_scale[kTiles][kChunks];
+  const auto load = [&](uint32_t tile) {
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      const uint32_t v = min(tile * kRows + t * kTileRows + r, V - 1);   // rows beyond the last are not stored
+#pragma unroll
+      for (int q = 0; q < kChunks; ++q) {
+        // columns beyond the last meet hidden values of 0; their groups' scales are 0
+        const uint32_t chunk = wave * kChunks + q;
+        const uint32_t at = min(chunk * (kChunk / 2) + quarter * 16, K / 2 - 16);
+        next[t][q] = *reinterpret_cast<const u32x4_memory*>(codes + static_cast<uint64_t>(v) * (K / 2) + at);
+        const uint32_t group = chunk * kGroups + quarter * 32 / kGroup;
+        const float s = logit_of(scales[static_cast<uint64_t>(v) * groups + min(group, groups - 1)]);
+        next_scale[t][q] = group < groups ? s : 0.0f;
+      }
+    }
+  };
+
+  const uint32_t tiles = (V + kRows - 1) / kRows;
+  uint32_t turn = 0;
+  load(blockIdx.x);
+  for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    u32x4 w[kTiles][kChunks];
+    float own_scale[kTiles][kChunks];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int q = 0; q < kChunks; ++q) {
+        w[t][q] = next[t][q];
+        own_scale[t][q] = next_scale[t][q];
+      }
+    if (tile + gridDim.x < tiles) load(tile + gridDim.x);
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      f32x4 total = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int q = 0; q < kChunks; ++q) {
+        exchange<kGroup>(w[t][q]);
+        float scale[kGroups];
+        spread<kGroup>(__float_as_uint(own_scale[t][q]), scale);
+        const uint32_t word[4] = {w[t][q].x, w[t][q].y, w[t][q].z, w[t][q].w};
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+          f32x4 of_group = {0.0f, 0.0f, 0.0f, 0.0f};
+          if (kHold) {
+            of_group = base[q][g];
+          } else {
+#pragma unroll
+            for (int i = 0; i < kPerGroup; ++i) of_group = mfma(h[q][g * kPerGroup + i], minus24, of_group);
+          }
+#pragma unroll
+          for (int i = 0; i < kPerGroup; ++i)
+            of_group = mfma(h[q][g * kPerGroup + i], widened(word[g * kPerGroup + i]), of_group);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) total[i] = __builtin_fmaf(of_group[i], scale[g], total[i]);
+        }
+      }
+      *reinterpret_cast<f32x4*>(&sums[turn][wave][(t * kWave + lane) * 4]) = total;
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < kTiles * kWave * 4; i += blockDim.x) {
+      // place i: head row (i / 4) % 16 of its tile, hidden state 4 * (i / 64 % 4) + i % 4
+      const uint32_t b = i / 64 % 4 * 4 + i % 4;
+      const uint32_t v = tile * kRows + i / (kWave * 4) * kTileRows + i / 4 % 16;
+      if (b >= batch || v >= V) continue;
+      float x = 0.0f;
+      for (uint32_t n = 0; n < waves; ++n) x += sums[turn][n][i];
+      put_logit(logits + (b0 + b) * row_stride + v, x);
+    }
+    turn ^= 1;
   }
 }
 
+template <typename S, typename T, int kGroup, int kChunks, int kTiles>
+void launch_head_shape(const void* hidden, int64_t B, uint32_t K, int64_t hidden_stride, const uint8_t* codes,
+                       const void* scales, uint32_t V, void* logits, int64_t row_stride, hipStream_t stream) {
+  const uint32_t waves = (K + kChunks * kChunk - 1) / (kChunks * kChunk);
+  const uint32_t tiles = (V + kTiles * kTileRows - 1) / (kTiles * kTileRows);
+  const uint32_t resident = 256u * (kHeadWaves / waves);
+  const dim3 grid(tiles < resident ? tiles : resident, static_cast<uint32_t>((B + 15) / 16));
+  head_logits_kernel<S, T, kGroup, kChunks, kTiles><<<grid, waves * kWave, 0, stream>>>(
+      static_cast<const uint16_t*>(hidden), B, K, hidden_stride, codes, static_cast<const S*>(scales), V,
+      static_cast<T*>(logits), row_stride);
+}
+
+template <typename S, typename T, int kGroup>
+void launch_head_group(const void* hidden, int64_t B, uint32_t K, int64_t hidden_stride, const uint8_t* codes,
+                       const void* scales, uint32_t V, void* logits, int64_t row_stride, hipStream_t stream) {
+  if (K <= kHeadWaves * 2 * kChunk)
+    launch_head_shape<S, T, kGroup, 2, 2>(hidden, B, K, hidden_stride, codes, scales, V, logits, row_stride, stream);
+  else
+    launch_head_shape<S, T, kGroup, 4, 1>(hidden, B, K, hidden_stride, codes, scales, V, logits, row_stride, stream);
+}
+
 template <typename S, typename T>
-void launch_head(const void* hidden, int64_t B, int64_t K, int64_t hidden_stride, const uint8_t* codes,
-                 const void* scales, int64_t group, int64_t V, void* logits, int64_t row_stride,
+void launch_head(const void* hidden, int64_t B, int64_t K_, int64_t hidden_stride, const uint8_t* codes,
+                 const void* scales, int64_t group, int64_t V_, void* logits, int64_t row_stride,
                  hipStream_t stream) {
-  const dim3 grid(static_cast<uint32_t>(grid_for((B * V + 3) / 4)));
-  head_logits_kernel<S, T><<<grid, kThreads, 0, stream>>>(
-      static_cast<const uint16_t*>(hidden), B, static_cast<uint32_t>(K), hidden_stride, codes,
-      static_cast<const S*>(scales), static_cast<uint32_t>(group), V, static_cast<T*>(logits), row_stride);
+  const auto K = static_cast<uint32_t>(K_), V = static_cast<uint32_t>(V_);
+  if (group == 32)
+    launch_head_group<S, T, 32>(hidden, B, K, hidden_stride, codes, scales, V, logits, row_stride, stream);
+  else if (group == 64)
+    launch_head_group<S, T, 64>(hidden, B, K, hidden_stride, codes, scales, V, logits, row_stride, stream);
+  else
+    launch_head_group<S, T, 128>(hidden, B, K, hidden_stride, codes, scales, V, logits, row_stride, stream);
 }
 
 }  // namespace
@@ -56,7 +259,8 @@ extern "C" sbw_status_t sbw_head_logits(const void* hidden, int64_t B, int64_t K
   if (B == 0 || V == 0) return SBW_OK;
   if (hidden == nullptr || codes == nullptr || scales == nullptr || logits == nullptr)
     return SBW_ERR_INVALID_ARG;
-  if (B > INT64_MAX / 4 / row_stride || B > INT64_MAX / 4 / hidden_stride) return SBW_ERR_UNSUPPORTED;
+  if (B > INT64_MAX / 4 / row_stride || B > INT64_MAX / 4 / hidden_stride || B > 16 * kMaxGridY)
+    return SBW_ERR_UNSUPPORTED;
   const sbw_status_t s = check_device();
   if (s != SBW_OK) return s;
   const auto st = static_cast<hipStream_t>(stream);

@@ -5,7 +5,8 @@
     token_logprobs(logits, tokens, inv_temperature=1.0, top=0) -> TokenLogprobs
     token_logprobs_grad(logits, tokens, stats, ...) -> the gradient, like logits
 
-Same conventions as the watermark's calls: tensors on the current HIP device, unit stride
+Ordinary calls are marshalled in native code (``_binding.so``), the others here.  Same conventions
+as the watermark's calls: tensors on the current HIP device, unit stride
 along the vocabulary, rows padded or not, the current stream unless one is given, every step
 in the HIP kernels of ``libsbw.so``.
 """
@@ -172,6 +173,12 @@ class _Differentiable(torch.autograd.Function):
 
 
 def _call(logits, tokens, inv_temperature, top, out, workspace, stream) -> TokenLogprobs:
+    if stream is None and out is None and workspace is None:
+        got = _native.token_logprobs(logits, tokens, inv_temperature, top)
+        if type(got) is tuple:
+            return tuple.__new__(TokenLogprobs, got)
+        if got is not None:
+            _check(got)
     return _forward(logits, tokens, inv_temperature, top, out, workspace, stream)
 
 
@@ -212,6 +219,13 @@ def token_logprobs_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor], st
     grad_* is float32, shaped as its output, or None.  stats and entropy are what the forward call
     returned (entropy is needed with grad_entropy only).  ``out`` is like logits; it may be the
     logits themselves."""
+    if stream is None and out is None:
+        got = _native.token_logprobs_grad(logits, tokens, stats, entropy, grad_logprobs, grad_lse,
+                                          grad_entropy, inv_temperature)
+        if type(got) is torch.Tensor:
+            return got
+        if got is not None:
+            _check(got)
     dtype, B, V, row_stride = _matrix(logits, "logits")
     n = _tokens(tokens, B)
     if out is None:
@@ -247,6 +261,12 @@ def top_candidates(logits: torch.Tensor, k: int, v_offset: int = 0,
     None), larger first, equal ones by their id, a NaN above every number.  Places beyond V hold
     -1 and -inf.  The ids are what ``watermark_candidates`` takes.  v_offset: the token id of
     column 0 when the logits are a vocabulary shard."""
+    if stream is None and ids is None and values is None and workspace is None and with_values:
+        got = _native.top_candidates(logits, k, v_offset)
+        if type(got) is tuple:
+            return got
+        if got is not None:
+            _check(got)
     dtype, B, V, row_stride = _matrix(logits, "logits")
     k = int(k)
     dev = logits.device
@@ -276,6 +296,12 @@ def head_logits(hidden: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
     float32 or bfloat16 [V, K / group], contiguous; group is 32, 64 or 128.  V may be a shard
     of the vocabulary.  dtype (of the logits): float32 or bfloat16.
     """
+    if stream is None and out is None and (dtype is torch.float32 or dtype is torch.bfloat16):
+        got = _native.head_logits(hidden, codes, scales, dtype is torch.bfloat16)
+        if type(got) is torch.Tensor:
+            return got
+        if got is not None:
+            _check(got)
     if hidden.dim() != 2 or hidden.dtype != torch.bfloat16:
         raise ValueError("hidden must be bfloat16 [B, K]")
     _, B, K, hidden_stride = _matrix(hidden, "hidden")
