@@ -10,7 +10,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kChunk = 128;              // columns of a wave's 16-byte loads: 16 rows x 64 bytes
 constexpr int kTileRows = 16;            // head rows of a matrix instruction
-constexpr int kHeadWaves = 16;           // most waves of a workgroup
+constexpr int kHeadWaves = 16;           // of a CU
 constexpr uint32_t kSixteens = 0x41804180u;   // two bf16 16.0: or a 4-bit q into bits 3-6 for 16 + q
 constexpr uint32_t kCodeBits = 0x00780078u;
 
@@ -19,10 +19,11 @@ __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
                                                  0, 0);
 }
 
-// Eight 4-bit codes as bf16 16 + q, in the order 0 4 1 5 2 6 3 7.
-__device__ __forceinline__ u32x4 widened(uint32_t w) {
-  return u32x4{((w << 3) & kCodeBits) | kSixteens, ((w >> 1) & kCodeBits) | kSixteens,
-               ((w >> 5) & kCodeBits) | kSixteens, ((w >> 9) & kCodeBits) | kSixteens};
+// Eight 4-bit codes as bf16 16 + q, in the order 0 4 1 5 2 6 3 7.  `sixteens` is kSixteens in a vector
+// register: an instruction reads one scalar operand, and the mask is that one.
+__device__ __forceinline__ u32x4 widened(uint32_t w, uint32_t sixteens) {
+  return u32x4{((w << 3) & kCodeBits) | sixteens, ((w >> 1) & kCodeBits) | sixteens,
+               ((w >> 5) & kCodeBits) | sixteens, ((w >> 9) & kCodeBits) | sixteens};
 }
 // Eight hidden values in the same order.
 __device__ __forceinline__ u32x4 in_code_order(u32x4 h) {
@@ -69,24 +70,6 @@ __device__ __forceinline__ void exchange(u32x4& w) {
   w = u32x4{w0, w1, w2, w3};
 }
 
-// The scales of a chunk's groups in every lane, from the one that each lane loaded (that of the group
-// quarter * 32 / kGroup of its row).
-template <int kGroup>
-__device__ __forceinline__ void spread(uint32_t own, float (&scale)[kChunk / kGroup]) {
-  uint32_t a = own, b = own;
-  if (kGroup < 128) swap32(a, b);               // a: quarters 0 1 0 1, b: 2 3 2 3
-  if (kGroup == 32) {
-    uint32_t c = a, d = b;
-    swap16(a, c);                               // a: 0 0 0 0, c: 1 1 1 1
-    swap16(b, d);
-    scale[1 % (kChunk / kGroup)] = __uint_as_float(c);
-    scale[3 % (kChunk / kGroup)] = __uint_as_float(d);
-  }
-  scale[0] = __uint_as_float(a);
-  if (kGroup == 64) scale[1 % (kChunk / kGroup)] = __uint_as_float(b);
-  if (kGroup == 32) scale[2 % (kChunk / kGroup)] = __uint_as_float(b);
-}
-
 // Logits of up to 16 hidden states (grid y) by tiles of kTiles * 16 head rows (grid x, in turn).
 //
 // The waves of a workgroup share the columns, kChunks chunks each, and keep their part of the hidden
@@ -94,36 +77,98 @@ __device__ __forceinline__ void spread(uint32_t own, float (&scale)[kChunk / kGr
 // shift and one and-or for two codes, straight into the matrix instructions (hidden states as rows,
 // head rows as columns).  Each group's sum starts at -24 times the sum of its hidden values, which leaves
 // sum (q - 8) h: every product is exact and all sums are fp32.  A lane then holds four hidden states'
-// sums for one head row, so a group's scale is one value a lane.  The waves' sums meet in LDS.
-template <typename S, typename T, int kGroup, int kChunks, int kTiles>
-__global__ void __launch_bounds__(kHeadWaves * kWave)
+// sums for one head row, so a group's scale is one value a lane; a tile's scales are loaded side by side
+// and handed out through LDS.  The waves' sums meet in LDS.
+template <typename S, typename T, int kGroup, int kChunks, int kTiles, int kMost>
+__global__ void __launch_bounds__(kMost * kWave, 4)
 head_logits_kernel(const uint16_t* __restrict__ hidden, int64_t B, uint32_t K, int64_t hidden_stride,
                    const uint8_t* __restrict__ codes, const S* __restrict__ scales, uint32_t V,
-                   T* __restrict__ logits, int64_t row_stride) {
+                   T* __restrict__ logits, int64_t row_stride, uint32_t waves) {
   constexpr int kGroups = kChunk / kGroup;           // groups of a chunk
   constexpr int kPerGroup = 4 / kGroups;             // matrix instructions of a group
   constexpr uint32_t kRows = kTiles * kTileRows;
-  __shared__ float sums[2][kHeadWaves][kTiles * kWave * 4];
-  const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
+  constexpr int kOwnScales = kRows * kChunks * kGroups / kWave;   // of a tile, that a lane loads
+  static_assert(kOwnScales * kWave == kRows * kChunks * kGroups, "a tile's scales fill the lanes");
+  __shared__ float sums[2][kMost][kTiles * kWave * 4];
+  __shared__ float tile_scales[2][kRows * (kMost * kChunks * kGroups + 1)];
+  const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, threads = waves * kWave;
   const uint32_t r = lane % 16, quarter = lane / 16;
   const int64_t b0 = static_cast<int64_t>(blockIdx.y) * 16;
   const uint32_t batch = static_cast<uint32_t>(B - b0 < 16 ? B - b0 : 16);
+
+  // A tile starts at row v0: the last one at V - kRows, where it meets rows of the one before it.
+  const uint32_t tiles = (V + kRows - 1) / kRows;
+  const uint32_t last = V > kRows ? V - kRows : 0u;
+  const uint32_t groups = K / kGroup, row_bytes = K / 2;
+  uint32_t code_at[kTiles][kChunks];                 // from the tile's first row
+#pragma unroll
+  for (int q = 0; q < kChunks; ++q)
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+      // columns beyond the last meet hidden values of 0
+      code_at[t][q] = min(t * kTileRows + r, V - 1) * row_bytes +
+                      min((wave * kChunks + q) * (kChunk / 2) + quarter * 16, row_bytes - 16);
+  u32x4 words[kTiles][kChunks];
+  const auto load = [&](uint32_t tile) {
+    const uint8_t* code = codes + static_cast<uint64_t>(min(tile * kRows, last)) * row_bytes;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int q = 0; q < kChunks; ++q) words[t][q] = *reinterpret_cast<const u32x4_memory*>(code + code_at[t][q]);
+  };
+  // The tile after `tile` in turn; past the end it is `tile` again, not nothing: with a branch around its
+  // loads the compiler would wait for every load before each use.
+  const auto next_of = [&](uint32_t tile) { return tile + gridDim.x < tiles ? tile + gridDim.x : tile; };
+  const uint32_t of_tile = min(kRows, V) * groups;   // scales of a tile, side by side
+  // a place for every group that the waves' chunks could hold, those beyond K with a scale of 0;
+  // an odd stride: a column of 16 rows falls into 16 LDS banks
+  const uint32_t scale_stride = waves * (kChunks * kGroups) | 1u;
+  S own_scale[kOwnScales];
+  const auto load_scales = [&](uint32_t tile) {
+    const S* scale = scales + static_cast<uint64_t>(min(tile * kRows, last)) * groups;
+#pragma unroll
+    for (int i = 0; i < kOwnScales; ++i) own_scale[i] = scale[min(threadIdx.x + i * threads, of_tile - 1)];
+  };
+  const auto put_scales = [&](float* to) {
+#pragma unroll
+    for (int i = 0; i < kOwnScales; ++i) {
+      const uint32_t n = threadIdx.x + i * threads;
+      if (n < of_tile) to[n / groups * scale_stride + n % groups] = logit_of(own_scale[i]);
+    }
+  };
+
+  load_scales(blockIdx.x);
+  load(blockIdx.x);
 
   u32x4 h[kChunks][4];
   // held where there are few groups; else it is summed again by a second matrix instruction
   constexpr bool kHold = kChunks * kGroups <= 4 && kChunks <= 2;
   f32x4 base[kChunks][kGroups];
   const u32x4 minus24 = {0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u};
+  // every load is made, from a place inside the states, so that all are on their way together
 #pragma unroll
-  for (int q = 0; q < kChunks; ++q) {
-    const uint32_t k0 = (wave * kChunks + q) * kChunk;
+  for (int q = 0; q < kChunks; ++q)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const Source at = source_of<kGroup>(i, quarter);
-      const uint32_t k = k0 + at.q * 32 + at.d * 8;
-      h[q][i] = u32x4{0u, 0u, 0u, 0u};
-      if (r < batch && k < K)
-        h[q][i] = in_code_order(*reinterpret_cast<const u32x4_memory*>(hidden + (b0 + r) * hidden_stride + k));
+      const uint32_t k = (wave * kChunks + q) * kChunk + at.q * 32 + at.d * 8;
+      h[q][i] = *reinterpret_cast<const u32x4_memory*>(hidden + (b0 + min(r, batch - 1)) * hidden_stride +
+                                                       min(k, K - 8));
+    }
+  for (uint32_t i = threadIdx.x; i < kTiles * kWave * 4; i += threads)
+    for (uint32_t n = waves; n < kMost; ++n) sums[0][n][i] = sums[1][n][i] = 0.0f;   // of no wave
+  for (uint32_t i = threadIdx.x; i < kRows * scale_stride; i += threads)
+    if (i % scale_stride >= groups) tile_scales[0][i] = tile_scales[1][i] = 0.0f;
+  put_scales(tile_scales[0]);
+  load_scales(next_of(blockIdx.x));
+#pragma unroll
+  for (int q = 0; q < kChunks; ++q) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const Source at = source_of<kGroup>(i, quarter);
+      const bool some = r < batch && (wave * kChunks + q) * kChunk + at.q * 32 + at.d * 8 < K;
+      const u32x4 x = in_code_order(h[q][i]);
+      h[q][i] = u32x4{some ? x.x : 0u, some ? x.y : 0u, some ? x.z : 0u, some ? x.w : 0u};
     }
     if (!kHold) continue;
 #pragma unroll
@@ -133,52 +178,23 @@ head_logits_kernel(const uint16_t* __restrict__ hidden, int64_t B, uint32_t K, i
       for (int i = 0; i < kPerGroup; ++i) base[q][g] = mfma(h[q][g * kPerGroup + i], minus24, base[q][g]);
     }
   }
+  uint32_t sixteens = kSixteens;
+  asm volatile("" : "+v"(sixteens));
+  __syncthreads();
 
-  const uint32_t groups = K / kGroup;
-  u32x4 next[kTiles][kChunks];
-  float next_scale[kTiles][kChunks];
-  const auto load = [&](uint32_t tile) {
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-      const uint32_t v = min(tile * kRows + t * kTileRows + r, V - 1);   // rows beyond the last are not stored
-#pragma unroll
-      for (int q = 0; q < kChunks; ++q) {
-        // columns beyond the last meet hidden values of 0; their groups' scales are 0
-        const uint32_t chunk = wave * kChunks + q;
-        const uint32_t at = min(chunk * (kChunk / 2) + quarter * 16, K / 2 - 16);
-        next[t][q] = *reinterpret_cast<const u32x4_memory*>(codes + static_cast<uint64_t>(v) * (K / 2) + at);
-        const uint32_t group = chunk * kGroups + quarter * 32 / kGroup;
-        const float s = logit_of(scales[static_cast<uint64_t>(v) * groups + min(group, groups - 1)]);
-        next_scale[t][q] = group < groups ? s : 0.0f;
-      }
-    }
-  };
-
-  const uint32_t tiles = (V + kRows - 1) / kRows;
   uint32_t turn = 0;
-  load(blockIdx.x);
   for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-    u32x4 w[kTiles][kChunks];
-    float own_scale[kTiles][kChunks];
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-      for (int q = 0; q < kChunks; ++q) {
-        w[t][q] = next[t][q];
-        own_scale[t][q] = next_scale[t][q];
-      }
-    if (tile + gridDim.x < tiles) load(tile + gridDim.x);
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
       f32x4 total = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int q = 0; q < kChunks; ++q) {
-        exchange<kGroup>(w[t][q]);
-        float scale[kGroups];
-        spread<kGroup>(__float_as_uint(own_scale[t][q]), scale);
-        const uint32_t word[4] = {w[t][q].x, w[t][q].y, w[t][q].z, w[t][q].w};
+        u32x4 w = words[t][q];
+        exchange<kGroup>(w);
+        const uint32_t word[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
+          const float scale = tile_scales[turn][(t * kTileRows + r) * scale_stride + (wave * kChunks + q) * kGroups + g];
           f32x4 of_group = {0.0f, 0.0f, 0.0f, 0.0f};
           if (kHold) {
             of_group = base[q][g];
@@ -188,46 +204,57 @@ head_logits_kernel(const uint16_t* __restrict__ hidden, int64_t B, uint32_t K, i
           }
 #pragma unroll
           for (int i = 0; i < kPerGroup; ++i)
-            of_group = mfma(h[q][g * kPerGroup + i], widened(word[g * kPerGroup + i]), of_group);
+            of_group = mfma(h[q][g * kPerGroup + i], widened(word[g * kPerGroup + i], sixteens), of_group);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) total[i] = __builtin_fmaf(of_group[i], scale[g], total[i]);
+          for (int i = 0; i < 4; ++i) total[i] = __builtin_fmaf(of_group[i], scale, total[i]);
         }
       }
       *reinterpret_cast<f32x4*>(&sums[turn][wave][(t * kWave + lane) * 4]) = total;
     }
+    __builtin_amdgcn_sched_barrier(0);   // into the registers just read, not into others to be copied later
+    load(next_of(tile));
+    __builtin_amdgcn_sched_barrier(0);
+    put_scales(tile_scales[turn ^ 1]);
+    load_scales(next_of(next_of(tile)));
+    __builtin_amdgcn_sched_barrier(0);
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < kTiles * kWave * 4; i += blockDim.x) {
-      // place i: head row (i / 4) % 16 of its tile, hidden state 4 * (i / 64 % 4) + i % 4
+    const uint32_t v0 = min(tile * kRows, last);
+    for (uint32_t i = threadIdx.x; i < kTiles * kWave * 4; i += threads) {
+      // place i: head row (i / 4) % 16 of its 16, hidden state 4 * (i / 64 % 4) + i % 4
       const uint32_t b = i / 64 % 4 * 4 + i % 4;
-      const uint32_t v = tile * kRows + i / (kWave * 4) * kTileRows + i / 4 % 16;
-      if (b >= batch || v >= V) continue;
-      float x = 0.0f;
-      for (uint32_t n = 0; n < waves; ++n) x += sums[turn][n][i];
+      const uint32_t v = v0 + i / (kWave * 4) * kTileRows + i / 4 % 16;
+      if (b >= batch || v >= V || v < tile * kRows) continue;
+      float x = sums[turn][0][i];
+#pragma unroll
+      for (int n = 1; n < kMost; ++n) x += sums[turn][n][i];
       put_logit(logits + (b0 + b) * row_stride + v, x);
     }
     turn ^= 1;
   }
 }
 
-template <typename S, typename T, int kGroup, int kChunks, int kTiles>
+template <typename S, typename T, int kGroup, int kChunks, int kTiles, int kMost>
 void launch_head_shape(const void* hidden, int64_t B, uint32_t K, int64_t hidden_stride, const uint8_t* codes,
                        const void* scales, uint32_t V, void* logits, int64_t row_stride, hipStream_t stream) {
   const uint32_t waves = (K + kChunks * kChunk - 1) / (kChunks * kChunk);
   const uint32_t tiles = (V + kTiles * kTileRows - 1) / (kTiles * kTileRows);
   const uint32_t resident = 256u * (kHeadWaves / waves);
   const dim3 grid(tiles < resident ? tiles : resident, static_cast<uint32_t>((B + 15) / 16));
-  head_logits_kernel<S, T, kGroup, kChunks, kTiles><<<grid, waves * kWave, 0, stream>>>(
+  head_logits_kernel<S, T, kGroup, kChunks, kTiles, kMost><<<grid, waves * kWave, 0, stream>>>(
       static_cast<const uint16_t*>(hidden), B, K, hidden_stride, codes, static_cast<const S*>(scales), V,
-      static_cast<T*>(logits), row_stride);
+      static_cast<T*>(logits), row_stride, waves);
 }
 
+// Few columns are shared by few waves, so that a CU holds 16 waves (their hidden states fill its registers)
+// in 4, 2 or 1 workgroups.
 template <typename S, typename T, int kGroup>
 void launch_head_group(const void* hidden, int64_t B, uint32_t K, int64_t hidden_stride, const uint8_t* codes,
                        const void* scales, uint32_t V, void* logits, int64_t row_stride, hipStream_t stream) {
-  if (K <= kHeadWaves * 2 * kChunk)
-    launch_head_shape<S, T, kGroup, 2, 2>(hidden, B, K, hidden_stride, codes, scales, V, logits, row_stride, stream);
-  else
-    launch_head_shape<S, T, kGroup, 4, 1>(hidden, B, K, hidden_stride, codes, scales, V, logits, row_stride, stream);
+  auto* launch = K <= 4 * 2 * kChunk    ? launch_head_shape<S, T, kGroup, 2, 2, 4>
+                 : K <= 8 * 2 * kChunk  ? launch_head_shape<S, T, kGroup, 2, 2, 8>
+                 : K <= 16 * 2 * kChunk ? launch_head_shape<S, T, kGroup, 2, 2, 16>
+                                        : launch_head_shape<S, T, kGroup, 4, 1, 16>;
+  launch(hidden, B, K, hidden_stride, codes, scales, V, logits, row_stride, stream);
 }
 
 template <typename S, typename T>
