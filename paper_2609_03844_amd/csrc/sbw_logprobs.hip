@@ -124,14 +124,34 @@ __device__ __forceinline__ Stats join_parts(const Stats* parts, uint32_t count, 
   return s;
 }
 
+// Keys of the largest logits of a row's groups, what one lane reads in the pass, and blocks of 16 groups.
+constexpr int kBlockLanes = 16;
+constexpr int kBlocksOf = kThreads / kBlockLanes;   // blocks of a segment
+struct Maxima {
+  uint32_t *groups, *blocks;
+};
+__device__ __forceinline__ Maxima row_maxima(Maxima of_launch, int64_t b, uint32_t segments) {
+  return Maxima{of_launch.groups + b * segments * kThreads, of_launch.blocks + b * segments * kBlocksOf};
+}
+// The largest of a row of 16 lanes, in each of them.
+__device__ __forceinline__ uint32_t row_largest(uint32_t k) {
+  const auto step = [](uint32_t a, int b) { return max(a, static_cast<uint32_t>(b)); };
+  k = step(k, __builtin_amdgcn_update_dpp(0, static_cast<int>(k), 0xB1, 0xF, 0xF, false));    // quad_perm [1,0,3,2]
+  k = step(k, __builtin_amdgcn_update_dpp(0, static_cast<int>(k), 0x4E, 0xF, 0xF, false));    // quad_perm [2,3,0,1]
+  k = step(k, __builtin_amdgcn_update_dpp(0, static_cast<int>(k), 0x141, 0xF, 0xF, false));   // row_half_mirror
+  return step(k, __builtin_amdgcn_update_dpp(0, static_cast<int>(k), 0x140, 0xF, 0xF, false)); // row_mirror
+}
+
 // The streaming pass: one read of every logit.  A workgroup takes a segment of kThreads * kVecs
 // vectors of a row, a lane kVecs of them, kThreads vectors apart.  A wave writes the statistics
 // of its part; with kTop a lane also writes the key of its largest logit (its group's maximum),
 // from which the selection finds the few groups that can hold one of the k largest.
+//
+// Sixteen lanes' maxima give the maximum of a larger group, a block, which a small k needs to look at first.
 template <typename T, int kVecs, bool kStats, bool kTop>
 __global__ void __launch_bounds__(kThreads)
 row_pass_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride, float c,
-                Stats* __restrict__ parts, uint32_t* __restrict__ maxima) {
+                Stats* __restrict__ parts, Maxima maxima) {
   constexpr uint32_t kPer = kPerOf<T>;
   const uint32_t j0 = blockIdx.x * (kThreads * kVecs) + threadIdx.x;
   const bool whole = (blockIdx.x + 1) * (kThreads * kVecs) <= V / kPer;
@@ -151,7 +171,13 @@ row_pass_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row
 #pragma unroll
       for (uint32_t e = 0; e < kPer; ++e) m = larger(m, elem(x[u], e));
     const int64_t segment = b * gridDim.x + blockIdx.x;
-    if (kTop) maxima[segment * kThreads + threadIdx.x] = order_key(m);
+    if (kTop) {
+      const uint32_t key = order_key(m);
+      maxima.groups[segment * kThreads + threadIdx.x] = key;
+      const uint32_t of_block = row_largest(key);
+      if (threadIdx.x % kBlockLanes == 0)
+        maxima.blocks[segment * kBlocksOf + threadIdx.x / kBlockLanes] = of_block;
+    }
     if (kStats) {
       m = wave_largest(m);
       const float base = m == -INFINITY ? 0.0f : m;
@@ -179,23 +205,35 @@ row_pass_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row
 // A threshold t with at least k group maxima at or above it has at least k logits there, all in
 // those groups; bisection stops at a t that leaves not many more than k groups.  Their logits
 // from t on are gathered as (key << 32 | ~column), which no two logits share, and sorted.
+// For a small k the blocks' maxima serve as well, a sixteenth as many: every wave bisects them by itself,
+// without a barrier.
 // Where too many groups tie at t (a mask, equal logits), only what lies above t is gathered,
 // fewer than k groups, and the rest are the first columns that equal t.
 // ---------------------------------------------------------------------------
-constexpr uint32_t kListMost = 4096;     // gathered logits
-constexpr uint32_t kGroupsMost = 2048;   // listed groups
-constexpr uint32_t kRankMost = 256;      // gathered logits that are ordered by counting
+// Two sizes: a few hundred logits by 4 waves, up to 1024 by 16.
+template <bool kSmall>
+struct SelectionSize {
+  static constexpr int kT = kSmall ? 256 : 1024;
+  static constexpr uint32_t kList = kSmall ? 1024 : 4096;     // gathered logits
+  static constexpr uint32_t kGroups = kSmall ? 512 : 2048;    // listed groups
+};
+constexpr uint32_t kSmallMost = 256;     // k of the small size
+constexpr uint32_t kRankMost = 128;      // gathered logits that are ordered by counting all of them
+constexpr uint32_t kBuckets = 256;       // the others are counted in their bucket of keys
 
-template <int kT>
+template <bool kSmall>
 struct Selection {
-  uint64_t list[kListMost], best[kRankMost];
-  uint32_t groups[kGroupsMost], slots[2][kT / kWave];
-  uint32_t taken, listed;
+  static constexpr int kT = SelectionSize<kSmall>::kT;
+  uint64_t list[SelectionSize<kSmall>::kList], other[SelectionSize<kSmall>::kList];
+  uint32_t starts[kBuckets];
+  uint32_t groups[SelectionSize<kSmall>::kGroups], slots[2][kT / kWave];
+  uint32_t taken, listed, blocks;
 };
 
 // The sum over the workgroup of one number a wave; `turn` alternates.
-template <int kT>
-__device__ __forceinline__ uint32_t group_sum(uint32_t of_wave, Selection<kT>& s, uint32_t turn) {
+template <bool kSmall>
+__device__ __forceinline__ uint32_t group_sum(uint32_t of_wave, Selection<kSmall>& s, uint32_t turn) {
+  constexpr int kT = SelectionSize<kSmall>::kT;
   if (threadIdx.x % kWave == 0) s.slots[turn & 1][threadIdx.x / kWave] = of_wave;
   __syncthreads();
   uint32_t n = 0;
@@ -204,29 +242,72 @@ __device__ __forceinline__ uint32_t group_sum(uint32_t of_wave, Selection<kT>& s
   return n;
 }
 
-// Bisection between two keys: lo has at least k at or above it, hi fewer.  In the logits' own
-// scale first, which is where they spread evenly, then bit by bit.
+// Bisection between two keys: lo has at least k at or above it, hi fewer.  The first steps go down from the
+// largest logit by a half of it and more; then between the keys, which is near enough to between the
+// logits where both have one sign.
 struct Bisection {
   uint32_t lo, hi, step = 0;
   float reach = 1.0f;
   __device__ __forceinline__ uint32_t middle() {
-    uint32_t mid = lo;
-    if (step < 16) {
-      const float a = logit_of_key(lo), z = logit_of_key(hi);
-      const float t = lo == kLowestKey ? z - __builtin_fmaf(0.5f, fabsf(z), 1.0f) * reach : 0.5f * a + 0.5f * z;
-      mid = order_key(t);
+    uint32_t mid = lo + (hi - lo) / 2;
+    const bool first = lo == kLowestKey;
+    if (step < 16 && (first || ((lo ^ hi) & 0x80000000u) != 0)) {
+      const float z = logit_of_key(hi);
+      const float t = first ? z - __builtin_fmaf(0.5f, fabsf(z), 1.0f) * reach : 0.5f * logit_of_key(lo) + 0.5f * z;
+      const uint32_t key = __builtin_amdgcn_readfirstlane(order_key(t));
       reach *= 4.0f;
+      if (key > lo && key < hi) mid = key;
     }
     ++step;
-    return mid > lo && mid < hi ? mid : lo + (hi - lo) / 2;
+    return mid;
   }
 };
 
-template <typename T, int kVecs, int kT>
-__device__ const uint64_t* select_row(const T* row, uint32_t V, const uint32_t* __restrict__ maxima,
-                                      uint32_t groups, uint32_t k, Selection<kT>& s) {
+// Appends the wanted logits of the listed groups to the list (counting on beyond its end).
+template <typename T, int kVecs, bool kSmall, typename F>
+__device__ __forceinline__ void gather_listed(const T* row, uint32_t V, Selection<kSmall>& s, F wanted) {
   constexpr uint32_t kPer = kPerOf<T>;
-  constexpr int kHeld = 8192 / kT;
+  constexpr int kT = SelectionSize<kSmall>::kT, kAhead = 4;
+  const uint32_t items = s.listed * kVecs;
+  for (uint32_t i = threadIdx.x; i < items; i += kAhead * kT) {
+    typename VecOf<T>::Value x[kAhead];
+    uint32_t j[kAhead];
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n) {
+      const uint32_t item = min(i + n * kT, items - 1), g = s.groups[item / kVecs];
+      j[n] = g / kThreads * (kThreads * kVecs) + item % kVecs * kThreads + g % kThreads;
+      if ((j[n] + 1) * kPer <= V) x[n] = load_whole(row, j[n]);
+    }
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n) {
+      if (i + n * kT >= items) break;
+      if ((j[n] + 1) * kPer > V) x[n] = load_any(row, V, j[n]);
+#pragma unroll
+      for (uint32_t e = 0; e < kPer; ++e) {
+        const uint32_t key = order_key(elem(x[n], e));
+        if (wanted(key) && j[n] * kPer + e < V) {
+          const uint32_t at = atomicAdd(&s.taken, 1u);
+          if (at < SelectionSize<kSmall>::kList) s.list[at] = static_cast<uint64_t>(key) << 32 | ~(j[n] * kPer + e);
+        }
+      }
+    }
+  }
+}
+
+// What s.list holds: `taken` logits, the k first among them; where `above` is set the fewer than k above
+// `key` only, and logits that equal it make up the rest.
+struct Gathered {
+  uint32_t taken, key;
+  bool above;
+};
+
+// Whatever the row holds.
+template <typename T, int kVecs, bool kSmall>
+__device__ __forceinline__ Gathered gather_any(const T* row, uint32_t V, const uint32_t* __restrict__ maxima,
+                                            uint32_t groups, uint32_t k, Selection<kSmall>& s) {
+  constexpr uint32_t kPer = kPerOf<T>;
+  constexpr int kT = SelectionSize<kSmall>::kT, kHeld = 8;
+  constexpr uint32_t kListMost = SelectionSize<kSmall>::kList, kGroupsMost = SelectionSize<kSmall>::kGroups;
   const uint32_t tid = threadIdx.x;
   uint32_t turn = 0;
   uint32_t held[kHeld];
@@ -254,7 +335,6 @@ __device__ const uint64_t* select_row(const T* row, uint32_t V, const uint32_t* 
       n += __popcll(__ballot(g0 + tid < groups && maxima[g0 + tid] >= t));
     return group_sum(n, s, turn++);
   };
-  k = min(k, V);
   Bisection at{kLowestKey, highest};
   uint32_t from = groups;                       // group maxima at or above at.lo
   if (from > k) {
@@ -300,11 +380,7 @@ __device__ const uint64_t* select_row(const T* row, uint32_t V, const uint32_t* 
     }
   };
   const auto gather = [&] {
-    each_listed([&](uint32_t key, uint32_t column) {
-      if (!wanted(key)) return;
-      const uint32_t n = atomicAdd(&s.taken, 1u);
-      if (n < kListMost) s.list[n] = static_cast<uint64_t>(key) << 32 | ~column;
-    });
+    gather_listed<T, kVecs>(row, V, s, wanted);
     __syncthreads();
   };
   gather();
@@ -344,85 +420,250 @@ __device__ const uint64_t* select_row(const T* row, uint32_t V, const uint32_t* 
     gather();
     taken = s.taken;
   }
-  if (above) {
-    // the first columns that equal at.lo
-    for (uint32_t j0 = 0; taken < k && j0 * kPer < V; j0 += kT) {
-      const uint32_t j = j0 + tid;
-      uint32_t equal = 0;
-      if (j * kPer < V) {
-        const auto x = load_any(row, V, j);
-#pragma unroll
-        for (uint32_t e = 0; e < kPer; ++e)
-          equal |= static_cast<uint32_t>(j * kPer + e < V && order_key(elem(x, e)) == at.lo) << e;
-      }
-      uint32_t before = __popc(equal);
-#pragma unroll
-      for (int d = 1; d < kWave; d *= 2) {
-        const uint32_t n = __shfl_up(before, d);
-        if (tid % kWave >= static_cast<uint32_t>(d)) before += n;
-      }
-      const uint32_t of_wave = __shfl(before, kWave - 1);
-      if (tid % kWave == 0) s.slots[turn & 1][tid / kWave] = of_wave;
-      __syncthreads();
-      before += taken - __popc(equal);
-      for (uint32_t w = 0; w < kT / kWave; ++w) {
-        if (w < tid / kWave) before += s.slots[turn & 1][w];
-        taken += s.slots[turn & 1][w];
-      }
-      ++turn;
-      for (uint32_t e = 0; e < kPer; ++e)
-        if (equal >> e & 1u) {
-          if (before < k) s.list[before] = static_cast<uint64_t>(at.lo) << 32 | ~(j * kPer + e);
-          ++before;
-        }
-    }
-    taken = k;
-    __syncthreads();
-  }
+  return Gathered{taken, at.lo, above};
+}
 
+// The list filled up to k by the first columns that equal `key`.
+template <typename T, bool kSmall>
+__device__ __forceinline__ void fill_equal(const T* row, uint32_t V, uint32_t k, uint32_t taken, uint32_t key,
+                                        Selection<kSmall>& s) {
+  constexpr uint32_t kPer = kPerOf<T>;
+  constexpr int kT = SelectionSize<kSmall>::kT;
+  const uint32_t tid = threadIdx.x;
+  uint32_t turn = 0;
+  __syncthreads();
+  for (uint32_t j0 = 0; taken < k && j0 * kPer < V; j0 += kT) {
+    const uint32_t j = j0 + tid;
+    uint32_t equal = 0;
+    if (j * kPer < V) {
+      const auto x = load_any(row, V, j);
+#pragma unroll
+      for (uint32_t e = 0; e < kPer; ++e)
+        equal |= static_cast<uint32_t>(j * kPer + e < V && order_key(elem(x, e)) == key) << e;
+    }
+    uint32_t before = __popc(equal);
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+      const uint32_t n = __shfl_up(before, d);
+      if (tid % kWave >= static_cast<uint32_t>(d)) before += n;
+    }
+    const uint32_t of_wave = __shfl(before, kWave - 1);
+    if (tid % kWave == 0) s.slots[turn & 1][tid / kWave] = of_wave;
+    __syncthreads();
+    before += taken - __popc(equal);
+    for (uint32_t w = 0; w < kT / kWave; ++w) {
+      if (w < tid / kWave) before += s.slots[turn & 1][w];
+      taken += s.slots[turn & 1][w];
+    }
+    ++turn;
+    for (uint32_t e = 0; e < kPer; ++e)
+      if (equal >> e & 1u) {
+        if (before < k) s.list[before] = static_cast<uint64_t>(key) << 32 | ~(j * kPer + e);
+        ++before;
+      }
+  }
+  __syncthreads();
+}
+
+// The same for k that the blocks' maxima suffice for; `taken` is more than the list holds where they do not
+// (the row's largest logits stand together).  A wave holds kHeld * 64 blocks.
+template <typename T, int kVecs, int kHeld>
+__device__ __forceinline__ Gathered gather_from_blocks(const T* row, uint32_t V, Maxima maxima, uint32_t blocks,
+                                                       uint32_t k, Selection<true>& s) {
+  constexpr uint32_t kPer = kPerOf<T>;
+  constexpr int kT = SelectionSize<true>::kT;
+  constexpr uint32_t kListMost = SelectionSize<true>::kList, kGroupsMost = SelectionSize<true>::kGroups;
+  const uint32_t tid = threadIdx.x, lane = tid % kWave;
+  uint32_t held[kHeld];
+  uint32_t highest = 0;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) held[i] = lane + i * kWave < blocks ? maxima.blocks[lane + i * kWave] : 0u;
+  if (tid == 0) s.taken = s.listed = s.blocks = 0;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) highest = max(highest, held[i]);
+  highest = row_largest(highest);
+  highest = max(highest, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(highest), 0x142, 0xA, 0xF, false)));
+  highest = max(highest, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(highest), 0x143, 0xC, 0xF, false)));
+  highest = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(highest), 63));
+  const auto blocks_from = [&](uint32_t t) {
+    uint32_t n = 0;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) n += __popcll(__ballot(held[i] >= t));
+    return n;
+  };
+  // every wave takes the same steps
+  const uint32_t most = k + k / 4 + 16;
+  Bisection at{kLowestKey, highest};
+  uint32_t from = blocks;
+  const uint32_t at_highest = blocks_from(highest);
+  if (at_highest >= k) {
+    at.lo = highest;
+    from = at_highest;
+  }
+  while (from > most && at.hi - at.lo > 1) {
+    const uint32_t mid = at.middle();
+    const uint32_t n = blocks_from(mid);
+    if (n >= k) {
+      at.lo = mid;
+      from = n;
+    } else {
+      at.hi = mid;
+    }
+  }
+  // too many blocks tie at at.lo: those above it, fewer than k
+  const bool above = from > most;
+  const uint32_t least = above ? min(at.lo, 0xFFFFFFFEu) + 1u : at.lo;
+  if (above) from = at.lo == 0xFFFFFFFFu ? 0u : blocks_from(least);
+  __syncthreads();
+  uint32_t* const listed_blocks = reinterpret_cast<uint32_t*>(s.list);   // until the logits are gathered
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i)
+    if (i % (kT / kWave) == static_cast<int>(tid / kWave) && held[i] >= least && from > 0)
+      listed_blocks[atomicAdd(&s.blocks, 1u)] = lane + i * kWave;
+  __syncthreads();
+  // the blocks' groups that reach the threshold, and their logits; several loads of a lane on their way together
+  const uint32_t candidates = from * kBlockLanes;
+  for (uint32_t i = tid; i < candidates; i += 8 * kT) {
+    uint32_t g[8], key[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t n = min(i + j * kT, candidates - 1);
+      g[j] = listed_blocks[n / kBlockLanes] * kBlockLanes + n % kBlockLanes;
+      key[j] = maxima.groups[g[j]];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (i + j * kT < candidates && key[j] >= least) {
+        const uint32_t n = atomicAdd(&s.listed, 1u);
+        if (n < kGroupsMost) s.groups[n] = g[j];
+      }
+  }
+  __syncthreads();
+  if (s.listed > kGroupsMost) return Gathered{kListMost + 1, at.lo, above};
+  gather_listed<T, kVecs>(row, V, s, [&](uint32_t key) { return key >= least; });
+  __syncthreads();
+  return Gathered{s.taken, at.lo, above};
+}
+
+// The gathered logits in order: each to the place that counting the larger ones gives it.  Many are first put
+// into buckets of neighbouring keys, in order of the buckets, so that only those of its bucket are counted.
+template <bool kSmall>
+__device__ __forceinline__ const uint64_t* sorted(uint32_t taken, Selection<kSmall>& s) {
+  constexpr int kT = SelectionSize<kSmall>::kT;
+  const uint32_t tid = threadIdx.x;
+  // how many of list[first .. end) are larger; eight reads on their way together
+  const auto larger_of = [](const uint64_t* list, uint32_t first, uint32_t end, uint64_t mine) {
+    uint32_t rank = 0;
+    for (uint32_t n = first; n < end; n += 8) {
+      uint64_t x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = list[min(n + i, end - 1)];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) rank += n + i < end && x[i] > mine;
+    }
+    return rank;
+  };
   if (taken <= kRankMost) {
-    for (uint32_t i = tid; i < taken; i += kT) {
-      const uint64_t mine = s.list[i];
-      uint32_t rank = 0;
-      for (uint32_t n = 0; n < taken; ++n) rank += s.list[n] > mine;
-      s.best[rank] = mine;
+    if (tid < taken) {
+      const uint64_t mine = s.list[tid];
+      s.other[larger_of(s.list, 0, taken, mine)] = mine;
     }
     __syncthreads();
-    return s.best;
+    return s.other;
   }
-  uint32_t size = 2 * kRankMost;
-  while (size < taken) size *= 2;
-  for (uint32_t i = taken + tid; i < size; i += kT) s.list[i] = 0;
-  for (uint32_t run = 2; run <= size; run *= 2)
-    for (uint32_t d = run / 2; d > 0; d /= 2) {
-      __syncthreads();
-      for (uint32_t i = tid; i < size / 2; i += kT) {
-        const uint32_t a = 2 * i - (i & (d - 1)), z = a + d;
-        const uint64_t p = s.list[a], q = s.list[z];
-        if ((p < q) == ((a & run) == 0)) {
-          s.list[a] = q;
-          s.list[z] = p;
-        }
-      }
+  // the range of keys
+  uint32_t low = 0xFFFFFFFFu, high = 0;
+  for (uint32_t i = tid; i < taken; i += kT) {
+    const uint32_t key = static_cast<uint32_t>(s.list[i] >> 32);
+    low = min(low, key);
+    high = max(high, key);
+  }
+#pragma unroll
+  for (int d = kWave / 2; d > 0; d /= 2) {
+    low = min(low, __shfl_xor(low, d));
+    high = max(high, __shfl_xor(high, d));
+  }
+  for (uint32_t i = tid; i < kBuckets; i += kT) s.starts[i] = 0;
+  if (tid % kWave == 0) {
+    s.slots[0][tid / kWave] = low;
+    s.slots[1][tid / kWave] = high;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kT / kWave; ++w) {
+    low = min(low, s.slots[0][w]);
+    high = max(high, s.slots[1][w]);
+  }
+  const int bits = 32 - __clz(high - low);            // 0 where all are equal
+  const uint32_t shift = bits > 8 ? bits - 8 : 0;     // keys of a bucket: 2^shift
+  const auto bucket_of = [&](uint64_t x) { return (high - static_cast<uint32_t>(x >> 32)) >> shift; };
+  for (uint32_t i = tid; i < taken; i += kT) atomicAdd(&s.starts[bucket_of(s.list[i])], 1u);
+  __syncthreads();
+  // counts into ends: a wave sums four buckets a lane
+  if (tid < kWave) {
+    uint32_t n[kBuckets / kWave], total = 0;
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(kBuckets / kWave); ++i) total += n[i] = s.starts[tid * (kBuckets / kWave) + i];
+    uint32_t before = total;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+      const uint32_t x = __shfl_up(before, d);
+      if (tid >= static_cast<uint32_t>(d)) before += x;
     }
+    before -= total;
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(kBuckets / kWave); ++i) {
+      before += n[i];
+      s.starts[tid * (kBuckets / kWave) + i] = before;
+    }
+  }
+  __syncthreads();
+  // from its end down, a bucket fills to its start: afterwards starts holds the starts
+  for (uint32_t i = tid; i < taken; i += kT) s.other[atomicSub(&s.starts[bucket_of(s.list[i])], 1u) - 1u] = s.list[i];
+  __syncthreads();
+  for (uint32_t i = tid; i < taken; i += kT) {
+    const uint64_t mine = s.other[i];
+    const uint32_t bucket = bucket_of(mine);
+    const uint32_t first = s.starts[bucket], end = bucket + 1 < kBuckets ? s.starts[bucket + 1] : taken;
+    s.list[first + larger_of(s.other, first, end, mine)] = mine;
+  }
   __syncthreads();
   return s.list;
 }
 
-constexpr int kFinishThreads = 1024;
+template <typename T, int kVecs, bool kSmall>
+__device__ const uint64_t* select_row(const T* row, uint32_t V, Maxima maxima, uint32_t segments, uint32_t k,
+                                      Selection<kSmall>& s) {
+  k = min(k, V);
+  const uint32_t blocks = segments * kBlocksOf;
+  Gathered r{SelectionSize<kSmall>::kList + 1, 0u, false};
+  if constexpr (kSmall) {
+    if (2 * k <= blocks && blocks <= 5 * kWave) r = gather_from_blocks<T, kVecs, 5>(row, V, maxima, blocks, k, s);
+    else if (2 * k <= blocks && blocks <= 20 * kWave) r = gather_from_blocks<T, kVecs, 20>(row, V, maxima, blocks, k, s);
+    __syncthreads();
+  }
+  if (r.taken > SelectionSize<kSmall>::kList)
+    r = gather_any<T, kVecs, kSmall>(row, V, maxima.groups, segments * kThreads, k, s);
+  if (r.above && r.taken < k) {
+    fill_equal(row, V, k, r.taken, r.key, s);
+    r.taken = k;
+  }
+  return sorted(r.taken, s);
+}
 
 // After the pass: one workgroup a row joins the statistics, looks up the given tokens and
 // selects the alternatives.
-template <typename T, int kVecs>
-__global__ void __launch_bounds__(kFinishThreads)
+template <typename T, int kVecs, bool kSmall>
+__global__ void __launch_bounds__(SelectionSize<kSmall>::kT)
 token_logprobs_top_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride,
                           const int32_t* __restrict__ tokens, uint32_t n, float inv_t, uint32_t top,
                           uint32_t segments, const Stats* __restrict__ parts,
-                          const uint32_t* __restrict__ maxima, float* __restrict__ logprobs,
+                          Maxima maxima, float* __restrict__ logprobs,
                           float* __restrict__ lse, float* __restrict__ entropy,
                           float* __restrict__ stats, int32_t* __restrict__ top_ids,
                           float* __restrict__ top_logprobs) {
-  __shared__ Selection<kFinishThreads> s;
+  constexpr int kT = SelectionSize<kSmall>::kT;
+  __shared__ Selection<kSmall> s;
   const uint32_t tid = threadIdx.x;
   for (int64_t b = blockIdx.x; b < B; b += gridDim.x) {
     const T* row = logits + b * row_stride;
@@ -435,14 +676,13 @@ token_logprobs_top_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, i
       if (entropy != nullptr) entropy[b] = empty ? 0.0f : ln_s - kLn2 * (r.A / r.S);
       if (stats != nullptr) stats[2 * b] = r.m, stats[2 * b + 1] = ln_s;
     }
-    for (uint32_t j = tid; j < n; j += kFinishThreads) {
+    for (uint32_t j = tid; j < n; j += kT) {
       const int32_t t = tokens[b * n + j];
       const bool token = t >= 0 && static_cast<uint32_t>(t) < V;
       logprobs[b * n + j] = !token ? 0.0f : empty ? -INFINITY : logprob_of(logit_of(row[t]), r.m, inv_t, ln_s);
     }
-    const uint64_t* best = select_row<T, kVecs>(row, V, maxima + b * segments * kThreads, segments * kThreads,
-                                                top, s);
-    for (uint32_t j = tid; j < top; j += kFinishThreads) {
+    const uint64_t* best = select_row<T, kVecs>(row, V, row_maxima(maxima, b, segments), segments, top, s);
+    for (uint32_t j = tid; j < top; j += kT) {
       const bool some = j < V;
       top_ids[b * top + j] = some ? static_cast<int32_t>(~static_cast<uint32_t>(best[j])) : -1;
       if (top_logprobs != nullptr)
@@ -483,17 +723,17 @@ token_logprobs_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64
   }
 }
 
-template <typename T, int kVecs>
-__global__ void __launch_bounds__(kFinishThreads)
+template <typename T, int kVecs, bool kSmall>
+__global__ void __launch_bounds__(SelectionSize<kSmall>::kT)
 top_candidates_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride,
                       uint32_t vbase, uint32_t k, uint32_t segments,
-                      const uint32_t* __restrict__ maxima, int32_t* __restrict__ ids,
+                      Maxima maxima, int32_t* __restrict__ ids,
                       float* __restrict__ values) {
-  __shared__ Selection<kFinishThreads> s;
+  constexpr int kT = SelectionSize<kSmall>::kT;
+  __shared__ Selection<kSmall> s;
   for (int64_t b = blockIdx.x; b < B; b += gridDim.x) {
-    const uint64_t* best = select_row<T, kVecs>(logits + b * row_stride, V, maxima + b * segments * kThreads,
-                                                segments * kThreads, k, s);
-    for (uint32_t j = threadIdx.x; j < k; j += kFinishThreads) {
+    const uint64_t* best = select_row<T, kVecs>(logits + b * row_stride, V, row_maxima(maxima, b, segments), segments, k, s);
+    for (uint32_t j = threadIdx.x; j < k; j += kT) {
       ids[b * k + j] = j < V ? static_cast<int32_t>(vbase + ~static_cast<uint32_t>(best[j])) : -1;
       if (values != nullptr)
         values[b * k + j] = j < V ? logit_of_key(static_cast<uint32_t>(best[j] >> 32)) : -INFINITY;
@@ -641,30 +881,34 @@ template <typename T>
 constexpr int kShortVecs = sizeof(T) == 4 ? 2 : 1;
 constexpr int64_t kLongSegment = kThreads * 32, kShortSegment = kThreads * 8;
 
-// Whether the pass takes the long form: rows that make enough workgroups of it, and enough
-// groups for the selection to leave few.
+// Whether the pass takes the long form: rows that make enough workgroups of it, and so many blocks (for a
+// large k, groups) that the selection is left with few.
 bool long_segments(int64_t B, int64_t V, int64_t top) {
-  return B * ((V + kLongSegment - 1) / kLongSegment) >= 512 && V / 32 >= 4 * top;
+  const int64_t segments = (V + kLongSegment - 1) / kLongSegment;
+  if (top > kSmallMost) return V / 32 >= 4 * top;
+  return B * segments >= 512 && segments * kBlocksOf >= 2 * top;
 }
 int64_t segments_of(int64_t B, int64_t V, int64_t top) {
   const int64_t size = long_segments(B, V, top) ? kLongSegment : kShortSegment;
   return (V + size - 1) / size;
 }
-// uint64 elements of the workspace a segment takes: the statistics of its waves, a key a lane
+// uint64 elements of the workspace a segment takes: the statistics of its waves, a key a lane and a block
 constexpr int64_t kPartElems = sizeof(Stats) * (kThreads / kWave) / 8;
-constexpr int64_t kMaximaElems = kThreads / 2;
+constexpr int64_t kMaximaElems = (kThreads + kBlocksOf) / 2;
+
+Maxima maxima_at(uint64_t* p, int64_t B, int64_t segments) {
+  auto* groups = reinterpret_cast<uint32_t*>(p);
+  return Maxima{groups, groups + B * segments * kThreads};
+}
 
 template <typename T, bool kStats, bool kTop>
 void launch_pass(const T* logits, int64_t B, uint32_t V, int64_t row_stride, float c, int64_t top, uint64_t* parts,
-                 uint64_t* maxima, hipStream_t stream) {
+                 Maxima maxima, hipStream_t stream) {
   const dim3 grid(static_cast<uint32_t>(segments_of(B, V, top)),
                   static_cast<uint32_t>(B < kMaxGridY ? B : kMaxGridY));
-  auto* p = reinterpret_cast<Stats*>(parts);
-  auto* m = reinterpret_cast<uint32_t*>(maxima);
-  if (long_segments(B, V, top))
-    row_pass_kernel<T, kLongVecs<T>, kStats, kTop><<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, c, p, m);
-  else
-    row_pass_kernel<T, kShortVecs<T>, kStats, kTop><<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, c, p, m);
+  auto* kernel = long_segments(B, V, top) ? row_pass_kernel<T, kLongVecs<T>, kStats, kTop>
+                                          : row_pass_kernel<T, kShortVecs<T>, kStats, kTop>;
+  kernel<<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, c, reinterpret_cast<Stats*>(parts), maxima);
 }
 
 template <typename T>
@@ -673,25 +917,25 @@ void launch_logprobs(const void* logits_, int64_t B, uint32_t V, int64_t row_str
                      float* stats, int32_t* top_ids, float* top_logprobs, uint64_t* workspace, hipStream_t stream) {
   const T* logits = static_cast<const T*>(logits_);
   const auto segments = static_cast<uint32_t>(segments_of(B, V, top));
-  uint64_t* maxima = workspace + B * segments * kPartElems;
   const auto* parts = reinterpret_cast<const Stats*>(workspace);
   const float c = inv_t * kLog2e;
   if (top == 0) {
-    launch_pass<T, true, false>(logits, B, V, row_stride, c, top, workspace, nullptr, stream);
+    launch_pass<T, true, false>(logits, B, V, row_stride, c, top, workspace, Maxima{}, stream);
     const dim3 grid(static_cast<uint32_t>(grid_for((B + 3) / 4)));
     token_logprobs_kernel<T><<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, tokens, n, inv_t, segments,
                                                              parts, logprobs, lse, entropy, stats);
     return;
   }
+  const Maxima maxima = maxima_at(workspace + B * segments * kPartElems, B, segments);
   launch_pass<T, true, true>(logits, B, V, row_stride, c, top, workspace, maxima, stream);
-  const dim3 grid(static_cast<uint32_t>(grid_for(B)));
-  const auto launch = [&](auto* kernel) {
-    kernel<<<grid, kFinishThreads, 0, stream>>>(logits, B, V, row_stride, tokens, n, inv_t, top, segments, parts,
-                                                 reinterpret_cast<const uint32_t*>(maxima), logprobs, lse, entropy,
-                                                 stats, top_ids, top_logprobs);
-  };
-  if (long_segments(B, V, top)) launch(token_logprobs_top_kernel<T, kLongVecs<T>>);
-  else launch(token_logprobs_top_kernel<T, kShortVecs<T>>);
+  const bool of_long = long_segments(B, V, top), small = top <= kSmallMost;
+  auto* kernel = of_long ? (small ? token_logprobs_top_kernel<T, kLongVecs<T>, true>
+                                  : token_logprobs_top_kernel<T, kLongVecs<T>, false>)
+                         : (small ? token_logprobs_top_kernel<T, kShortVecs<T>, true>
+                                  : token_logprobs_top_kernel<T, kShortVecs<T>, false>);
+  kernel<<<static_cast<uint32_t>(grid_for(B)), small ? SelectionSize<true>::kT : SelectionSize<false>::kT, 0, stream>>>(
+      logits, B, V, row_stride, tokens, n, inv_t, top, segments, parts, maxima, logprobs, lse, entropy, stats,
+      top_ids, top_logprobs);
 }
 
 template <typename T>
@@ -699,14 +943,15 @@ void launch_candidates(const void* logits_, int64_t B, uint32_t V, int64_t row_s
                        int32_t* ids, float* values, uint64_t* workspace, hipStream_t stream) {
   const T* logits = static_cast<const T*>(logits_);
   const auto segments = static_cast<uint32_t>(segments_of(B, V, k));
-  launch_pass<T, false, true>(logits, B, V, row_stride, 1.0f, k, nullptr, workspace, stream);
-  const dim3 grid(static_cast<uint32_t>(grid_for(B)));
-  const auto launch = [&](auto* kernel) {
-    kernel<<<grid, kFinishThreads, 0, stream>>>(logits, B, V, row_stride, vbase, k, segments,
-                                                 reinterpret_cast<const uint32_t*>(workspace), ids, values);
-  };
-  if (long_segments(B, V, k)) launch(top_candidates_kernel<T, kLongVecs<T>>);
-  else launch(top_candidates_kernel<T, kShortVecs<T>>);
+  const Maxima maxima = maxima_at(workspace, B, segments);
+  launch_pass<T, false, true>(logits, B, V, row_stride, 1.0f, k, nullptr, maxima, stream);
+  const bool of_long = long_segments(B, V, k), small = k <= kSmallMost;
+  auto* kernel = of_long ? (small ? top_candidates_kernel<T, kLongVecs<T>, true>
+                                  : top_candidates_kernel<T, kLongVecs<T>, false>)
+                         : (small ? top_candidates_kernel<T, kShortVecs<T>, true>
+                                  : top_candidates_kernel<T, kShortVecs<T>, false>);
+  kernel<<<static_cast<uint32_t>(grid_for(B)), small ? SelectionSize<true>::kT : SelectionSize<false>::kT, 0, stream>>>(
+      logits, B, V, row_stride, vbase, k, segments, maxima, ids, values);
 }
 
 template <typename T>
