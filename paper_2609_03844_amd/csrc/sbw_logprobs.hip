@@ -263,34 +263,45 @@ struct Bisection {
   }
 };
 
-// Appends the wanted logits of the listed groups to the list (counting on beyond its end).
+// One more in a counter of LDS, lane by lane: few lanes of a wave count at a time, and the code that joins
+// them is longer than they take (the kernels here run once through, and their instructions come from L2).
+__device__ __forceinline__ uint32_t count_one(uint32_t& counter) {
+  uint32_t one = 1;
+  asm volatile("" : "+v"(one));
+  return atomicAdd(&counter, one);
+}
+
+// Appends the wanted logits of the listed groups to the list (counting on beyond its end).  The row has at
+// least one whole vector: a partial one is read as the last kPer columns, without those before it.
 template <typename T, int kVecs, bool kSmall, typename F>
 __device__ __forceinline__ void gather_listed(const T* row, uint32_t V, Selection<kSmall>& s, F wanted) {
   constexpr uint32_t kPer = kPerOf<T>;
-  constexpr int kT = SelectionSize<kSmall>::kT, kAhead = 4;
+  constexpr int kT = SelectionSize<kSmall>::kT;
   const uint32_t items = s.listed * kVecs;
-  for (uint32_t i = threadIdx.x; i < items; i += kAhead * kT) {
-    typename VecOf<T>::Value x[kAhead];
-    uint32_t j[kAhead];
+  const auto column_of = [&](uint32_t item) {
+    const uint32_t g = s.groups[item / kVecs];
+    return (g / kThreads * (kThreads * kVecs) + item % kVecs * kThreads + g % kThreads) * kPer;
+  };
+  const auto load_at = [&](uint32_t column) {
+    return *reinterpret_cast<const typename VecOf<T>::Memory*>(row + min(column, V - kPer));
+  };
+  if (threadIdx.x >= items) return;
+  uint32_t column = column_of(threadIdx.x);
+  auto x = load_at(column);
+  for (uint32_t i = threadIdx.x; i < items; i += kT) {
+    const uint32_t next_column = column_of(min(i + kT, items - 1));   // on its way while this one is looked at
+    const auto next = load_at(next_column);
+    const uint32_t first = min(column, V - kPer);
 #pragma unroll
-    for (int n = 0; n < kAhead; ++n) {
-      const uint32_t item = min(i + n * kT, items - 1), g = s.groups[item / kVecs];
-      j[n] = g / kThreads * (kThreads * kVecs) + item % kVecs * kThreads + g % kThreads;
-      if ((j[n] + 1) * kPer <= V) x[n] = load_whole(row, j[n]);
-    }
-#pragma unroll
-    for (int n = 0; n < kAhead; ++n) {
-      if (i + n * kT >= items) break;
-      if ((j[n] + 1) * kPer > V) x[n] = load_any(row, V, j[n]);
-#pragma unroll
-      for (uint32_t e = 0; e < kPer; ++e) {
-        const uint32_t key = order_key(elem(x[n], e));
-        if (wanted(key) && j[n] * kPer + e < V) {
-          const uint32_t at = atomicAdd(&s.taken, 1u);
-          if (at < SelectionSize<kSmall>::kList) s.list[at] = static_cast<uint64_t>(key) << 32 | ~(j[n] * kPer + e);
-        }
+    for (uint32_t e = 0; e < kPer; ++e) {
+      const uint32_t key = order_key(elem(x, e));
+      if (wanted(key) && first + e >= column) {
+        const uint32_t at = count_one(s.taken);
+        if (at < SelectionSize<kSmall>::kList) s.list[at] = static_cast<uint64_t>(key) << 32 | ~(first + e);
       }
     }
+    x = next;
+    column = next_column;
   }
 }
 
@@ -359,7 +370,7 @@ __device__ __forceinline__ Gathered gather_any(const T* row, uint32_t V, const u
   bool above = from > kGroupsMost;
   const auto wanted = [&](uint32_t key) { return above ? key > at.lo : key >= at.lo; };
   const auto list_group = [&](uint32_t g, uint32_t key) {
-    if (wanted(key)) s.groups[atomicAdd(&s.listed, 1u)] = g;
+    if (wanted(key)) s.groups[count_one(s.listed)] = g;
   };
 #pragma unroll
   for (int i = 0; i < kHeld; ++i)
@@ -380,7 +391,12 @@ __device__ __forceinline__ Gathered gather_any(const T* row, uint32_t V, const u
     }
   };
   const auto gather = [&] {
-    gather_listed<T, kVecs>(row, V, s, wanted);
+    if (V >= kPer) {
+      gather_listed<T, kVecs>(row, V, s, wanted);
+    } else if (tid < V) {
+      const uint32_t key = order_key(logit_of(row[tid]));
+      if (wanted(key)) s.list[count_one(s.taken)] = static_cast<uint64_t>(key) << 32 | ~tid;
+    }
     __syncthreads();
   };
   gather();
@@ -519,22 +535,22 @@ __device__ __forceinline__ Gathered gather_from_blocks(const T* row, uint32_t V,
 #pragma unroll
   for (int i = 0; i < kHeld; ++i)
     if (i % (kT / kWave) == static_cast<int>(tid / kWave) && held[i] >= least && from > 0)
-      listed_blocks[atomicAdd(&s.blocks, 1u)] = lane + i * kWave;
+      listed_blocks[count_one(s.blocks)] = lane + i * kWave;
   __syncthreads();
   // the blocks' groups that reach the threshold, and their logits; several loads of a lane on their way together
   const uint32_t candidates = from * kBlockLanes;
-  for (uint32_t i = tid; i < candidates; i += 8 * kT) {
-    uint32_t g[8], key[8];
+  for (uint32_t i = tid; i < candidates; i += 4 * kT) {
+    uint32_t g[4], key[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < 4; ++j) {
       const uint32_t n = min(i + j * kT, candidates - 1);
       g[j] = listed_blocks[n / kBlockLanes] * kBlockLanes + n % kBlockLanes;
       key[j] = maxima.groups[g[j]];
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+    for (int j = 0; j < 4; ++j)
       if (i + j * kT < candidates && key[j] >= least) {
-        const uint32_t n = atomicAdd(&s.listed, 1u);
+        const uint32_t n = count_one(s.listed);
         if (n < kGroupsMost) s.groups[n] = g[j];
       }
   }
@@ -551,22 +567,29 @@ template <bool kSmall>
 __device__ __forceinline__ const uint64_t* sorted(uint32_t taken, Selection<kSmall>& s) {
   constexpr int kT = SelectionSize<kSmall>::kT;
   const uint32_t tid = threadIdx.x;
-  // how many of list[first .. end) are larger; eight reads on their way together
+  // how many of list[first .. end) are larger; four reads on their way together
   const auto larger_of = [](const uint64_t* list, uint32_t first, uint32_t end, uint64_t mine) {
     uint32_t rank = 0;
-    for (uint32_t n = first; n < end; n += 8) {
-      uint64_t x[8];
+    for (uint32_t n = first; n < end; n += 4) {
+      uint64_t x[4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = list[min(n + i, end - 1)];
+      for (int i = 0; i < 4; ++i) x[i] = list[min(n + i, end - 1)];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) rank += n + i < end && x[i] > mine;
+      for (int i = 0; i < 4; ++i) rank += n + i < end && x[i] > mine;
     }
     return rank;
   };
   if (taken <= kRankMost) {
+    // 0 is below every logit; the list has room for a whole number of eights
+    if (tid < 8) s.list[taken + tid] = 0;
+    __syncthreads();
     if (tid < taken) {
       const uint64_t mine = s.list[tid];
-      s.other[larger_of(s.list, 0, taken, mine)] = mine;
+      uint32_t rank = 0;
+      for (uint32_t n = 0; n < taken; n += 8)
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) rank += s.list[n + i] > mine;
+      s.other[rank] = mine;
     }
     __syncthreads();
     return s.other;
@@ -638,8 +661,10 @@ __device__ const uint64_t* select_row(const T* row, uint32_t V, Maxima maxima, u
   const uint32_t blocks = segments * kBlocksOf;
   Gathered r{SelectionSize<kSmall>::kList + 1, 0u, false};
   if constexpr (kSmall) {
-    if (2 * k <= blocks && blocks <= 5 * kWave) r = gather_from_blocks<T, kVecs, 5>(row, V, maxima, blocks, k, s);
-    else if (2 * k <= blocks && blocks <= 20 * kWave) r = gather_from_blocks<T, kVecs, 20>(row, V, maxima, blocks, k, s);
+    if (V >= kPerOf<T> && 2 * k <= blocks) {
+      if (blocks <= 5 * kWave) r = gather_from_blocks<T, kVecs, 5>(row, V, maxima, blocks, k, s);
+      else if (blocks <= 20 * kWave) r = gather_from_blocks<T, kVecs, 20>(row, V, maxima, blocks, k, s);
+    }
     __syncthreads();
   }
   if (r.taken > SelectionSize<kSmall>::kList)
