@@ -79,6 +79,23 @@ __device__ __forceinline__ void set_elem(u32x4& v, int e, uint16_t x) {
   v[e >> 1] = (v[e >> 1] & ~(0xFFFFu << shift)) | static_cast<uint32_t>(x) << shift;
 }
 
+
+// -inf in the first n places.
+__device__ __forceinline__ f32x4 without_first(f32x4 v, uint32_t n) {
+#pragma unroll
+  for (uint32_t e = 0; e < 4; ++e)
+    if (e < n) v[e] = -INFINITY;
+  return v;
+}
+__device__ __forceinline__ u32x4 without_first(u32x4 v, uint32_t n) {
+#pragma unroll
+  for (uint32_t e = 0; e < 4; ++e) {
+    const uint32_t low = 2 * e < n ? 0xFF80u : v[e] & 0xFFFFu, high = 2 * e + 1 < n ? 0xFF800000u : v[e] & 0xFFFF0000u;
+    v[e] = low | high;
+  }
+  return v;
+}
+
 template <typename T>
 __device__ __forceinline__ typename VecOf<T>::Value load_whole(const T* row, uint32_t j) {
   return *reinterpret_cast<const typename VecOf<T>::Memory*>(row + j * kPerOf<T>);
@@ -111,10 +128,8 @@ __device__ __forceinline__ Stats join(Stats a, Stats b, float c) {
                    fb * __builtin_fmaf(b.S, fmaxf(db, kScoreFloor), b.A)};
 }
 
-// The row's statistics from its parts, the same in every lane of the wave.
-__device__ __forceinline__ Stats join_parts(const Stats* parts, uint32_t count, float c) {
-  Stats s{-INFINITY, 0.0f, 0.0f};
-  for (uint32_t i = threadIdx.x % kWave; i < count; i += kWave) s = join(s, parts[i], c);
+// Of a wave's lanes, the same in every lane.
+__device__ __forceinline__ Stats join_lanes(Stats s, float c) {
   const float m = wave_largest(s.m);
   const float d = s.m == -INFINITY ? kScoreFloor : (s.m - m) * c;
   const float f = __builtin_amdgcn_exp2f(d);
@@ -122,6 +137,13 @@ __device__ __forceinline__ Stats join_parts(const Stats* parts, uint32_t count, 
   s.S = wave_sum(f * s.S);
   s.m = m;
   return s;
+}
+
+// The row's statistics from its parts, the same in every lane of the wave.
+__device__ __forceinline__ Stats join_parts(const Stats* parts, uint32_t count, float c) {
+  Stats s{-INFINITY, 0.0f, 0.0f};
+  for (uint32_t i = threadIdx.x % kWave; i < count; i += kWave) s = join(s, parts[i], c);
+  return join_lanes(s, c);
 }
 
 // Keys of the largest logits of a row's groups, what one lane reads in the pass, and blocks of 16 groups.
@@ -141,6 +163,26 @@ __device__ __forceinline__ uint32_t row_largest(uint32_t k) {
   k = step(k, __builtin_amdgcn_update_dpp(0, static_cast<int>(k), 0x141, 0xF, 0xF, false));   // row_half_mirror
   return step(k, __builtin_amdgcn_update_dpp(0, static_cast<int>(k), 0x140, 0xF, 0xF, false)); // row_mirror
 }
+
+__device__ __forceinline__ uint32_t wave_highest(uint32_t k) {
+  k = row_largest(k);
+  k = max(k, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(k), 0x142, 0xA, 0xF, false)));
+  k = max(k, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(k), 0x143, 0xC, 0xF, false)));
+  return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(k), 63));
+}
+
+// Sums over logits x relative to a base m.  (Scores by one fma, x c - m c, would save an instruction of ten,
+// but the rounding of m c is past any range for rows masked with the type's lowest value.)
+struct Sums {
+  float base, c, S = 0.0f, A = 0.0f;
+  __device__ __forceinline__ Sums(float m, float c_) : base(m == -INFINITY ? 0.0f : m), c(c_) {}
+  __device__ __forceinline__ void add(float x) {
+    const float y = (x - base) * c;
+    const float p = __builtin_amdgcn_exp2f(y);
+    S += p;
+    A = __builtin_fmaf(p, fmaxf(y, kScoreFloor), A);   // 0 * -inf is no part of the sum
+  }
+};
 
 // The streaming pass: one read of every logit.  A workgroup takes a segment of kThreads * kVecs
 // vectors of a row, a lane kVecs of them, kThreads vectors apart.  A wave writes the statistics
@@ -180,21 +222,15 @@ row_pass_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row
     }
     if (kStats) {
       m = wave_largest(m);
-      const float base = m == -INFINITY ? 0.0f : m;
-      float S = 0.0f, A = 0.0f;
+      Sums sums(m, c);
 #pragma unroll
       for (int u = 0; u < kVecs; ++u)
 #pragma unroll
-        for (uint32_t e = 0; e < kPer; ++e) {
-          const float y = (elem(x[u], e) - base) * c;
-          const float p = __builtin_amdgcn_exp2f(y);
-          S += p;
-          A = __builtin_fmaf(p, fmaxf(y, kScoreFloor), A);
-        }
-      S = wave_sum(S);
-      A = wave_sum(A);
+        for (uint32_t e = 0; e < kPer; ++e) sums.add(elem(x[u], e));
+      sums.S = wave_sum(sums.S);
+      sums.A = wave_sum(sums.A);
       if (threadIdx.x % kWave == 0)
-        parts[segment * (kThreads / kWave) + threadIdx.x / kWave] = Stats{m, S, A};
+        parts[segment * (kThreads / kWave) + threadIdx.x / kWave] = Stats{m, sums.S, sums.A};
     }
   }
 }
@@ -210,10 +246,12 @@ row_pass_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row
 // Where too many groups tie at t (a mask, equal logits), only what lies above t is gathered,
 // fewer than k groups, and the rest are the first columns that equal t.
 // ---------------------------------------------------------------------------
-// Two sizes: a few hundred logits by 4 waves, up to 1024 by 16.
-template <bool kSmall>
+// kT lanes select; the row's groups were read by kLanes lanes at a time.  Two sizes: a few hundred logits, or up
+// to 1024.
+template <int kT_, int kLanes_, bool kSmall_>
 struct SelectionSize {
-  static constexpr int kT = kSmall ? 256 : 1024;
+  static constexpr int kT = kT_, kLanes = kLanes_, kBlocks = kLanes / kBlockLanes;
+  static constexpr bool kSmall = kSmall_;
   static constexpr uint32_t kList = kSmall ? 1024 : 4096;     // gathered logits
   static constexpr uint32_t kGroups = kSmall ? 512 : 2048;    // listed groups
 };
@@ -221,19 +259,18 @@ constexpr uint32_t kSmallMost = 256;     // k of the small size
 constexpr uint32_t kRankMost = 128;      // gathered logits that are ordered by counting all of them
 constexpr uint32_t kBuckets = 256;       // the others are counted in their bucket of keys
 
-template <bool kSmall>
+template <typename Size>
 struct Selection {
-  static constexpr int kT = SelectionSize<kSmall>::kT;
-  uint64_t list[SelectionSize<kSmall>::kList], other[SelectionSize<kSmall>::kList];
+  uint64_t list[Size::kList], other[Size::kList];
   uint32_t starts[kBuckets];
-  uint32_t groups[SelectionSize<kSmall>::kGroups], slots[2][kT / kWave];
-  uint32_t taken, listed, blocks;
+  uint32_t groups[Size::kGroups], slots[2][Size::kT / kWave];
+  uint32_t taken, listed, blocks, key, from;
 };
 
 // The sum over the workgroup of one number a wave; `turn` alternates.
-template <bool kSmall>
-__device__ __forceinline__ uint32_t group_sum(uint32_t of_wave, Selection<kSmall>& s, uint32_t turn) {
-  constexpr int kT = SelectionSize<kSmall>::kT;
+template <typename Size>
+__device__ __forceinline__ uint32_t group_sum(uint32_t of_wave, Selection<Size>& s, uint32_t turn) {
+  constexpr int kT = Size::kT;
   if (threadIdx.x % kWave == 0) s.slots[turn & 1][threadIdx.x / kWave] = of_wave;
   __syncthreads();
   uint32_t n = 0;
@@ -273,14 +310,14 @@ __device__ __forceinline__ uint32_t count_one(uint32_t& counter) {
 
 // Appends the wanted logits of the listed groups to the list (counting on beyond its end).  The row has at
 // least one whole vector: a partial one is read as the last kPer columns, without those before it.
-template <typename T, int kVecs, bool kSmall, typename F>
-__device__ __forceinline__ void gather_listed(const T* row, uint32_t V, Selection<kSmall>& s, F wanted) {
+template <typename T, int kVecs, typename Size, typename F>
+__device__ __forceinline__ void gather_listed(const T* row, uint32_t V, Selection<Size>& s, F wanted) {
   constexpr uint32_t kPer = kPerOf<T>;
-  constexpr int kT = SelectionSize<kSmall>::kT;
+  constexpr int kT = Size::kT;
   const uint32_t items = s.listed * kVecs;
   const auto column_of = [&](uint32_t item) {
     const uint32_t g = s.groups[item / kVecs];
-    return (g / kThreads * (kThreads * kVecs) + item % kVecs * kThreads + g % kThreads) * kPer;
+    return (g / Size::kLanes * (Size::kLanes * kVecs) + item % kVecs * Size::kLanes + g % Size::kLanes) * kPer;
   };
   const auto load_at = [&](uint32_t column) {
     return *reinterpret_cast<const typename VecOf<T>::Memory*>(row + min(column, V - kPer));
@@ -297,7 +334,7 @@ __device__ __forceinline__ void gather_listed(const T* row, uint32_t V, Selectio
       const uint32_t key = order_key(elem(x, e));
       if (wanted(key) && first + e >= column) {
         const uint32_t at = count_one(s.taken);
-        if (at < SelectionSize<kSmall>::kList) s.list[at] = static_cast<uint64_t>(key) << 32 | ~(first + e);
+        if (at < Size::kList) s.list[at] = static_cast<uint64_t>(key) << 32 | ~(first + e);
       }
     }
     x = next;
@@ -313,12 +350,12 @@ struct Gathered {
 };
 
 // Whatever the row holds.
-template <typename T, int kVecs, bool kSmall>
-__device__ __forceinline__ Gathered gather_any(const T* row, uint32_t V, const uint32_t* __restrict__ maxima,
-                                            uint32_t groups, uint32_t k, Selection<kSmall>& s) {
+template <typename T, int kVecs, typename Size>
+__device__ __forceinline__ Gathered gather_any(const T* row, uint32_t V, const uint32_t* maxima,
+                                            uint32_t groups, uint32_t k, Selection<Size>& s) {
   constexpr uint32_t kPer = kPerOf<T>;
-  constexpr int kT = SelectionSize<kSmall>::kT, kHeld = 8;
-  constexpr uint32_t kListMost = SelectionSize<kSmall>::kList, kGroupsMost = SelectionSize<kSmall>::kGroups;
+  constexpr int kT = Size::kT, kHeld = 8;
+  constexpr uint32_t kListMost = Size::kList, kGroupsMost = Size::kGroups;
   const uint32_t tid = threadIdx.x;
   uint32_t turn = 0;
   uint32_t held[kHeld];
@@ -383,7 +420,7 @@ __device__ __forceinline__ Gathered gather_any(const T* row, uint32_t V, const u
   const auto each_listed = [&](auto&& f) {
     for (uint32_t i = tid; i < items; i += kT) {
       const uint32_t g = s.groups[i / kVecs];
-      const uint32_t j = g / kThreads * (kThreads * kVecs) + i % kVecs * kThreads + g % kThreads;
+      const uint32_t j = g / Size::kLanes * (Size::kLanes * kVecs) + i % kVecs * Size::kLanes + g % Size::kLanes;
       const auto x = load_any(row, V, j);
 #pragma unroll
       for (uint32_t e = 0; e < kPer; ++e)
@@ -440,11 +477,11 @@ __device__ __forceinline__ Gathered gather_any(const T* row, uint32_t V, const u
 }
 
 // The list filled up to k by the first columns that equal `key`.
-template <typename T, bool kSmall>
+template <typename T, typename Size>
 __device__ __forceinline__ void fill_equal(const T* row, uint32_t V, uint32_t k, uint32_t taken, uint32_t key,
-                                        Selection<kSmall>& s) {
+                                        Selection<Size>& s) {
   constexpr uint32_t kPer = kPerOf<T>;
-  constexpr int kT = SelectionSize<kSmall>::kT;
+  constexpr int kT = Size::kT;
   const uint32_t tid = threadIdx.x;
   uint32_t turn = 0;
   __syncthreads();
@@ -483,62 +520,70 @@ __device__ __forceinline__ void fill_equal(const T* row, uint32_t V, uint32_t k,
 
 // The same for k that the blocks' maxima suffice for; `taken` is more than the list holds where they do not
 // (the row's largest logits stand together).  A wave holds kHeld * 64 blocks.
-template <typename T, int kVecs, int kHeld>
+template <typename T, int kVecs, int kHeld, typename Size>
 __device__ __forceinline__ Gathered gather_from_blocks(const T* row, uint32_t V, Maxima maxima, uint32_t blocks,
-                                                       uint32_t k, Selection<true>& s) {
-  constexpr uint32_t kPer = kPerOf<T>;
-  constexpr int kT = SelectionSize<true>::kT;
-  constexpr uint32_t kListMost = SelectionSize<true>::kList, kGroupsMost = SelectionSize<true>::kGroups;
-  const uint32_t tid = threadIdx.x, lane = tid % kWave;
-  uint32_t held[kHeld];
-  uint32_t highest = 0;
+                                                       uint32_t k, Selection<Size>& s) {
+  constexpr int kT = Size::kT;
+  constexpr uint32_t kListMost = Size::kList, kGroupsMost = Size::kGroups;
+  const uint32_t tid = threadIdx.x;
+  uint32_t* const listed_blocks = reinterpret_cast<uint32_t*>(s.list);   // until the logits are gathered
+  if (tid < kWave) {
+    uint32_t held[kHeld];
+    uint32_t highest = 0;
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) held[i] = lane + i * kWave < blocks ? maxima.blocks[lane + i * kWave] : 0u;
-  if (tid == 0) s.taken = s.listed = s.blocks = 0;
+    for (int i = 0; i < kHeld; ++i) held[i] = tid + i * kWave < blocks ? maxima.blocks[tid + i * kWave] : 0u;
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) highest = max(highest, held[i]);
-  highest = row_largest(highest);
-  highest = max(highest, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(highest), 0x142, 0xA, 0xF, false)));
-  highest = max(highest, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(highest), 0x143, 0xC, 0xF, false)));
-  highest = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(highest), 63));
-  const auto blocks_from = [&](uint32_t t) {
-    uint32_t n = 0;
+    for (int i = 0; i < kHeld; ++i) highest = max(highest, held[i]);
+    highest = wave_highest(highest);
+    const auto blocks_from = [&](uint32_t t) {
+      uint32_t n = 0;
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) n += __popcll(__ballot(held[i] >= t));
-    return n;
-  };
-  // every wave takes the same steps
-  const uint32_t most = k + k / 4 + 16;
-  Bisection at{kLowestKey, highest};
-  uint32_t from = blocks;
-  const uint32_t at_highest = blocks_from(highest);
-  if (at_highest >= k) {
-    at.lo = highest;
-    from = at_highest;
-  }
-  while (from > most && at.hi - at.lo > 1) {
-    const uint32_t mid = at.middle();
-    const uint32_t n = blocks_from(mid);
-    if (n >= k) {
-      at.lo = mid;
-      from = n;
-    } else {
-      at.hi = mid;
+      for (int i = 0; i < kHeld; ++i) n += __popcll(__ballot(held[i] >= t));
+      return n;
+    };
+    const uint32_t most = k + k / 4 + 16;
+    Bisection at{kLowestKey, highest};
+    uint32_t from = blocks;
+    const uint32_t at_highest = blocks_from(highest);
+    if (at_highest >= k) {
+      at.lo = highest;
+      from = at_highest;
+    }
+    while (from > most && at.hi - at.lo > 1) {
+      const uint32_t mid = at.middle();
+      const uint32_t n = blocks_from(mid);
+      if (n >= k) {
+        at.lo = mid;
+        from = n;
+      } else {
+        at.hi = mid;
+      }
+    }
+    // too many blocks tie at at.lo: those above it, fewer than k
+    const bool above = from > most;
+    uint32_t listed = 0;
+    if (!above || at.lo != 0xFFFFFFFFu) {
+      const uint32_t least = at.lo + (above ? 1u : 0u);
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) {
+        const uint64_t mask = __ballot(held[i] >= least);
+        if (held[i] >= least)
+          listed_blocks[listed + __popcll(mask & ((uint64_t{1} << tid) - 1u))] = tid + i * kWave;
+        listed += __popcll(mask);
+      }
+    }
+    if (tid == 0) {
+      s.taken = s.listed = 0;
+      s.blocks = listed;
+      s.key = at.lo;
+      s.from = above;
     }
   }
-  // too many blocks tie at at.lo: those above it, fewer than k
-  const bool above = from > most;
-  const uint32_t least = above ? min(at.lo, 0xFFFFFFFEu) + 1u : at.lo;
-  if (above) from = at.lo == 0xFFFFFFFFu ? 0u : blocks_from(least);
   __syncthreads();
-  uint32_t* const listed_blocks = reinterpret_cast<uint32_t*>(s.list);   // until the logits are gathered
-#pragma unroll
-  for (int i = 0; i < kHeld; ++i)
-    if (i % (kT / kWave) == static_cast<int>(tid / kWave) && held[i] >= least && from > 0)
-      listed_blocks[count_one(s.blocks)] = lane + i * kWave;
-  __syncthreads();
+  const bool above = s.from != 0;
+  const uint32_t key_at = s.key, least = key_at + (above ? 1u : 0u);
   // the blocks' groups that reach the threshold, and their logits; several loads of a lane on their way together
-  const uint32_t candidates = from * kBlockLanes;
+  const uint32_t candidates = s.blocks * kBlockLanes;
   for (uint32_t i = tid; i < candidates; i += 4 * kT) {
     uint32_t g[4], key[4];
 #pragma unroll
@@ -555,17 +600,17 @@ __device__ __forceinline__ Gathered gather_from_blocks(const T* row, uint32_t V,
       }
   }
   __syncthreads();
-  if (s.listed > kGroupsMost) return Gathered{kListMost + 1, at.lo, above};
+  if (s.listed > kGroupsMost) return Gathered{kListMost + 1, key_at, above};
   gather_listed<T, kVecs>(row, V, s, [&](uint32_t key) { return key >= least; });
   __syncthreads();
-  return Gathered{s.taken, at.lo, above};
+  return Gathered{s.taken, key_at, above};
 }
 
 // The gathered logits in order: each to the place that counting the larger ones gives it.  Many are first put
 // into buckets of neighbouring keys, in order of the buckets, so that only those of its bucket are counted.
-template <bool kSmall>
-__device__ __forceinline__ const uint64_t* sorted(uint32_t taken, Selection<kSmall>& s) {
-  constexpr int kT = SelectionSize<kSmall>::kT;
+template <typename Size>
+__device__ __forceinline__ const uint64_t* sorted(uint32_t taken, Selection<Size>& s) {
+  constexpr int kT = Size::kT;
   const uint32_t tid = threadIdx.x;
   // how many of list[first .. end) are larger; four reads on their way together
   const auto larger_of = [](const uint64_t* list, uint32_t first, uint32_t end, uint64_t mine) {
@@ -654,21 +699,33 @@ __device__ __forceinline__ const uint64_t* sorted(uint32_t taken, Selection<kSma
   return s.list;
 }
 
-template <typename T, int kVecs, bool kSmall>
-__device__ const uint64_t* select_row(const T* row, uint32_t V, Maxima maxima, uint32_t segments, uint32_t k,
-                                      Selection<kSmall>& s) {
+// A function of its own, not part of its kernels: within them it has too few scalar registers and takes a third
+// longer (1024 of 16 x 151936: 33 us, 24 so).  Its pointers carry their address spaces, or every
+// access of LDS and memory would be a flat one.
+#define SBW_LDS __attribute__((address_space(3)))
+#define SBW_GLOBAL __attribute__((address_space(1)))
+template <typename T, int kVecs, typename Size, bool kOfLds>
+__device__ __noinline__ const uint64_t* select_row(const SBW_GLOBAL T* row_, uint32_t V, const SBW_GLOBAL uint32_t* global_groups,
+                                                   const SBW_GLOBAL uint32_t* global_blocks,
+                                                   const SBW_LDS uint32_t* lds_groups,
+                                                   const SBW_LDS uint32_t* lds_blocks, uint32_t segments, uint32_t k,
+                                                   SBW_LDS Selection<Size>* selection) {
+  const T* row = (const T*)row_;
+  Selection<Size>& s = *(Selection<Size>*)selection;
+  const Maxima maxima = kOfLds ? Maxima{(uint32_t*)lds_groups, (uint32_t*)lds_blocks}
+                               : Maxima{(uint32_t*)global_groups, (uint32_t*)global_blocks};
   k = min(k, V);
-  const uint32_t blocks = segments * kBlocksOf;
-  Gathered r{SelectionSize<kSmall>::kList + 1, 0u, false};
-  if constexpr (kSmall) {
+  const uint32_t blocks = segments * Size::kBlocks;
+  Gathered r{Size::kList + 1, 0u, false};
+  if constexpr (Size::kSmall) {
     if (V >= kPerOf<T> && 2 * k <= blocks) {
-      if (blocks <= 5 * kWave) r = gather_from_blocks<T, kVecs, 5>(row, V, maxima, blocks, k, s);
-      else if (blocks <= 20 * kWave) r = gather_from_blocks<T, kVecs, 20>(row, V, maxima, blocks, k, s);
+      if (blocks <= 5 * kWave) r = gather_from_blocks<T, kVecs, 5, Size>(row, V, maxima, blocks, k, s);
+      else if (blocks <= 20 * kWave) r = gather_from_blocks<T, kVecs, 20, Size>(row, V, maxima, blocks, k, s);
     }
     __syncthreads();
   }
-  if (r.taken > SelectionSize<kSmall>::kList)
-    r = gather_any<T, kVecs, kSmall>(row, V, maxima.groups, segments * kThreads, k, s);
+  if (r.taken > Size::kList)
+    r = gather_any<T, kVecs, Size>(row, V, maxima.groups, segments * Size::kLanes, k, s);
   if (r.above && r.taken < k) {
     fill_equal(row, V, k, r.taken, r.key, s);
     r.taken = k;
@@ -676,93 +733,164 @@ __device__ const uint64_t* select_row(const T* row, uint32_t V, Maxima maxima, u
   return sorted(r.taken, s);
 }
 
-// After the pass: one workgroup a row joins the statistics, looks up the given tokens and
-// selects the alternatives.
-template <typename T, int kVecs, bool kSmall>
-__global__ void __launch_bounds__(SelectionSize<kSmall>::kT)
-token_logprobs_top_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride,
-                          const int32_t* __restrict__ tokens, uint32_t n, float inv_t, uint32_t top,
-                          uint32_t segments, const Stats* __restrict__ parts,
-                          Maxima maxima, float* __restrict__ logprobs,
-                          float* __restrict__ lse, float* __restrict__ entropy,
-                          float* __restrict__ stats, int32_t* __restrict__ top_ids,
-                          float* __restrict__ top_logprobs) {
-  constexpr int kT = SelectionSize<kSmall>::kT;
-  __shared__ Selection<kSmall> s;
-  const uint32_t tid = threadIdx.x;
+// ---------------------------------------------------------------------------
+// What a call writes for each row.
+// ---------------------------------------------------------------------------
+struct Outputs {
+  const int32_t* tokens;
+  uint32_t n, top;
+  float inv_t;
+  uint32_t vbase;          // of the candidates' ids
+  float *logprobs, *lse, *entropy, *stats;
+  int32_t* top_ids;
+  float* top_values;       // log probabilities, or logits of candidates
+};
+
+// A lane's given token, read before its row's statistics are known.
+template <typename T>
+struct Given {
+  int32_t token = -1;
+  float logit = 0.0f;
+  __device__ __forceinline__ Given(const Outputs& o, int64_t b, const T* row, uint32_t V, uint32_t j) {
+    if (j < o.n) token = o.tokens[b * o.n + j];
+    if (token >= 0 && static_cast<uint32_t>(token) < V) logit = logit_of(row[token]);
+    else token = -1;
+  }
+};
+
+// Log sum, entropy and the given tokens' log probabilities, by `lanes` lanes; ln S.
+template <typename T>
+__device__ __forceinline__ float write_statistics(const Outputs& o, int64_t b, const T* row, uint32_t V, Stats r,
+                                                  Given<T> given, uint32_t lane, uint32_t lanes) {
+  const float ln_s = logf(r.S);
+  const bool empty = r.m == -INFINITY;
+  if (lane == 0) {
+    if (o.lse != nullptr) o.lse[b] = empty ? -INFINITY : __builtin_fmaf(r.m, o.inv_t, ln_s);
+    if (o.entropy != nullptr) o.entropy[b] = empty ? 0.0f : ln_s - kLn2 * (r.A / r.S);
+    if (o.stats != nullptr) o.stats[2 * b] = r.m, o.stats[2 * b + 1] = ln_s;
+  }
+  for (uint32_t j = lane; j < o.n; j += lanes) {
+    if (j != lane) given = Given<T>(o, b, row, V, j);
+    o.logprobs[b * o.n + j] =
+        given.token < 0 ? 0.0f : empty ? -INFINITY : logprob_of(given.logit, r.m, o.inv_t, ln_s);
+  }
+  return ln_s;
+}
+
+// The selected columns with their log probabilities (kStats) or logits.
+template <bool kStats>
+__device__ __forceinline__ void write_selected(const Outputs& o, int64_t b, uint32_t V, const uint64_t* best, float m,
+                                               float ln_s, uint32_t lanes) {
+  for (uint32_t j = threadIdx.x; j < o.top; j += lanes) {
+    const bool some = j < V;
+    const uint64_t x = best[some ? j : 0u];
+    const float logit = logit_of_key(static_cast<uint32_t>(x >> 32));
+    o.top_ids[b * o.top + j] = some ? static_cast<int32_t>(o.vbase + ~static_cast<uint32_t>(x)) : -1;
+    if (o.top_values == nullptr) continue;
+    o.top_values[b * o.top + j] = !some                              ? -INFINITY
+                                  : !kStats                         ? logit
+                                  : m == -INFINITY                   ? -INFINITY
+                                                                     : logprob_of(logit, m, o.inv_t, ln_s);
+  }
+}
+
+// After the pass.  Without a selection one wave a row joins the statistics and writes; with one a workgroup.
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+join_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride, uint32_t segments,
+            const Stats* __restrict__ parts, Outputs o) {
+  for (int64_t b = static_cast<int64_t>(blockIdx.x) * (kThreads / kWave) + threadIdx.x / kWave; b < B;
+       b += static_cast<int64_t>(gridDim.x) * (kThreads / kWave)) {
+    const uint32_t count = segments * (kThreads / kWave), lane = threadIdx.x % kWave;
+    const T* row = logits + b * row_stride;
+    const Given<T> given(o, b, row, V, lane);
+    const Stats r = join_parts(parts + b * count, count, o.inv_t * kLog2e);
+    write_statistics(o, b, row, V, r, given, lane, kWave);
+  }
+}
+
+template <typename T, int kVecs, typename Size, bool kStats>
+__global__ void __launch_bounds__(Size::kT)
+select_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride, uint32_t segments,
+              const Stats* __restrict__ parts, Maxima maxima, Outputs o) {
+  __shared__ Selection<Size> s;
+  __shared__ float of_row[2];
   for (int64_t b = blockIdx.x; b < B; b += gridDim.x) {
     const T* row = logits + b * row_stride;
-    const uint32_t count = segments * (kThreads / kWave);
-    const Stats r = join_parts(parts + b * count, count, inv_t * kLog2e);
-    const float ln_s = logf(r.S);
-    const bool empty = r.m == -INFINITY;
-    if (tid == 0) {
-      if (lse != nullptr) lse[b] = empty ? -INFINITY : __builtin_fmaf(r.m, inv_t, ln_s);
-      if (entropy != nullptr) entropy[b] = empty ? 0.0f : ln_s - kLn2 * (r.A / r.S);
-      if (stats != nullptr) stats[2 * b] = r.m, stats[2 * b + 1] = ln_s;
+    // the statistics are the other waves' while the first one looks for the threshold
+    if (kStats && threadIdx.x >= kWave) {
+      const uint32_t lane = threadIdx.x - kWave, count = segments * (kThreads / kWave);
+      const Given<T> given(o, b, row, V, lane);
+      const Stats r = join_parts(parts + b * count, count, o.inv_t * kLog2e);
+      const float ln_s = write_statistics(o, b, row, V, r, given, lane, Size::kT - kWave);
+      if (lane == 0) of_row[0] = r.m, of_row[1] = ln_s;
     }
-    for (uint32_t j = tid; j < n; j += kT) {
-      const int32_t t = tokens[b * n + j];
-      const bool token = t >= 0 && static_cast<uint32_t>(t) < V;
-      logprobs[b * n + j] = !token ? 0.0f : empty ? -INFINITY : logprob_of(logit_of(row[t]), r.m, inv_t, ln_s);
-    }
-    const uint64_t* best = select_row<T, kVecs>(row, V, row_maxima(maxima, b, segments), segments, top, s);
-    for (uint32_t j = tid; j < top; j += kT) {
-      const bool some = j < V;
-      top_ids[b * top + j] = some ? static_cast<int32_t>(~static_cast<uint32_t>(best[j])) : -1;
-      if (top_logprobs != nullptr)
-        top_logprobs[b * top + j] =
-            !some || empty ? -INFINITY
-                           : logprob_of(logit_of_key(static_cast<uint32_t>(best[j] >> 32)), r.m, inv_t, ln_s);
-    }
+    const Maxima m = row_maxima(maxima, b, segments);
+    const uint64_t* best = select_row<T, kVecs, Size, false>(
+        (const SBW_GLOBAL T*)row, V, (const SBW_GLOBAL uint32_t*)m.groups, (const SBW_GLOBAL uint32_t*)m.blocks,
+        nullptr, nullptr, segments, o.top, (SBW_LDS Selection<Size>*)&s);
+    write_selected<kStats>(o, b, V, best, of_row[0], of_row[1], Size::kT);
     __syncthreads();
   }
 }
 
-// The same without alternatives: one wave a row.
+// ---------------------------------------------------------------------------
+// Candidates in one launch: a workgroup reads its row in rounds of kT * kVecs vectors, the next round's
+// loads on their way while this one is looked at, keeps the groups' maxima in LDS and selects from there.
+// (The statistics cost too many instructions a logit for one CU to take a row: 14 us for one row of 152064,
+// 5.7 with its segments spread over the chip; and 60 us against 59 for 512 rows.)
+// ---------------------------------------------------------------------------
+// Vector j as load_any, without a branch, for rows of at least one whole vector.
 template <typename T>
-__global__ void __launch_bounds__(kThreads)
-token_logprobs_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride,
-                      const int32_t* __restrict__ tokens, uint32_t n, float inv_t, uint32_t segments,
-                      const Stats* __restrict__ parts, float* __restrict__ logprobs,
-                      float* __restrict__ lse, float* __restrict__ entropy, float* __restrict__ stats) {
-  const uint32_t lane = threadIdx.x % kWave;
-  for (int64_t b = static_cast<int64_t>(blockIdx.x) * (kThreads / kWave) + threadIdx.x / kWave; b < B;
-       b += static_cast<int64_t>(gridDim.x) * (kThreads / kWave)) {
-    const uint32_t count = segments * (kThreads / kWave);
-    const Stats r = join_parts(parts + b * count, count, inv_t * kLog2e);
-    const float ln_s = logf(r.S);
-    const bool empty = r.m == -INFINITY;
-    if (lane == 0) {
-      if (lse != nullptr) lse[b] = empty ? -INFINITY : __builtin_fmaf(r.m, inv_t, ln_s);
-      if (entropy != nullptr) entropy[b] = empty ? 0.0f : ln_s - kLn2 * (r.A / r.S);
-      if (stats != nullptr) stats[2 * b] = r.m, stats[2 * b + 1] = ln_s;
-    }
-    for (uint32_t j = lane; j < n; j += kWave) {
-      const int32_t t = tokens[b * n + j];
-      const bool token = t >= 0 && static_cast<uint32_t>(t) < V;
-      logprobs[b * n + j] = !token ? 0.0f
-                            : empty ? -INFINITY
-                                    : logprob_of(logit_of(logits[b * row_stride + t]), r.m, inv_t, ln_s);
-    }
-  }
+__device__ __forceinline__ typename VecOf<T>::Value load_end(const T* row, uint32_t V, uint32_t j) {
+  const uint32_t at = j * kPerOf<T>, first = min(at, V - kPerOf<T>);
+  const typename VecOf<T>::Value v = *reinterpret_cast<const typename VecOf<T>::Memory*>(row + first);
+  return without_first(v, at - first);
 }
 
-template <typename T, int kVecs, bool kSmall>
-__global__ void __launch_bounds__(SelectionSize<kSmall>::kT)
-top_candidates_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride,
-                      uint32_t vbase, uint32_t k, uint32_t segments,
-                      Maxima maxima, int32_t* __restrict__ ids,
-                      float* __restrict__ values) {
-  constexpr int kT = SelectionSize<kSmall>::kT;
-  __shared__ Selection<kSmall> s;
+template <typename T, int kVecs, typename Size, int kRounds>
+__global__ void __launch_bounds__(Size::kT)
+row_select_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride, Outputs o) {
+  constexpr int kT = Size::kT;
+  constexpr uint32_t kPer = kPerOf<T>;
+  static_assert(kT == Size::kLanes, "every lane reads and selects");
+  __shared__ Selection<Size> s;
+  __shared__ uint32_t group_maxima[kRounds * kT], block_maxima[kRounds * Size::kBlocks];
+  const uint32_t tid = threadIdx.x;
+  constexpr uint32_t kRound = kPer * kT * kVecs;
+  const uint32_t whole = V / kRound, rounds = (V + kRound - 1) / kRound;
   for (int64_t b = blockIdx.x; b < B; b += gridDim.x) {
-    const uint64_t* best = select_row<T, kVecs>(logits + b * row_stride, V, row_maxima(maxima, b, segments), segments, k, s);
-    for (uint32_t j = threadIdx.x; j < k; j += kT) {
-      ids[b * k + j] = j < V ? static_cast<int32_t>(vbase + ~static_cast<uint32_t>(best[j])) : -1;
-      if (values != nullptr)
-        values[b * k + j] = j < V ? logit_of_key(static_cast<uint32_t>(best[j] >> 32)) : -INFINITY;
+    const T* row = logits + b * row_stride;
+    const auto load = [&](typename VecOf<T>::Value (&x)[kVecs], uint32_t round) {
+      const uint32_t j = round * (kT * kVecs) + tid;
+      if (round < whole) {
+#pragma unroll
+        for (int u = 0; u < kVecs; ++u) x[u] = load_whole(row, j + u * kT);
+      } else {
+#pragma unroll
+        for (int u = 0; u < kVecs; ++u) x[u] = load_end(row, V, j + u * kT);
+      }
+    };
+    typename VecOf<T>::Value x[kVecs], next[kVecs];
+    load(x, 0);
+    for (uint32_t round = 0; round < rounds; ++round) {
+      load(next, min(round + 1, rounds - 1));
+      float m = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < kVecs; ++u)
+#pragma unroll
+        for (uint32_t e = 0; e < kPer; ++e) m = larger(m, elem(x[u], e));
+      const uint32_t key = order_key(m), of_block = row_largest(key);
+      group_maxima[round * kT + tid] = key;
+      if (tid % kBlockLanes == 0) block_maxima[round * Size::kBlocks + tid / kBlockLanes] = of_block;
+#pragma unroll
+      for (int u = 0; u < kVecs; ++u) x[u] = next[u];
     }
+    __syncthreads();
+    const uint64_t* best = select_row<T, kVecs, Size, true>(
+        (const SBW_GLOBAL T*)row, V, nullptr, nullptr, (const SBW_LDS uint32_t*)group_maxima,
+        (const SBW_LDS uint32_t*)block_maxima, rounds, o.top, (SBW_LDS Selection<Size>*)&s);
+    write_selected<false>(o, b, V, best, 0.0f, 0.0f, kT);
     __syncthreads();
   }
 }
@@ -936,47 +1064,48 @@ void launch_pass(const T* logits, int64_t B, uint32_t V, int64_t row_stride, flo
   kernel<<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, c, reinterpret_cast<Stats*>(parts), maxima);
 }
 
-template <typename T>
-void launch_logprobs(const void* logits_, int64_t B, uint32_t V, int64_t row_stride, const int32_t* tokens,
-                     uint32_t n, float inv_t, uint32_t top, float* logprobs, float* lse, float* entropy,
-                     float* stats, int32_t* top_ids, float* top_logprobs, uint64_t* workspace, hipStream_t stream) {
-  const T* logits = static_cast<const T*>(logits_);
-  const auto segments = static_cast<uint32_t>(segments_of(B, V, top));
-  const auto* parts = reinterpret_cast<const Stats*>(workspace);
-  const float c = inv_t * kLog2e;
-  if (top == 0) {
-    launch_pass<T, true, false>(logits, B, V, row_stride, c, top, workspace, Maxima{}, stream);
-    const dim3 grid(static_cast<uint32_t>(grid_for((B + 3) / 4)));
-    token_logprobs_kernel<T><<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, tokens, n, inv_t, segments,
-                                                             parts, logprobs, lse, entropy, stats);
-    return;
-  }
-  const Maxima maxima = maxima_at(workspace + B * segments * kPartElems, B, segments);
-  launch_pass<T, true, true>(logits, B, V, row_stride, c, top, workspace, maxima, stream);
-  const bool of_long = long_segments(B, V, top), small = top <= kSmallMost;
-  auto* kernel = of_long ? (small ? token_logprobs_top_kernel<T, kLongVecs<T>, true>
-                                  : token_logprobs_top_kernel<T, kLongVecs<T>, false>)
-                         : (small ? token_logprobs_top_kernel<T, kShortVecs<T>, true>
-                                  : token_logprobs_top_kernel<T, kShortVecs<T>, false>);
-  kernel<<<static_cast<uint32_t>(grid_for(B)), small ? SelectionSize<true>::kT : SelectionSize<false>::kT, 0, stream>>>(
-      logits, B, V, row_stride, tokens, n, inv_t, top, segments, parts, maxima, logprobs, lse, entropy, stats,
-      top_ids, top_logprobs);
+// Candidates that take one launch: k of the small size, rows whose groups LDS holds.
+constexpr int kRowLong = 8, kRowShort = 16;   // rounds of 32768 and 8192 logits
+using RowSize = SelectionSize<1024, 1024, true>;
+bool row_takes_long(int64_t V, int64_t k) { return V / (32 * kBlockLanes) >= 2 * k; }
+bool one_launch(int64_t V, int64_t k) {
+  return k <= kSmallMost && V >= 64 && V <= (row_takes_long(V, k) ? kRowLong * 32768 : kRowShort * 8192);
 }
 
-template <typename T>
-void launch_candidates(const void* logits_, int64_t B, uint32_t V, int64_t row_stride, uint32_t vbase, uint32_t k,
-                       int32_t* ids, float* values, uint64_t* workspace, hipStream_t stream) {
+template <typename T, bool kStats>
+void launch_rows(const void* logits_, int64_t B, uint32_t V, int64_t row_stride, const Outputs& o,
+                 uint64_t* workspace, hipStream_t stream) {
   const T* logits = static_cast<const T*>(logits_);
-  const auto segments = static_cast<uint32_t>(segments_of(B, V, k));
-  const Maxima maxima = maxima_at(workspace, B, segments);
-  launch_pass<T, false, true>(logits, B, V, row_stride, 1.0f, k, nullptr, maxima, stream);
-  const bool of_long = long_segments(B, V, k), small = k <= kSmallMost;
-  auto* kernel = of_long ? (small ? top_candidates_kernel<T, kLongVecs<T>, true>
-                                  : top_candidates_kernel<T, kLongVecs<T>, false>)
-                         : (small ? top_candidates_kernel<T, kShortVecs<T>, true>
-                                  : top_candidates_kernel<T, kShortVecs<T>, false>);
-  kernel<<<static_cast<uint32_t>(grid_for(B)), small ? SelectionSize<true>::kT : SelectionSize<false>::kT, 0, stream>>>(
-      logits, B, V, row_stride, vbase, k, segments, maxima, ids, values);
+  const uint32_t rows = static_cast<uint32_t>(grid_for(B));
+  const bool small = o.top <= kSmallMost;
+  if constexpr (!kStats) {
+    if (one_launch(V, o.top)) {
+      auto* kernel = row_takes_long(V, o.top) ? row_select_kernel<T, kLongVecs<T>, RowSize, kRowLong>
+                                              : row_select_kernel<T, kShortVecs<T>, RowSize, kRowShort>;
+      kernel<<<rows, RowSize::kT, 0, stream>>>(logits, B, V, row_stride, o);
+      return;
+    }
+  }
+  const auto segments = static_cast<uint32_t>(segments_of(B, V, o.top));
+  const auto* parts = reinterpret_cast<const Stats*>(workspace);
+  const float c = o.inv_t * kLog2e;
+  if (o.top == 0) {
+    if constexpr (kStats) {
+      launch_pass<T, true, false>(logits, B, V, row_stride, c, 0, workspace, Maxima{}, stream);
+      join_kernel<T><<<static_cast<uint32_t>(grid_for((B + 3) / 4)), kThreads, 0, stream>>>(
+          logits, B, V, row_stride, segments, parts, o);
+    }
+    return;
+  }
+  const Maxima maxima = maxima_at(workspace + (kStats ? B * segments * kPartElems : 0), B, segments);
+  launch_pass<T, kStats, true>(logits, B, V, row_stride, c, o.top, workspace, maxima, stream);
+  using Small = SelectionSize<256, kThreads, true>;
+  using Large = SelectionSize<1024, kThreads, false>;
+  auto* kernel = long_segments(B, V, o.top) ? (small ? select_kernel<T, kLongVecs<T>, Small, kStats>
+                                                     : select_kernel<T, kLongVecs<T>, Large, kStats>)
+                                            : (small ? select_kernel<T, kShortVecs<T>, Small, kStats>
+                                                     : select_kernel<T, kShortVecs<T>, Large, kStats>);
+  kernel<<<rows, small ? Small::kT : Large::kT, 0, stream>>>(logits, B, V, row_stride, segments, parts, maxima, o);
 }
 
 template <typename T>
@@ -1024,7 +1153,7 @@ int64_t sbw_token_logprobs_workspace(int64_t B, int64_t V, int64_t top) {
 }
 
 int64_t sbw_top_candidates_workspace(int64_t B, int64_t V, int64_t k) {
-  if (B <= 0 || V <= 0 || V > kMostColumns || k < 1 || k > kMostTokens) return 0;
+  if (B <= 0 || V <= 0 || V > kMostColumns || k < 1 || k > kMostTokens || one_launch(V, k)) return 0;
   return B * segments_of(B, V, k) * kMaximaElems;
 }
 
@@ -1045,9 +1174,10 @@ sbw_status_t sbw_token_logprobs(const void* logits, sbw_dtype_t dtype, int64_t B
   s = check_device();
   if (s != SBW_OK) return s;
   const auto st = static_cast<hipStream_t>(stream);
-  auto* launch = dtype == SBW_F32 ? launch_logprobs<float> : launch_logprobs<uint16_t>;
-  launch(logits, B, static_cast<uint32_t>(V), row_stride, tokens, static_cast<uint32_t>(n), inv_temperature,
-         static_cast<uint32_t>(top), logprobs, lse, entropy, stats, top_ids, top_logprobs, workspace, st);
+  const Outputs o{tokens, static_cast<uint32_t>(n), static_cast<uint32_t>(top), inv_temperature, 0u, logprobs, lse,
+                  entropy, stats, top_ids, top_logprobs};
+  auto* launch = dtype == SBW_F32 ? launch_rows<float, true> : launch_rows<uint16_t, true>;
+  launch(logits, B, static_cast<uint32_t>(V), row_stride, o, workspace, st);
   return after_launch();
 }
 
@@ -1090,9 +1220,10 @@ sbw_status_t sbw_top_candidates(const void* logits, sbw_dtype_t dtype, int64_t B
   s = check_device();
   if (s != SBW_OK) return s;
   const auto st = static_cast<hipStream_t>(stream);
-  auto* launch = dtype == SBW_F32 ? launch_candidates<float> : launch_candidates<uint16_t>;
-  launch(logits, B, static_cast<uint32_t>(V), row_stride, static_cast<uint32_t>(v_offset), static_cast<uint32_t>(k),
-         ids, values, workspace, st);
+  const Outputs o{nullptr, 0u, static_cast<uint32_t>(k), 1.0f, static_cast<uint32_t>(v_offset), nullptr, nullptr,
+                  nullptr, nullptr, ids, values};
+  auto* launch = dtype == SBW_F32 ? launch_rows<float, false> : launch_rows<uint16_t, false>;
+  launch(logits, B, static_cast<uint32_t>(V), row_stride, o, workspace, st);
   return after_launch();
 }
 
