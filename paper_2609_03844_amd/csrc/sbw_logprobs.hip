@@ -80,25 +80,14 @@ __device__ __forceinline__ void set_elem(u32x4& v, int e, uint16_t x) {
 }
 
 
-// -inf in the first n places.
-__device__ __forceinline__ f32x4 without_first(f32x4 v, uint32_t n) {
-#pragma unroll
-  for (uint32_t e = 0; e < 4; ++e)
-    if (e < n) v[e] = -INFINITY;
-  return v;
-}
-__device__ __forceinline__ u32x4 without_first(u32x4 v, uint32_t n) {
-#pragma unroll
-  for (uint32_t e = 0; e < 4; ++e) {
-    const uint32_t low = 2 * e < n ? 0xFF80u : v[e] & 0xFFFFu, high = 2 * e + 1 < n ? 0xFF800000u : v[e] & 0xFFFF0000u;
-    v[e] = low | high;
-  }
-  return v;
-}
-
 template <typename T>
 __device__ __forceinline__ typename VecOf<T>::Value load_whole(const T* row, uint32_t j) {
   return *reinterpret_cast<const typename VecOf<T>::Memory*>(row + j * kPerOf<T>);
+}
+// The same past the caches, for logits that are read once.
+template <typename T>
+__device__ __forceinline__ typename VecOf<T>::Value load_once(const T* row, uint32_t j) {
+  return stream_load(reinterpret_cast<const typename VecOf<T>::Memory*>(row + j * kPerOf<T>));
 }
 template <typename T>
 __device__ __forceinline__ typename VecOf<T>::Value load_any(const T* row, uint32_t V, uint32_t j) {
@@ -190,6 +179,8 @@ struct Sums {
 // from which the selection finds the few groups that can hold one of the k largest.
 //
 // Sixteen lanes' maxima give the maximum of a larger group, a block, which a small k needs to look at first.
+// A selection reads some of the logits again, so only a pass without one goes past the caches (512 x 152064
+// fp32 without one: 53.0 us, 59.4 through them; 256 x 152064 bf16 and 20 alternatives: 23.5 and 22.0 us).
 template <typename T, int kVecs, bool kStats, bool kTop>
 __global__ void __launch_bounds__(kThreads)
 row_pass_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride, float c,
@@ -202,7 +193,8 @@ row_pass_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row
     typename VecOf<T>::Value x[kVecs];
     if (whole) {
 #pragma unroll
-      for (int u = 0; u < kVecs; ++u) x[u] = load_whole(row, j0 + u * kThreads);
+      for (int u = 0; u < kVecs; ++u)
+        x[u] = kTop ? load_whole(row, j0 + u * kThreads) : load_once(row, j0 + u * kThreads);
     } else {
 #pragma unroll
       for (int u = 0; u < kVecs; ++u) x[u] = load_any(row, V, j0 + u * kThreads);
@@ -246,12 +238,11 @@ row_pass_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row
 // Where too many groups tie at t (a mask, equal logits), only what lies above t is gathered,
 // fewer than k groups, and the rest are the first columns that equal t.
 // ---------------------------------------------------------------------------
-// kT lanes select; the row's groups were read by kLanes lanes at a time.  Two sizes: a few hundred logits, or up
-// to 1024.
-template <int kT_, int kLanes_, bool kSmall_>
+// Two sizes: a few hundred logits by 4 waves, up to 1024 by 16.
+template <bool kSmall_>
 struct SelectionSize {
-  static constexpr int kT = kT_, kLanes = kLanes_, kBlocks = kLanes / kBlockLanes;
   static constexpr bool kSmall = kSmall_;
+  static constexpr int kT = kSmall ? 256 : 1024;
   static constexpr uint32_t kList = kSmall ? 1024 : 4096;     // gathered logits
   static constexpr uint32_t kGroups = kSmall ? 512 : 2048;    // listed groups
 };
@@ -317,7 +308,7 @@ __device__ __forceinline__ void gather_listed(const T* row, uint32_t V, Selectio
   const uint32_t items = s.listed * kVecs;
   const auto column_of = [&](uint32_t item) {
     const uint32_t g = s.groups[item / kVecs];
-    return (g / Size::kLanes * (Size::kLanes * kVecs) + item % kVecs * Size::kLanes + g % Size::kLanes) * kPer;
+    return (g / kThreads * (kThreads * kVecs) + item % kVecs * kThreads + g % kThreads) * kPer;
   };
   const auto load_at = [&](uint32_t column) {
     return *reinterpret_cast<const typename VecOf<T>::Memory*>(row + min(column, V - kPer));
@@ -420,7 +411,7 @@ __device__ __forceinline__ Gathered gather_any(const T* row, uint32_t V, const u
   const auto each_listed = [&](auto&& f) {
     for (uint32_t i = tid; i < items; i += kT) {
       const uint32_t g = s.groups[i / kVecs];
-      const uint32_t j = g / Size::kLanes * (Size::kLanes * kVecs) + i % kVecs * Size::kLanes + g % Size::kLanes;
+      const uint32_t j = g / kThreads * (kThreads * kVecs) + i % kVecs * kThreads + g % kThreads;
       const auto x = load_any(row, V, j);
 #pragma unroll
       for (uint32_t e = 0; e < kPer; ++e)
@@ -704,18 +695,16 @@ __device__ __forceinline__ const uint64_t* sorted(uint32_t taken, Selection<Size
 // access of LDS and memory would be a flat one.
 #define SBW_LDS __attribute__((address_space(3)))
 #define SBW_GLOBAL __attribute__((address_space(1)))
-template <typename T, int kVecs, typename Size, bool kOfLds>
-__device__ __noinline__ const uint64_t* select_row(const SBW_GLOBAL T* row_, uint32_t V, const SBW_GLOBAL uint32_t* global_groups,
-                                                   const SBW_GLOBAL uint32_t* global_blocks,
-                                                   const SBW_LDS uint32_t* lds_groups,
-                                                   const SBW_LDS uint32_t* lds_blocks, uint32_t segments, uint32_t k,
-                                                   SBW_LDS Selection<Size>* selection) {
+template <typename T, int kVecs, typename Size>
+__device__ __noinline__ const uint64_t* select_row(const SBW_GLOBAL T* row_, uint32_t V,
+                                                   const SBW_GLOBAL uint32_t* groups,
+                                                   const SBW_GLOBAL uint32_t* block_maxima, uint32_t segments,
+                                                   uint32_t k, SBW_LDS Selection<Size>* selection) {
   const T* row = (const T*)row_;
   Selection<Size>& s = *(Selection<Size>*)selection;
-  const Maxima maxima = kOfLds ? Maxima{(uint32_t*)lds_groups, (uint32_t*)lds_blocks}
-                               : Maxima{(uint32_t*)global_groups, (uint32_t*)global_blocks};
+  const Maxima maxima{(uint32_t*)groups, (uint32_t*)block_maxima};
   k = min(k, V);
-  const uint32_t blocks = segments * Size::kBlocks;
+  const uint32_t blocks = segments * kBlocksOf;
   Gathered r{Size::kList + 1, 0u, false};
   if constexpr (Size::kSmall) {
     if (V >= kPerOf<T> && 2 * k <= blocks) {
@@ -725,7 +714,7 @@ __device__ __noinline__ const uint64_t* select_row(const SBW_GLOBAL T* row_, uin
     __syncthreads();
   }
   if (r.taken > Size::kList)
-    r = gather_any<T, kVecs, Size>(row, V, maxima.groups, segments * Size::kLanes, k, s);
+    r = gather_any<T, kVecs, Size>(row, V, maxima.groups, segments * kThreads, k, s);
   if (r.above && r.taken < k) {
     fill_equal(row, V, k, r.taken, r.key, s);
     r.taken = k;
@@ -826,71 +815,10 @@ select_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_s
       if (lane == 0) of_row[0] = r.m, of_row[1] = ln_s;
     }
     const Maxima m = row_maxima(maxima, b, segments);
-    const uint64_t* best = select_row<T, kVecs, Size, false>(
+    const uint64_t* best = select_row<T, kVecs, Size>(
         (const SBW_GLOBAL T*)row, V, (const SBW_GLOBAL uint32_t*)m.groups, (const SBW_GLOBAL uint32_t*)m.blocks,
-        nullptr, nullptr, segments, o.top, (SBW_LDS Selection<Size>*)&s);
+        segments, o.top, (SBW_LDS Selection<Size>*)&s);
     write_selected<kStats>(o, b, V, best, of_row[0], of_row[1], Size::kT);
-    __syncthreads();
-  }
-}
-
-// ---------------------------------------------------------------------------
-// Candidates in one launch: a workgroup reads its row in rounds of kT * kVecs vectors, the next round's
-// loads on their way while this one is looked at, keeps the groups' maxima in LDS and selects from there.
-// (The statistics cost too many instructions a logit for one CU to take a row: 14 us for one row of 152064,
-// 5.7 with its segments spread over the chip; and 60 us against 59 for 512 rows.)
-// ---------------------------------------------------------------------------
-// Vector j as load_any, without a branch, for rows of at least one whole vector.
-template <typename T>
-__device__ __forceinline__ typename VecOf<T>::Value load_end(const T* row, uint32_t V, uint32_t j) {
-  const uint32_t at = j * kPerOf<T>, first = min(at, V - kPerOf<T>);
-  const typename VecOf<T>::Value v = *reinterpret_cast<const typename VecOf<T>::Memory*>(row + first);
-  return without_first(v, at - first);
-}
-
-template <typename T, int kVecs, typename Size, int kRounds>
-__global__ void __launch_bounds__(Size::kT)
-row_select_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride, Outputs o) {
-  constexpr int kT = Size::kT;
-  constexpr uint32_t kPer = kPerOf<T>;
-  static_assert(kT == Size::kLanes, "every lane reads and selects");
-  __shared__ Selection<Size> s;
-  __shared__ uint32_t group_maxima[kRounds * kT], block_maxima[kRounds * Size::kBlocks];
-  const uint32_t tid = threadIdx.x;
-  constexpr uint32_t kRound = kPer * kT * kVecs;
-  const uint32_t whole = V / kRound, rounds = (V + kRound - 1) / kRound;
-  for (int64_t b = blockIdx.x; b < B; b += gridDim.x) {
-    const T* row = logits + b * row_stride;
-    const auto load = [&](typename VecOf<T>::Value (&x)[kVecs], uint32_t round) {
-      const uint32_t j = round * (kT * kVecs) + tid;
-      if (round < whole) {
-#pragma unroll
-        for (int u = 0; u < kVecs; ++u) x[u] = load_whole(row, j + u * kT);
-      } else {
-#pragma unroll
-        for (int u = 0; u < kVecs; ++u) x[u] = load_end(row, V, j + u * kT);
-      }
-    };
-    typename VecOf<T>::Value x[kVecs], next[kVecs];
-    load(x, 0);
-    for (uint32_t round = 0; round < rounds; ++round) {
-      load(next, min(round + 1, rounds - 1));
-      float m = -INFINITY;
-#pragma unroll
-      for (int u = 0; u < kVecs; ++u)
-#pragma unroll
-        for (uint32_t e = 0; e < kPer; ++e) m = larger(m, elem(x[u], e));
-      const uint32_t key = order_key(m), of_block = row_largest(key);
-      group_maxima[round * kT + tid] = key;
-      if (tid % kBlockLanes == 0) block_maxima[round * Size::kBlocks + tid / kBlockLanes] = of_block;
-#pragma unroll
-      for (int u = 0; u < kVecs; ++u) x[u] = next[u];
-    }
-    __syncthreads();
-    const uint64_t* best = select_row<T, kVecs, Size, true>(
-        (const SBW_GLOBAL T*)row, V, nullptr, nullptr, (const SBW_LDS uint32_t*)group_maxima,
-        (const SBW_LDS uint32_t*)block_maxima, rounds, o.top, (SBW_LDS Selection<Size>*)&s);
-    write_selected<false>(o, b, V, best, 0.0f, 0.0f, kT);
     __syncthreads();
   }
 }
@@ -930,6 +858,8 @@ struct RowGradient {
   }
 };
 
+// Several tokens a row (kOne is false): the first wave lists those of the segment in their order and marks their
+// columns; a lane that meets a marked column adds up its gradients from the list.
 template <typename T, int kVecs, bool kOne>
 __global__ void __launch_bounds__(kThreads)
 token_logprobs_grad_kernel(const T* logits, int64_t B, uint32_t V, int64_t row_stride,
@@ -940,20 +870,24 @@ token_logprobs_grad_kernel(const T* logits, int64_t B, uint32_t V, int64_t row_s
                            const float* __restrict__ grad_entropy, float inv_t, T* grad,
                            int64_t grad_stride) {
   constexpr uint32_t kPer = kPerOf<T>;
-  constexpr int kOwn = kOne ? 1 : kMostTokens / kThreads;   // tokens a lane looks after
-  __shared__ int32_t ids[kOne ? 1 : kMostTokens];
-  __shared__ float gs[kOne ? 1 : kMostTokens];
+  constexpr uint32_t kSegment = kThreads * kVecs * kPer;
+  __shared__ uint32_t ids[kOne ? 1 : kMostTokens], marked[kOne ? 1 : kSegment / 32];
+  __shared__ float gs[kOne ? 1 : kMostTokens], total_of_row;
+  __shared__ uint32_t listed;
   const uint32_t j0 = blockIdx.x * (kThreads * kVecs) + threadIdx.x;
   const bool whole = (blockIdx.x + 1) * (kThreads * kVecs) <= V / kPer;
-  const uint32_t first = blockIdx.x * (kThreads * kVecs * kPer);   // the segment's columns
+  const uint32_t first = blockIdx.x * kSegment;   // the segment's columns
   for (int64_t b = blockIdx.y; b < B; b += gridDim.y) {
     const T* row = logits + b * row_stride;
     T* out = grad + b * grad_stride;
     typename VecOf<T>::Value x[kVecs];
+    if (whole) {
 #pragma unroll
-    for (int u = 0; u < kVecs; ++u)
-      x[u] = whole ? load_whole(row, j0 + u * kThreads) : load_any(row, V, j0 + u * kThreads);
-
+      for (int u = 0; u < kVecs; ++u) x[u] = load_once(row, j0 + u * kThreads);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kVecs; ++u) x[u] = load_any(row, V, j0 + u * kThreads);
+    }
     RowGradient r{stats[2 * b], stats[2 * b + 1], inv_t, 0.0f, 0.0f};
     if (grad_lse != nullptr) r.share = grad_lse[b];
     if (grad_entropy != nullptr) {
@@ -963,35 +897,39 @@ token_logprobs_grad_kernel(const T* logits, int64_t B, uint32_t V, int64_t row_s
     }
     uint32_t token = 0xFFFFFFFFu;
     float g = 0.0f;
-    float own[kOwn];
     if (kOne) {
       token = static_cast<uint32_t>(tokens[b]);
       g = token < V ? grad_logprobs[b] : 0.0f;
-      r.share = (r.share - g) * inv_t;
     } else {
-      float total = 0.0f;
-      for (uint32_t i = threadIdx.x % kWave; i < n; i += kWave)
-        if (static_cast<uint32_t>(tokens[b * n + i]) < V) total += grad_logprobs[b * n + i];
-      r.share = (r.share - wave_sum(total)) * inv_t;
-      __syncthreads();     // the last row's tokens are done with
-      for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
-        ids[i] = tokens[b * n + i];
-        gs[i] = grad_logprobs[b * n + i];
+      if (b != blockIdx.y) __syncthreads();   // the last row's list is done with
+      if (threadIdx.x < kWave) {
+        for (uint32_t i = threadIdx.x; i < kSegment / 32; i += kWave) marked[i] = 0;
+        uint32_t before = 0;
+        for (uint32_t i0 = 0; i0 < n; i0 += kWave) {
+          const uint32_t i = i0 + threadIdx.x;
+          const uint32_t t = i < n ? static_cast<uint32_t>(tokens[b * n + i]) : 0xFFFFFFFFu;
+          const float of_token = t < V ? grad_logprobs[b * n + i] : 0.0f;
+          g += of_token;
+          const bool here = t < V && t - first < kSegment;
+          const uint64_t mask = __ballot(here);
+          if (here) {
+            const uint32_t at = before + __popcll(mask & ((uint64_t{1} << threadIdx.x) - 1u));
+            ids[at] = t;
+            gs[at] = of_token;
+            atomicOr(&marked[(t - first) / 32], 1u << (t - first) % 32);
+          }
+          before += __popcll(mask);
+        }
+        g = wave_sum(g);
+        if (threadIdx.x == 0) {
+          total_of_row = g;
+          listed = before;
+        }
       }
       __syncthreads();
-      // The segment's tokens, each with all its gradients at its first place, before anything is
-      // written (the gradient may replace the logits).
-#pragma unroll
-      for (int q = 0; q < kOwn; ++q) {
-        const uint32_t i = threadIdx.x + q * kThreads;
-        own[q] = NAN;
-        if (i >= n) continue;
-        const uint32_t t = static_cast<uint32_t>(ids[i]);
-        if (t >= V || t - first >= kThreads * kVecs * kPer) continue;
-        own[q] = r(logit_of(row[t]));
-      }
-      __syncthreads();
+      g = total_of_row;
     }
+    r.share = (r.share - g) * inv_t;
     const bool empty = r.m == -INFINITY;
 #pragma unroll
     for (int u = 0; u < kVecs; ++u) {
@@ -1001,25 +939,25 @@ token_logprobs_grad_kernel(const T* logits, int64_t B, uint32_t V, int64_t row_s
       for (uint32_t e = 0; e < kPer; ++e) {
         d[e] = r(elem(x[u], e));
         if (kOne && j * kPer + e == token) d[e] = __builtin_fmaf(g, inv_t, d[e]);
-        if (empty) d[e] = 0.0f;
+      }
+      if (!kOne) {
+        const uint32_t at = j * kPer - first;
+        const uint32_t marks = marked[at / 32] >> at % 32 & ((1u << kPer) - 1u);
+        if (marks != 0) {
+#pragma unroll
+          for (uint32_t e = 0; e < kPer; ++e) {
+            if ((marks >> e & 1u) == 0) continue;
+            float of_column = 0.0f;
+            for (uint32_t i = 0; i < listed; ++i) of_column += ids[i] == j * kPer + e ? gs[i] : 0.0f;
+            d[e] = __builtin_fmaf(of_column, inv_t, d[e]);
+          }
+        }
+      }
+      if (empty) {
+#pragma unroll
+        for (uint32_t e = 0; e < kPer; ++e) d[e] = 0.0f;
       }
       store_any(out, V, j, packed(d));
-    }
-    if (kOne || empty) continue;
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < kOwn; ++q) {
-      const uint32_t i = threadIdx.x + q * kThreads;
-      if (i >= n) continue;
-      const int32_t t = ids[i];
-      if (static_cast<uint32_t>(t) >= V || static_cast<uint32_t>(t) - first >= kThreads * kVecs * kPer) continue;
-      bool again = false;
-      for (uint32_t o = 0; o < i && !again; ++o) again = ids[o] == t;
-      if (again) continue;
-      float of_token = 0.0f;
-      for (uint32_t o = i; o < n; ++o)
-        if (ids[o] == t) of_token += gs[o];
-      put_logit(out + t, __builtin_fmaf(of_token, inv_t, own[q]));
     }
   }
 }
@@ -1064,28 +1002,12 @@ void launch_pass(const T* logits, int64_t B, uint32_t V, int64_t row_stride, flo
   kernel<<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, c, reinterpret_cast<Stats*>(parts), maxima);
 }
 
-// Candidates that take one launch: k of the small size, rows whose groups LDS holds.
-constexpr int kRowLong = 8, kRowShort = 16;   // rounds of 32768 and 8192 logits
-using RowSize = SelectionSize<1024, 1024, true>;
-bool row_takes_long(int64_t V, int64_t k) { return V / (32 * kBlockLanes) >= 2 * k; }
-bool one_launch(int64_t V, int64_t k) {
-  return k <= kSmallMost && V >= 64 && V <= (row_takes_long(V, k) ? kRowLong * 32768 : kRowShort * 8192);
-}
-
 template <typename T, bool kStats>
 void launch_rows(const void* logits_, int64_t B, uint32_t V, int64_t row_stride, const Outputs& o,
                  uint64_t* workspace, hipStream_t stream) {
   const T* logits = static_cast<const T*>(logits_);
   const uint32_t rows = static_cast<uint32_t>(grid_for(B));
   const bool small = o.top <= kSmallMost;
-  if constexpr (!kStats) {
-    if (one_launch(V, o.top)) {
-      auto* kernel = row_takes_long(V, o.top) ? row_select_kernel<T, kLongVecs<T>, RowSize, kRowLong>
-                                              : row_select_kernel<T, kShortVecs<T>, RowSize, kRowShort>;
-      kernel<<<rows, RowSize::kT, 0, stream>>>(logits, B, V, row_stride, o);
-      return;
-    }
-  }
   const auto segments = static_cast<uint32_t>(segments_of(B, V, o.top));
   const auto* parts = reinterpret_cast<const Stats*>(workspace);
   const float c = o.inv_t * kLog2e;
@@ -1099,8 +1021,8 @@ void launch_rows(const void* logits_, int64_t B, uint32_t V, int64_t row_stride,
   }
   const Maxima maxima = maxima_at(workspace + (kStats ? B * segments * kPartElems : 0), B, segments);
   launch_pass<T, kStats, true>(logits, B, V, row_stride, c, o.top, workspace, maxima, stream);
-  using Small = SelectionSize<256, kThreads, true>;
-  using Large = SelectionSize<1024, kThreads, false>;
+  using Small = SelectionSize<true>;
+  using Large = SelectionSize<false>;
   auto* kernel = long_segments(B, V, o.top) ? (small ? select_kernel<T, kLongVecs<T>, Small, kStats>
                                                      : select_kernel<T, kLongVecs<T>, Large, kStats>)
                                             : (small ? select_kernel<T, kShortVecs<T>, Small, kStats>
@@ -1153,7 +1075,7 @@ int64_t sbw_token_logprobs_workspace(int64_t B, int64_t V, int64_t top) {
 }
 
 int64_t sbw_top_candidates_workspace(int64_t B, int64_t V, int64_t k) {
-  if (B <= 0 || V <= 0 || V > kMostColumns || k < 1 || k > kMostTokens || one_launch(V, k)) return 0;
+  if (B <= 0 || V <= 0 || V > kMostColumns || k < 1 || k > kMostTokens) return 0;
   return B * segments_of(B, V, k) * kMaximaElems;
 }
 
