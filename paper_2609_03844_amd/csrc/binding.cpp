@@ -12,6 +12,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/TensorImpl.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -336,6 +337,23 @@ PyObject* tuple_of(PyObject* (&objects)[count]) {
   return t;
 }
 
+// Outputs of four-byte elements side by side in one allocation (an allocation costs the host about a
+// microsecond, a tensor on a part of one a tenth).
+struct Block {
+  Tensor whole;
+  int64_t used = 0;
+  Block(int64_t elements, const Call& c)
+      : whole(at::empty({elements}, c.matrix->options().dtype(at::kFloat).requires_grad(false))) {}
+  Tensor take(at::ScalarType type, at::IntArrayRef sizes) {
+    auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(whole.storage()), whole.key_set(),
+                                                     at::scalarTypeToTypeMeta(type));
+    impl->set_sizes_contiguous(sizes);
+    impl->set_storage_offset(used);
+    used += impl->numel();
+    return Tensor(std::move(impl));
+  }
+};
+
 // logits and, unless None, tokens [rows] or [rows, n]
 bool tokens_call(PyObject* logits, PyObject* tokens, Call* c, const Tensor** ids, int64_t* n) {
   if (!matrix_of(logits, c) || (c->rows > 1 && c->row_stride < c->columns)) return false;
@@ -369,19 +387,18 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t count) {
     int64_t n, top;
     double inv_t;
     if (count != 4 || !tokens_call(a[0], a[1], &c, &ids, &n) || !number(a[2], &inv_t) || !integer(a[3], &top) ||
-        top < 0)
+        top < 0 || top > SBW_STEP_MAX_TOKENS || n > SBW_STEP_MAX_TOKENS)
       Py_RETURN_NONE;
-    const auto floats = c.matrix->options().dtype(at::kFloat).requires_grad(false);
-    const auto ints = floats.dtype(at::kInt);
     const int64_t need = sbw_token_logprobs_workspace(c.rows, c.columns, top);
-    Tensor workspace = at::empty({need}, floats.dtype(at::kLong));
+    Tensor workspace = at::empty({need}, c.matrix->options().dtype(at::kLong).requires_grad(false));
+    Block block(c.rows * (4 + n + 2 * top), c);
+    Tensor stats = block.take(at::kFloat, {c.rows, 2});
+    Tensor lse = block.take(at::kFloat, {c.rows}), entropy = block.take(at::kFloat, {c.rows});
     Tensor logprobs, top_ids, top_logprobs;
-    if (ids != nullptr) logprobs = at::empty(ids->sizes(), floats);
-    Tensor lse = at::empty({c.rows}, floats), entropy = at::empty({c.rows}, floats);
-    Tensor stats = at::empty({c.rows, 2}, floats);
+    if (ids != nullptr) logprobs = block.take(at::kFloat, ids->sizes());
     if (top > 0) {
-      top_ids = at::empty({c.rows, top}, ints);
-      top_logprobs = at::empty({c.rows, top}, floats);
+      top_ids = block.take(at::kInt, {c.rows, top});
+      top_logprobs = block.take(at::kFloat, {c.rows, top});
     }
     const void* logits = c.matrix->data_ptr();
     const auto* token = ids != nullptr ? static_cast<const int32_t*>(ids->data_ptr()) : nullptr;
@@ -441,12 +458,12 @@ PyObject* top_candidates(PyObject*, PyObject* const* a, Py_ssize_t count) {
     const Tensor* none;
     int64_t n, k, v_offset;
     if (count != 3 || !tokens_call(a[0], Py_None, &c, &none, &n) || !integer(a[1], &k) || k < 1 ||
-        !integer(a[2], &v_offset))
+        !integer(a[2], &v_offset) || k > SBW_STEP_MAX_TOKENS)
       Py_RETURN_NONE;
     const int64_t need = sbw_top_candidates_workspace(c.rows, c.columns, k);
-    const auto floats = c.matrix->options().dtype(at::kFloat).requires_grad(false);
-    Tensor workspace = at::empty({need}, floats.dtype(at::kLong));
-    Tensor ids = at::empty({c.rows, k}, floats.dtype(at::kInt)), values = at::empty({c.rows, k}, floats);
+    Tensor workspace = at::empty({need}, c.matrix->options().dtype(at::kLong).requires_grad(false));
+    Block block(2 * c.rows * k, c);
+    Tensor ids = block.take(at::kInt, {c.rows, k}), values = block.take(at::kFloat, {c.rows, k});
     const void* logits = c.matrix->data_ptr();
     auto* id = static_cast<int32_t*>(ids.data_ptr());
     auto* value = static_cast<float*>(values.data_ptr());
