@@ -338,12 +338,21 @@ PyObject* tuple_of(PyObject* (&objects)[count]) {
 }
 
 // Outputs of four-byte elements side by side in one allocation (an allocation costs the host about a
-// microsecond, a tensor on a part of one a tenth).
+// microsecond, a tensor on a part of one a tenth), behind a workspace that is small; a larger one has an
+// allocation of its own, so that no output keeps it alive.
+constexpr int64_t kSmallWorkspace = 8192;   // 64 KiB
 struct Block {
-  Tensor whole;
+  Tensor whole, own_workspace;
   int64_t used = 0;
-  Block(int64_t elements, const Call& c)
-      : whole(at::empty({elements}, c.matrix->options().dtype(at::kFloat).requires_grad(false))) {}
+  Block(int64_t workspace, int64_t elements, const Call& c) {
+    const auto options = c.matrix->options().requires_grad(false);
+    if (workspace <= kSmallWorkspace) used = 2 * workspace;
+    else own_workspace = at::empty({workspace}, options.dtype(at::kLong));
+    whole = at::empty({used + elements}, options.dtype(at::kFloat));
+  }
+  uint64_t* workspace() const {
+    return static_cast<uint64_t*>((own_workspace.defined() ? own_workspace : whole).data_ptr());
+  }
   Tensor take(at::ScalarType type, at::IntArrayRef sizes) {
     auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(whole.storage()), whole.key_set(),
                                                      at::scalarTypeToTypeMeta(type));
@@ -389,9 +398,7 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t count) {
     if (count != 4 || !tokens_call(a[0], a[1], &c, &ids, &n) || !number(a[2], &inv_t) || !integer(a[3], &top) ||
         top < 0 || top > SBW_STEP_MAX_TOKENS || n > SBW_STEP_MAX_TOKENS)
       Py_RETURN_NONE;
-    const int64_t need = sbw_token_logprobs_workspace(c.rows, c.columns, top);
-    Tensor workspace = at::empty({need}, c.matrix->options().dtype(at::kLong).requires_grad(false));
-    Block block(c.rows * (4 + n + 2 * top), c);
+    Block block(sbw_token_logprobs_workspace(c.rows, c.columns, top), c.rows * (4 + n + 2 * top), c);
     Tensor stats = block.take(at::kFloat, {c.rows, 2});
     Tensor lse = block.take(at::kFloat, {c.rows}), entropy = block.take(at::kFloat, {c.rows});
     Tensor logprobs, top_ids, top_logprobs;
@@ -406,7 +413,7 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t count) {
     float *lp = address(logprobs), *l = address(lse), *h = address(entropy), *st = address(stats);
     float* tl = address(top_logprobs);
     auto* ti = top > 0 ? static_cast<int32_t*>(top_ids.data_ptr()) : nullptr;
-    auto* scratch = static_cast<uint64_t*>(workspace.data_ptr());
+    uint64_t* scratch = block.workspace();
     void* stream = stream_of(c);
     PyObject* objects[6] = {};
     const Tensor* outputs[6] = {&logprobs, &lse, &entropy, &stats, &top_ids, &top_logprobs};
@@ -460,14 +467,12 @@ PyObject* top_candidates(PyObject*, PyObject* const* a, Py_ssize_t count) {
     if (count != 3 || !tokens_call(a[0], Py_None, &c, &none, &n) || !integer(a[1], &k) || k < 1 ||
         !integer(a[2], &v_offset) || k > SBW_STEP_MAX_TOKENS)
       Py_RETURN_NONE;
-    const int64_t need = sbw_top_candidates_workspace(c.rows, c.columns, k);
-    Tensor workspace = at::empty({need}, c.matrix->options().dtype(at::kLong).requires_grad(false));
-    Block block(2 * c.rows * k, c);
+    Block block(sbw_top_candidates_workspace(c.rows, c.columns, k), 2 * c.rows * k, c);
     Tensor ids = block.take(at::kInt, {c.rows, k}), values = block.take(at::kFloat, {c.rows, k});
     const void* logits = c.matrix->data_ptr();
     auto* id = static_cast<int32_t*>(ids.data_ptr());
     auto* value = static_cast<float*>(values.data_ptr());
-    auto* scratch = static_cast<uint64_t*>(workspace.data_ptr());
+    uint64_t* scratch = block.workspace();
     void* stream = stream_of(c);
     PyObject* result = tuple_of(THPVariable_Wrap(ids), THPVariable_Wrap(values), nullptr);
     if (result == nullptr) return nullptr;
