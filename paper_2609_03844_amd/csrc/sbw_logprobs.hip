@@ -398,7 +398,9 @@ __device__ __forceinline__ Gathered gather_any(const T* row, uint32_t V, const u
   bool above = from > kGroupsMost;
   const auto wanted = [&](uint32_t key) { return above ? key > at.lo : key >= at.lo; };
   const auto list_group = [&](uint32_t g, uint32_t key) {
-    if (wanted(key)) s.groups[count_one(s.listed)] = g;
+    if (!wanted(key)) return;
+    const uint32_t n = count_one(s.listed);
+    if (n < kGroupsMost) s.groups[n] = g;
   };
 #pragma unroll
   for (int i = 0; i < kHeld; ++i)

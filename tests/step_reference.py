@@ -69,7 +69,8 @@ def logprobs(x, tokens, inv_t, top=0):
         t_lse[b] = of_sum + 4 * U * (abs(lse[b]) + abs(m * inv_t))
         second = (e[kept] * y[kept] ** 2).sum() / S
         t_H[b] = 2 * of_sum + U * (2 * adds(V) * abs(mean) + 8 * second + 8 * abs(H[b]))
-    lp, lse, tl = (np.where(np.abs(v) > np.finfo(np.float32).max, np.sign(v) * np.inf, v) for v in (lp, lse, tl))
+    limit = np.float64(np.finfo(np.float32).max)
+    lp, lse, tl = (np.where(v > limit, np.inf, np.where(v < -limit, -np.inf, v)) for v in (lp, lse, tl))
     return (lp, lse, H, ids, tl), (t_lp, t_lse, t_H, None, t_tl)
 
 

@@ -88,8 +88,9 @@ def close(got, want, tol, what):
     assert np.array_equal(got[inf], want[inf]), what
     fine = np.isfinite(want)
     assert np.isfinite(got[fine]).all(), what
-    bad = np.abs(got - want)[fine] > np.broadcast_to(tol, want.shape)[fine]
-    assert not bad.any(), (what, np.abs(got - want)[fine][bad][:5], np.broadcast_to(tol, want.shape)[fine][bad][:5])
+    off, most = np.abs(got[fine] - want[fine]), np.broadcast_to(tol, want.shape)[fine]
+    bad = off > most
+    assert not bad.any(), (what, off[bad][:5], most[bad][:5])
 
 
 def check_forward(sbw, x, tokens, inv_t, top, dtype, pad=0, offset=0, what=""):
@@ -528,3 +529,82 @@ def test_empty_batches(sbw):
     assert sbw.head_logits(torch.zeros((0, 128), dtype=torch.bfloat16, device="cuda"), codes, s).shape == (0, 7)
     assert sbw.head_logits(torch.zeros((2, 128), dtype=torch.bfloat16, device="cuda"), codes[:0], s[:0]).shape == (2, 0)
     torch.cuda.synchronize()
+
+
+def test_more_rows_than_the_grid(sbw):
+    """70001 rows: more than a grid's second dimension holds."""
+    rng = np.random.default_rng(15)
+    B, V = 70001, 37
+    x = logits(rng, B, V)
+    t = torch.from_numpy(x).cuda()
+    tokens = rng.integers(0, V, (B, 2)).astype(np.int32)
+    ids = torch.from_numpy(tokens).cuda()
+    r = sbw.token_logprobs(t, ids, top=3)
+    plain = sbw.token_logprobs(t, ids)
+    assert torch.equal(r.logprobs, plain.logprobs) and torch.equal(r.entropy, plain.entropy)
+    g = torch.full((B, 2), 0.5, device="cuda")
+    d = sbw.token_logprobs_grad(t, ids, r.stats, None, g)
+    one = sbw.token_logprobs_grad(t, ids[:, 0].contiguous(), r.stats, None, g[:, 0].contiguous())
+    top = sbw.top_candidates(t, 3)[0]
+    assert torch.equal(top, r.top_ids)
+    some = np.r_[0:40, 65500:65580, B - 40:B]
+    want, tol = ref.logprobs(x[some], tokens[some], 1.0, 3)
+    close(r.logprobs[some], want[0], tol[0], "logprobs")
+    assert np.array_equal(r.top_ids[some].cpu().numpy(), want[3])
+    zero = np.zeros(len(some))
+    half = np.full((len(some), 2), 0.5, np.float32)
+    stats, H = r.stats[some].cpu().numpy(), r.entropy[some].cpu().numpy()
+    want, tol = ref.gradient(x[some], tokens[some], 1.0, stats, H, half, zero, zero)
+    close(d[some], want, tol, "gradient")
+    want, tol = ref.gradient(x[some], tokens[some, :1], 1.0, stats, H, half[:, :1], zero, zero)
+    close(one[some], want, tol, "gradient of one token")
+
+
+def test_both_call_paths(sbw):
+    """An explicit stream takes the calls marshalled in Python: the same bits, and the same refusals."""
+    rng = np.random.default_rng(16)
+    x = torch.from_numpy(logits(rng, 7, 5003)).cuda()
+    ids = torch.from_numpy(given(rng, 7, 5003, 3)).cuda()
+    stream = torch.cuda.current_stream()
+    for top in (0, 6, 300):
+        a, b = sbw.token_logprobs(x, ids, 0.7, top=top), sbw.token_logprobs(x, ids, 0.7, top=top, stream=stream)
+        for u, v in zip(a, b):
+            assert (u is None and v is None) or (u.shape == v.shape and u.dtype == v.dtype and torch.equal(u, v))
+    for k in (1, 300):
+        for u, v in zip(sbw.top_candidates(x, k, 5), sbw.top_candidates(x, k, 5, stream=stream)):
+            assert torch.equal(u, v)
+    g, gl, gh = (torch.from_numpy(u).cuda() for u in upstream(rng, 7, 3, "plh"))
+    assert torch.equal(sbw.token_logprobs_grad(x, ids, a.stats, a.entropy, g, gl, gh, 0.7),
+                       sbw.token_logprobs_grad(x, ids, a.stats, a.entropy, g, gl, gh, 0.7, stream=stream))
+    codes, s, _ = packed(rng, 77, 256, 64, "bf16")
+    h = torch.from_numpy(rng.standard_normal((3, 256)).astype(np.float32)).to(torch.bfloat16).cuda()
+    codes = torch.from_numpy(codes).cuda()
+    for dtype in (torch.float32, torch.bfloat16):
+        assert torch.equal(sbw.head_logits(h, codes, s, dtype), sbw.head_logits(h, codes, s, dtype, stream=stream))
+
+
+def test_outputs_are_apart(sbw):
+    """The outputs share an allocation: writing one leaves the others alone, and each is a whole tensor."""
+    rng = np.random.default_rng(17)
+    x = torch.from_numpy(logits(rng, 3, 901)).cuda()
+    ids = torch.from_numpy(given(rng, 3, 901, 2)).cuda()
+    want = sbw.token_logprobs(x, ids, top=4)
+    for i in range(6):
+        got = sbw.token_logprobs(x, ids, top=4)
+        got[i].zero_()
+        for j in range(6):
+            assert got[j].is_contiguous()
+            if j != i:
+                assert torch.equal(got[j], want[j])
+
+
+def test_example(capsys):
+    import importlib.util
+    import pathlib
+    path = pathlib.Path(__file__).resolve().parents[1] / "examples" / "decode_step.py"
+    spec = importlib.util.spec_from_file_location("decode_step", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    example.main(6, 5003, 256)
+    out = capsys.readouterr().out
+    assert "green" in out and "gradient norm" in out
