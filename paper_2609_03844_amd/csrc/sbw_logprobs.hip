@@ -258,16 +258,21 @@ struct Selection {
   uint32_t taken, listed, blocks, key, from;
 };
 
-// The sum over the workgroup of one number a wave; `turn` alternates.
+// The sum over the workgroup of one number a wave, the same in every lane; `turn` alternates.
 template <typename Size>
 __device__ __forceinline__ uint32_t group_sum(uint32_t of_wave, Selection<Size>& s, uint32_t turn) {
-  constexpr int kT = Size::kT;
+  constexpr uint32_t kWaves = Size::kT / kWave;
+  static_assert(kWaves == 4 || kWaves == 16, "the sums of a quad, or of a row of lanes");
   if (threadIdx.x % kWave == 0) s.slots[turn & 1][threadIdx.x / kWave] = of_wave;
   __syncthreads();
-  uint32_t n = 0;
-#pragma unroll
-  for (int w = 0; w < kT / kWave; ++w) n += s.slots[turn & 1][w];
-  return n;
+  int n = static_cast<int>(s.slots[turn & 1][threadIdx.x % kWaves]);
+  n += __builtin_amdgcn_update_dpp(0, n, 0xB1, 0xF, 0xF, false);    // quad_perm [1,0,3,2]
+  n += __builtin_amdgcn_update_dpp(0, n, 0x4E, 0xF, 0xF, false);    // quad_perm [2,3,0,1]
+  if (kWaves == 16) {
+    n += __builtin_amdgcn_update_dpp(0, n, 0x141, 0xF, 0xF, false);   // row_half_mirror
+    n += __builtin_amdgcn_update_dpp(0, n, 0x140, 0xF, 0xF, false);   // row_mirror
+  }
+  return static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(n));
 }
 
 // Bisection between two keys: lo has at least k at or above it, hi fewer.  The first steps go down from the
@@ -340,12 +345,12 @@ struct Gathered {
   bool above;
 };
 
-// Whatever the row holds.
-template <typename T, int kVecs, typename Size>
+// Whatever the row holds.  A lane holds kHeld groups' keys, and reads any others each time.
+template <typename T, int kVecs, int kHeld, typename Size>
 __device__ __forceinline__ Gathered gather_any(const T* row, uint32_t V, const uint32_t* maxima,
                                             uint32_t groups, uint32_t k, Selection<Size>& s) {
   constexpr uint32_t kPer = kPerOf<T>;
-  constexpr int kT = Size::kT, kHeld = 8;
+  constexpr int kT = Size::kT;
   constexpr uint32_t kListMost = Size::kList, kGroupsMost = Size::kGroups;
   const uint32_t tid = threadIdx.x;
   uint32_t turn = 0;
@@ -357,8 +362,7 @@ __device__ __forceinline__ Gathered gather_any(const T* row, uint32_t V, const u
     highest = max(highest, held[i]);
   }
   for (uint32_t g = tid + kHeld * kT; g < groups; g += kT) highest = max(highest, maxima[g]);
-#pragma unroll
-  for (int d = kWave / 2; d > 0; d /= 2) highest = max(highest, __shfl_xor(highest, d));
+  highest = wave_highest(highest);
   if (tid % kWave == 0) s.slots[turn & 1][tid / kWave] = highest;
   if (tid == 0) s.taken = s.listed = 0;
   __syncthreads();
@@ -715,8 +719,12 @@ __device__ __noinline__ const uint64_t* select_row(const SBW_GLOBAL T* row_, uin
     }
     __syncthreads();
   }
-  if (r.taken > Size::kList)
-    r = gather_any<T, kVecs, Size>(row, V, maxima.groups, segments * kThreads, k, s);
+  if (r.taken > Size::kList) {
+    const uint32_t count = segments * kThreads;
+    if constexpr (Size::kSmall) r = gather_any<T, kVecs, 8, Size>(row, V, maxima.groups, count, k, s);
+    else if (count <= 5 * Size::kT) r = gather_any<T, kVecs, 5, Size>(row, V, maxima.groups, count, k, s);
+    else r = gather_any<T, kVecs, 20, Size>(row, V, maxima.groups, count, k, s);
+  }
   if (r.above && r.taken < k) {
     fill_equal(row, V, k, r.taken, r.key, s);
     r.taken = k;
@@ -974,11 +982,13 @@ template <typename T>
 constexpr int kShortVecs = sizeof(T) == 4 ? 2 : 1;
 constexpr int64_t kLongSegment = kThreads * 32, kShortSegment = kThreads * 8;
 
-// Whether the pass takes the long form: rows that make enough workgroups of it, and so many blocks (for a
-// large k, groups) that the selection is left with few.
+// Whether the pass takes the long form: rows that make enough workgroups of it, and so many blocks that the
+// selection is left with few.  For a large k only with eight groups for each, as every vector of a listed group
+// is another line to fetch, or where the lanes could not hold the short form's (1024 of 16 x 151936 fp32: 20.9 us short, 23.6 long;
+// 500 of 100 x 150000 bf16, 24.7 and 22.3).
 bool long_segments(int64_t B, int64_t V, int64_t top) {
   const int64_t segments = (V + kLongSegment - 1) / kLongSegment;
-  if (top > kSmallMost) return V / 32 >= 4 * top;
+  if (top > kSmallMost) return V / 32 >= 8 * top || V / 8 > 20 * SelectionSize<false>::kT;
   return B * segments >= 512 && segments * kBlocksOf >= 2 * top;
 }
 int64_t segments_of(int64_t B, int64_t V, int64_t top) {
