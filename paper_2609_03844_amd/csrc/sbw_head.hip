@@ -79,6 +79,14 @@ __device__ __forceinline__ void exchange(u32x4& w) {
 // sum (q - 8) h: every product is exact and all sums are fp32.  A lane then holds four hidden states'
 // sums for one head row, so a group's scale is one value a lane; a tile's scales are loaded side by side
 // and handed out through LDS.  The waves' sums meet in LDS.
+//
+// Bound by HBM, less what a tile's barrier, sums and stores leave uncovered: one state through 128256 x 4096 in
+// groups of 128 49 us (5.5 TB/s), 16 states in groups of 64 59 us (5.1 TB/s; one state in
+// those groups 53; all-zero states are faster, 59 where others took 66 in the same run), groups of 32 for
+// one state 57 us, 32000 x 2048 9.5 us.  Measured and not
+// kept: two tiles in registers (52 us against 50), eight waves with four chunks each in two
+// workgroups a CU (56 against 50), non-temporal codes (53 against 49: two loads share a 128-byte line), neighbouring tiles to a
+// workgroup (52), the sums shared by all waves (50).
 template <typename S, typename T, int kGroup, int kChunks, int kTiles, int kMost>
 __global__ void __launch_bounds__(kMost * kWave, 4)
 head_logits_kernel(const uint16_t* __restrict__ hidden, int64_t B, uint32_t K, int64_t hidden_stride,

@@ -173,7 +173,10 @@ struct Sums {
   }
 };
 
-// The streaming pass: one read of every logit.  A workgroup takes a segment of kThreads * kVecs
+// The streaming pass: one read of every logit, bound by HBM (bf16 statistics: nearly as much by the ten
+// instructions a logit, four of them its exponential).  512 x 152064 fp32: 47.3 us, 6.6 TB/s; 256 x 152064 bf16, maxima
+// only: 13.7 us, 5.7 TB/s; one row of 32000: 2.6 us, a launch and a memory round trip.
+// A workgroup takes a segment of kThreads * kVecs
 // vectors of a row, a lane kVecs of them, kThreads vectors apart.  A wave writes the statistics
 // of its part; with kTop a lane also writes the key of its largest logit (its group's maximum),
 // from which the selection finds the few groups that can hold one of the k largest.
@@ -230,6 +233,8 @@ row_pass_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row
 // ---------------------------------------------------------------------------
 // The k first logits of a row in order, by one workgroup, from the maxima of its groups.
 //
+// A chain of short dependent steps: threshold, groups, logits and order take 11-14 thousand cycles (the kernel 5-7.5 us)
+// for 5 to 50 of a row, 19 for 100; 1024 of 151936 take the kernel 18 us.
 // A threshold t with at least k group maxima at or above it has at least k logits there, all in
 // those groups; bisection stops at a t that leaves not many more than k groups.  Their logits
 // from t on are gathered as (key << 32 | ~column), which no two logits share, and sorted.
@@ -793,7 +798,8 @@ __device__ __forceinline__ void write_selected(const Outputs& o, int64_t b, uint
   }
 }
 
-// After the pass.  Without a selection one wave a row joins the statistics and writes; with one a workgroup.
+// After the pass.  Without a selection one wave a row joins the statistics and writes (a launch and the two loads of
+// token and logit: 4.9 us for 512 rows); with one a workgroup.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 join_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride, uint32_t segments,
@@ -834,7 +840,8 @@ select_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_s
 }
 
 // ---------------------------------------------------------------------------
-// Gradient: one read and one write of every logit.
+// Gradient: one read and one write of every logit, bound by HBM: 256 x 152064 fp32 49 us (6.3 TB/s),
+// 1024 x 128256 bf16 82 us (6.4).
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ void put_logit(float* p, float x) { *p = x; }
 __device__ __forceinline__ void put_logit(uint16_t* p, float x) {
