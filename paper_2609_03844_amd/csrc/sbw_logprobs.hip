@@ -14,9 +14,11 @@ namespace {
 constexpr int kMostTokens = SBW_STEP_MAX_TOKENS;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.693147180559945309417f;
-// A score's floor inside the weighted sums: its exponential is 0, and 0 times it is 0 where 0
-// times -inf would be NaN (2^32 of them together still fit fp32).
-constexpr float kScoreFloor = -1e20f;
+// A score's floor inside the weighted sums: its exponential is 0, and 0 times it is 0 where 0 times -inf
+// would be NaN.  No lower than it has to be, as the gradient multiplies it by an upstream one and inv_t.
+constexpr float kScoreFloor = -1000.0f;
+// c; finite for every inv_t, as the largest logit's score is 0 times it.
+__host__ __device__ inline float score_factor(float inv_t) { return fminf(inv_t * kLog2e, 3.402823466e38f); }
 
 __device__ __forceinline__ float logit_of(float x) { return x; }
 __device__ __forceinline__ float logit_of(uint16_t x) {
@@ -809,7 +811,7 @@ join_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_str
     const uint32_t count = segments * (kThreads / kWave), lane = threadIdx.x % kWave;
     const T* row = logits + b * row_stride;
     const Given<T> given(o, b, row, V, lane);
-    const Stats r = join_parts(parts + b * count, count, o.inv_t * kLog2e);
+    const Stats r = join_parts(parts + b * count, count, score_factor(o.inv_t));
     write_statistics(o, b, row, V, r, given, lane, kWave);
   }
 }
@@ -826,7 +828,7 @@ select_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_s
     if (kStats && threadIdx.x >= kWave) {
       const uint32_t lane = threadIdx.x - kWave, count = segments * (kThreads / kWave);
       const Given<T> given(o, b, row, V, lane);
-      const Stats r = join_parts(parts + b * count, count, o.inv_t * kLog2e);
+      const Stats r = join_parts(parts + b * count, count, score_factor(o.inv_t));
       const float ln_s = write_statistics(o, b, row, V, r, given, lane, Size::kT - kWave);
       if (lane == 0) of_row[0] = r.m, of_row[1] = ln_s;
     }
@@ -1029,7 +1031,7 @@ void launch_rows(const void* logits_, int64_t B, uint32_t V, int64_t row_stride,
   const bool small = o.top <= kSmallMost;
   const auto segments = static_cast<uint32_t>(segments_of(B, V, o.top));
   const auto* parts = reinterpret_cast<const Stats*>(workspace);
-  const float c = o.inv_t * kLog2e;
+  const float c = score_factor(o.inv_t);
   if (o.top == 0) {
     if constexpr (kStats) {
       launch_pass<T, true, false>(logits, B, V, row_stride, c, 0, workspace, Maxima{}, stream);

@@ -279,6 +279,27 @@ def test_gradient_launch_shapes(sbw, dtype, B, V, n):
     close(d, want, tol, "gradient")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("inv_t", [3e38, 1e20, 1e-30])
+def test_extreme_temperatures(sbw, dtype, inv_t):
+    """Any positive finite factor: whole logits up to 0, so that the scores are 0 or far away, or all close."""
+    rng = np.random.default_rng(9)
+    B, V, n = 4, 3001, 3
+    x = -np.abs(np.round(4 * rng.standard_normal((B, V)))).astype(np.float32)
+    x[1] -= 1
+    x[1, 77] = 0                               # one alone
+    x[2] = 0                                   # all alike
+    tokens = given(rng, B, V, n)
+    t, flat, r = check_forward(sbw, x, tokens, inv_t, 5, dtype, what=f"{inv_t}")
+    if inv_t > 1e30:
+        return                                 # the gradient itself passes fp32's range
+    g, gl, gh = upstream(rng, B, n, "plh")
+    d = sbw.token_logprobs_grad(t, flat, r.stats, r.entropy, *(torch.from_numpy(u).cuda() for u in (g, gl, gh)), inv_t)
+    want, tol = ref.gradient(x, tokens, inv_t, r.stats.cpu().numpy(), r.entropy.cpu().numpy(), g, gl, gh,
+                             bf16=dtype == "bf16")
+    close(d, want, tol, "gradient")
+
+
 def test_gradient_against_differences(sbw):
     """Central differences of the 64-bit loss, at every column of small rows."""
     rng = np.random.default_rng(8)
