@@ -101,9 +101,31 @@ def _vector(t: Optional[torch.Tensor], shape, dtype, name: str) -> Optional[int]
     return t.data_ptr()
 
 
-def _scratch(workspace: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
+def _side(stream, device):
+    """The torch stream of a stream argument that is not the current one, else None."""
+    if stream is None or device.type != "cuda" or _stream(stream) == _stream(None):
+        return None
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    return torch.cuda.ExternalStream(_stream(stream)) if _stream(stream) else torch.cuda.default_stream()
+
+
+def _empty(shape, dtype, device, side, kept=True) -> torch.Tensor:
+    """Memory for work on ``side`` comes from that stream's, so that its last use there is over and the
+    next one waits; what the caller keeps is known to the current stream too."""
+    if side is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    here = torch.cuda.current_stream()
+    with torch.cuda.stream(side):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if kept:
+        t.record_stream(here)
+    return t
+
+
+def _scratch(workspace: Optional[torch.Tensor], need: int, device, side) -> torch.Tensor:
     if workspace is None:
-        return torch.empty(max(need, 1), dtype=torch.int64, device=device)
+        return _empty(max(need, 1), torch.int64, device, side, kept=False)
     if workspace.dtype != torch.int64 or not workspace.is_contiguous() or workspace.numel() < need:
         raise ValueError(f"workspace must be contiguous int64 with >= {need} elements")
     return workspace
@@ -126,16 +148,16 @@ def _forward(logits, tokens, inv_temperature, top, out, workspace, stream) -> To
     n = _tokens(tokens, B)
     top = int(top)
     dev = logits.device
+    side = _side(stream, dev)
     if out is None:
-        f32 = dict(dtype=torch.float32, device=dev)
+        f32 = functools.partial(_empty, dtype=torch.float32, device=dev, side=side)
         k = max(top, 0)
-        out = TokenLogprobs(torch.empty(tokens.shape, **f32) if tokens is not None else None,
-                            torch.empty(B, **f32), torch.empty(B, **f32), torch.empty((B, 2), **f32),
-                            torch.empty((B, k), dtype=torch.int32, device=dev) if top else None,
-                            torch.empty((B, k), **f32) if top else None)
+        out = TokenLogprobs(f32(tokens.shape) if tokens is not None else None, f32(B), f32(B), f32((B, 2)),
+                            _empty((B, k), torch.int32, dev, side) if top else None,
+                            f32((B, k)) if top else None)
     if (tokens is not None) != (out.logprobs is not None) or (top > 0 and out.top_ids is None):
         raise ValueError("out must hold what the call writes")
-    workspace = _scratch(workspace, token_logprobs_workspace_size(B, V, top), dev)
+    workspace = _scratch(workspace, token_logprobs_workspace_size(B, V, top), dev, side)
     pointers = [_vector(out.logprobs, tokens.shape if tokens is not None else (), torch.float32, "logprobs"),
                 _vector(out.lse, (B,), torch.float32, "lse"),
                 _vector(out.entropy, (B,), torch.float32, "entropy"),
@@ -156,7 +178,7 @@ class _Differentiable(torch.autograd.Function):
         out = _call(logits.detach(), tokens, inv_temperature, top, None, workspace, stream)
         ctx.set_materialize_grads(False)
         ctx.save_for_backward(logits, tokens, out.stats, out.entropy)
-        ctx.inv_temperature, ctx.stream = inv_temperature, stream
+        ctx.inv_temperature = inv_temperature
         ctx.mark_non_differentiable(*(t for t in out[3:] if t is not None))   # stats and alternatives
         return tuple(out)
 
@@ -167,8 +189,9 @@ class _Differentiable(torch.autograd.Function):
         if g_logprobs is None and g_lse is None and g_entropy is None:
             return (None,) * 6
         g = [t.contiguous() if t is not None else None for t in (g_logprobs, g_lse, g_entropy)]
-        grad = token_logprobs_grad(logits.detach(), tokens, stats, entropy, *g, ctx.inv_temperature,
-                                   stream=ctx.stream)
+        # on autograd's stream, whatever the forward call's: it has waited for these gradients, and they came
+        # after the outputs that they are the gradients of
+        grad = token_logprobs_grad(logits.detach(), tokens, stats, entropy, *g, ctx.inv_temperature)
         return grad, None, None, None, None, None
 
 
@@ -229,7 +252,7 @@ def token_logprobs_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor], st
     dtype, B, V, row_stride = _matrix(logits, "logits")
     n = _tokens(tokens, B)
     if out is None:
-        out = torch.empty((B, V), dtype=logits.dtype, device=logits.device)
+        out = _empty((B, V), logits.dtype, logits.device, _side(stream, logits.device))
     out_dtype, *out_shape, out_stride = _matrix(out, "out")
     if out_dtype != dtype or out_shape != [B, V]:
         raise ValueError("out must be like logits")
@@ -270,11 +293,12 @@ def top_candidates(logits: torch.Tensor, k: int, v_offset: int = 0,
     dtype, B, V, row_stride = _matrix(logits, "logits")
     k = int(k)
     dev = logits.device
+    side = _side(stream, dev)
     if ids is None:
-        ids = torch.empty((B, max(k, 0)), dtype=torch.int32, device=dev)
+        ids = _empty((B, max(k, 0)), torch.int32, dev, side)
     if values is None and with_values:
-        values = torch.empty((B, max(k, 0)), dtype=torch.float32, device=dev)
-    workspace = _scratch(workspace, top_candidates_workspace_size(B, V, k), dev)
+        values = _empty((B, max(k, 0)), torch.float32, dev, side)
+    workspace = _scratch(workspace, top_candidates_workspace_size(B, V, k), dev, side)
     if k > 0:
         _vector(ids, (B, k), torch.int32, "ids")
         _vector(values, (B, k), torch.float32, "values")
@@ -315,7 +339,7 @@ def head_logits(hidden: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
     if groups == 0 or K % groups != 0:
         raise ValueError("K must be a multiple of the groups")
     if out is None:
-        out = torch.empty((B, V), dtype=dtype, device=hidden.device)
+        out = _empty((B, V), dtype, hidden.device, _side(stream, hidden.device))
     out_dtype, *out_shape, row_stride = _matrix(out, "out")
     if out_shape != [B, V] or out.dtype != dtype:
         raise ValueError("out must be [B, V] of dtype")

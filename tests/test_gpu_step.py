@@ -490,6 +490,64 @@ def test_streams_graphs_and_repeats(sbw):
         assert all(torch.equal(a, b) for a, b in zip(first, held)), replay
 
 
+@pytest.mark.parametrize("raw", [False, True])
+def test_memory_of_another_stream(sbw, raw):
+    """Calls on a busy stream that is not the current one, while the current one allocates and writes: a call's
+    workspace and outputs are not memory that the current stream still uses or is given meanwhile."""
+    rng = np.random.default_rng(12)
+    x = torch.from_numpy(logits(rng, 64, 20011)).cuda()
+    ids = torch.from_numpy(given(rng, 64, 20011, 3)).cuda()
+    h = torch.randn(4, 256, device="cuda").bfloat16()
+    codes = torch.randint(0, 256, (20011, 128), dtype=torch.uint8, device="cuda")
+    scales = torch.rand(20011, 4, device="cuda")
+    g = torch.ones(64, 3, device="cuda")
+
+    def calls(stream=None):
+        r = sbw.token_logprobs(x, ids, top=20, stream=stream)
+        return (*r, *sbw.top_candidates(x, 300, stream=stream), sbw.head_logits(h, codes, scales, stream=stream),
+                sbw.token_logprobs_grad(x, ids, r.stats, r.entropy, g, stream=stream))
+    want = calls()
+    busy = torch.randn(4096, 4096, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            for _ in range(10):
+                busy = busy @ busy * 1e-3
+        got = calls(side.cuda_stream if raw else side)
+        for t in want:                         # the sizes that a call allocates, and its workspaces'
+            torch.empty_like(t).fill_(1)
+        for need in (sbw.token_logprobs_workspace_size(64, 20011, 20), sbw.top_candidates_workspace_size(64, 20011, 300)):
+            torch.empty(need, dtype=torch.int64, device="cuda").fill_(-1)
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+
+
+def test_backward_of_a_call_on_another_stream(sbw):
+    """The gradient is computed where autograd's stream is, after the upstream one that is still on its way."""
+    rng = np.random.default_rng(13)
+    x = torch.from_numpy(logits(rng, 16, 4097)).cuda()
+    ids = torch.from_numpy(given(rng, 16, 4097, 1)[:, 0].copy()).cuda()
+    side = torch.cuda.Stream()
+    busy = torch.randn(4096, 4096, device="cuda")
+
+    def gradient(stream):
+        z = x.clone().requires_grad_()
+        torch.cuda.synchronize()
+        r = sbw.token_logprobs(z, ids, stream=stream)
+        torch.cuda.current_stream().wait_stream(side)
+        up = busy
+        for _ in range(10):
+            up = up @ busy * 1e-3
+        (r.logprobs * (1 + 0 * up.nan_to_num(0, 0, 0)[:16, 0])).sum().backward()
+        d = z.grad * 1
+        torch.cuda.synchronize()
+        return d
+    want = gradient(None)
+    assert torch.equal(gradient(side), want)
+
+
 def test_candidates_feed_the_watermark(sbw):
     """The top-k scheme from logits alone equals the oracle's on the same candidates."""
     rng = np.random.default_rng(14)
