@@ -85,8 +85,8 @@ __device__ __forceinline__ void exchange(u32x4& w) {
 // those groups 53; all-zero states are faster, 59 where others took 66 in the same run), groups of 32 for
 // one state 57 us, 32000 x 2048 9.5 us.  Measured and not
 // kept: two tiles in registers (52 us against 50), eight waves with four chunks each in two
-// workgroups a CU (56 against 50), non-temporal codes (53 against 49: two loads share a 128-byte line), neighbouring tiles to a
-// workgroup (52), the sums shared by all waves (50).
+// workgroups a CU (56 against 50), non-temporal codes (53 against 49: two loads share a
+// 128-byte line), neighbouring tiles to a workgroup (52), the sums shared by all waves (50).
 template <typename S, typename T, int kGroup, int kChunks, int kTiles, int kMost>
 __global__ void __launch_bounds__(kMost * kWave, 4)
 head_logits_kernel(const uint16_t* __restrict__ hidden, int64_t B, uint32_t K, int64_t hidden_stride,

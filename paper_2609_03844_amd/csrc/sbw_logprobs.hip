@@ -235,8 +235,8 @@ row_pass_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row
 // ---------------------------------------------------------------------------
 // The k first logits of a row in order, by one workgroup, from the maxima of its groups.
 //
-// A chain of short dependent steps: threshold, groups, logits and order take 11-14 thousand cycles (the kernel 5-7.5 us)
-// for 5 to 50 of a row, 19 for 100; 1024 of 151936 take the kernel 18 us.
+// A chain of short dependent steps: threshold, groups, logits and order take 11-14 thousand cycles (the kernel
+// 5-7.5 us) for 5 to 50 of a row, 19 for 100; 1024 of 151936 take the kernel 18 us.
 // A threshold t with at least k group maxima at or above it has at least k logits there, all in
 // those groups; bisection stops at a t that leaves not many more than k groups.  Their logits
 // from t on are gathered as (key << 32 | ~column), which no two logits share, and sorted.
@@ -896,6 +896,7 @@ token_logprobs_grad_kernel(const T* logits, int64_t B, uint32_t V, int64_t row_s
   const uint32_t j0 = blockIdx.x * (kThreads * kVecs) + threadIdx.x;
   const bool whole = (blockIdx.x + 1) * (kThreads * kVecs) <= V / kPer;
   const uint32_t first = blockIdx.x * kSegment;   // the segment's columns
+  const uint32_t ids_end = min(V, 0x80000000u);   // of tokens, from where on they are negative ids
   for (int64_t b = blockIdx.y; b < B; b += gridDim.y) {
     const T* row = logits + b * row_stride;
     T* out = grad + b * grad_stride;
@@ -918,7 +919,8 @@ token_logprobs_grad_kernel(const T* logits, int64_t B, uint32_t V, int64_t row_s
     float g = 0.0f;
     if (kOne) {
       token = static_cast<uint32_t>(tokens[b]);
-      g = token < V ? grad_logprobs[b] : 0.0f;
+      if (token >= ids_end) token = 0xFFFFFFFFu;
+      g = token < ids_end ? grad_logprobs[b] : 0.0f;
     } else {
       if (b != blockIdx.y) __syncthreads();   // the last row's list is done with
       if (threadIdx.x < kWave) {
@@ -927,9 +929,9 @@ token_logprobs_grad_kernel(const T* logits, int64_t B, uint32_t V, int64_t row_s
         for (uint32_t i0 = 0; i0 < n; i0 += kWave) {
           const uint32_t i = i0 + threadIdx.x;
           const uint32_t t = i < n ? static_cast<uint32_t>(tokens[b * n + i]) : 0xFFFFFFFFu;
-          const float of_token = t < V ? grad_logprobs[b * n + i] : 0.0f;
+          const float of_token = t < ids_end ? grad_logprobs[b * n + i] : 0.0f;
           g += of_token;
-          const bool here = t < V && t - first < kSegment;
+          const bool here = t < ids_end && t - first < kSegment;
           const uint64_t mask = __ballot(here);
           if (here) {
             const uint32_t at = before + __popcll(mask & ((uint64_t{1} << threadIdx.x) - 1u));
@@ -993,8 +995,8 @@ constexpr int64_t kLongSegment = kThreads * 32, kShortSegment = kThreads * 8;
 
 // Whether the pass takes the long form: rows that make enough workgroups of it, and so many blocks that the
 // selection is left with few.  For a large k only with eight groups for each, as every vector of a listed group
-// is another line to fetch, or where the lanes could not hold the short form's (1024 of 16 x 151936 fp32: 20.9 us short, 23.6 long;
-// 500 of 100 x 150000 bf16, 24.7 and 22.3).
+// is another line to fetch, or where the lanes could not hold the short form's (1024 of 16 x 151936
+// fp32: 20.9 us short, 23.6 long; 500 of 100 x 150000 bf16, 24.7 and 22.3).
 bool long_segments(int64_t B, int64_t V, int64_t top) {
   const int64_t segments = (V + kLongSegment - 1) / kLongSegment;
   if (top > kSmallMost) return V / 32 >= 8 * top || V / 8 > 20 * SelectionSize<false>::kT;

@@ -448,6 +448,19 @@ def test_far_rows(sbw):
     close(d, want, tol, "gradient")
 
 
+@pytest.mark.parametrize("n", [1, 2])
+def test_columns_beyond_the_ids(sbw, n):
+    """A negative id is padding also where the row has a column of that number without a sign."""
+    V = 2 ** 31 + 64
+    x = torch.zeros((1, V), dtype=torch.bfloat16, device="cuda")
+    ids = torch.full((1, n), -2 ** 31, dtype=torch.int32, device="cuda")
+    r = sbw.token_logprobs(x, ids)
+    assert r.logprobs.count_nonzero().item() == 0 and abs(r.lse.item() - np.log(V)) < 1e-5
+    d = sbw.token_logprobs_grad(x, ids, r.stats, r.entropy, torch.ones((1, n), device="cuda"))
+    for part in d[0].split(2 ** 28):
+        assert part.count_nonzero().item() == 0
+
+
 def test_streams_graphs_and_repeats(sbw):
     """Another stream, a captured step replayed with other work between, and the same bits every time."""
     rng = np.random.default_rng(13)
