@@ -15,7 +15,7 @@ constexpr int kMostTokens = SBW_STEP_MAX_TOKENS;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.693147180559945309417f;
 // A score's floor inside the weighted sums: its exponential is 0, and 0 times it is 0 where 0 times -inf
-// would be NaN.  No lower than it has to be, as the gradient multiplies it by an upstream one and inv_t.
+// would be NaN.  No lower than it has to be, as the gradient multiplies it by an upstream one.
 constexpr float kScoreFloor = -1000.0f;
 // c; finite for every inv_t, as the largest logit's score is 0 times it.
 __host__ __device__ inline float score_factor(float inv_t) { return fminf(inv_t * kLog2e, 3.402823466e38f); }
@@ -866,14 +866,15 @@ __device__ __forceinline__ void store_any(T* row, uint32_t V, uint32_t j, typena
 }
 
 // What a row's gradient is made of.  For column v with score y = (x_v - m) inv_t and
-// log p = y - ln S:  d_v = p (share - slope log p) + inv_t * (the gradients of the tokens v),
-// share = inv_t (g_lse - sum_j g_j - g_H H), slope = inv_t g_H.
+// log p = y - ln S:  d_v = inv_t * (p (share - g_H log p) + the gradients of the tokens v),
+// share = g_lse - sum_j g_j - g_H H.  This is all but the last product, by inv_t, which comes after the sum: only
+// a gradient beyond the type's range is infinite then, and a column of probability 0 has 0 for any inv_t.
 struct RowGradient {
-  float m, ln_s, inv_t, share, slope;
-  __device__ __forceinline__ float operator()(float x) const {
+  float m, ln_s, inv_t, share, g_entropy;
+  __device__ __forceinline__ float operator()(float x, float of_tokens) const {
     const float y = __builtin_fmaf(x - m, inv_t, -ln_s);
     const float p = __builtin_amdgcn_exp2f(y * kLog2e);
-    return p * __builtin_fmaf(-slope, fmaxf(y, kScoreFloor), share);
+    return __builtin_fmaf(p, __builtin_fmaf(-g_entropy, fmaxf(y, kScoreFloor), share), of_tokens);
   }
 };
 
@@ -911,9 +912,8 @@ token_logprobs_grad_kernel(const T* logits, int64_t B, uint32_t V, int64_t row_s
     RowGradient r{stats[2 * b], stats[2 * b + 1], inv_t, 0.0f, 0.0f};
     if (grad_lse != nullptr) r.share = grad_lse[b];
     if (grad_entropy != nullptr) {
-      r.slope = grad_entropy[b];
-      r.share = __builtin_fmaf(-r.slope, entropy[b], r.share);
-      r.slope *= inv_t;
+      r.g_entropy = grad_entropy[b];
+      r.share = __builtin_fmaf(-r.g_entropy, entropy[b], r.share);
     }
     uint32_t token = 0xFFFFFFFFu;
     float g = 0.0f;
@@ -950,17 +950,14 @@ token_logprobs_grad_kernel(const T* logits, int64_t B, uint32_t V, int64_t row_s
       __syncthreads();
       g = total_of_row;
     }
-    r.share = (r.share - g) * inv_t;
+    r.share -= g;
     const bool empty = r.m == -INFINITY;
 #pragma unroll
     for (int u = 0; u < kVecs; ++u) {
       const uint32_t j = j0 + u * kThreads;
       float d[kPer];
 #pragma unroll
-      for (uint32_t e = 0; e < kPer; ++e) {
-        d[e] = r(elem(x[u], e));
-        if (kOne && j * kPer + e == token) d[e] = __builtin_fmaf(g, inv_t, d[e]);
-      }
+      for (uint32_t e = 0; e < kPer; ++e) d[e] = r(elem(x[u], e), kOne && j * kPer + e == token ? g : 0.0f);
       if (!kOne) {
         const uint32_t at = j * kPer - first;
         const uint32_t marks = marked[at / 32] >> at % 32 & ((1u << kPer) - 1u);
@@ -970,10 +967,12 @@ token_logprobs_grad_kernel(const T* logits, int64_t B, uint32_t V, int64_t row_s
             if ((marks >> e & 1u) == 0) continue;
             float of_column = 0.0f;
             for (uint32_t i = 0; i < listed; ++i) of_column += ids[i] == j * kPer + e ? gs[i] : 0.0f;
-            d[e] = __builtin_fmaf(of_column, inv_t, d[e]);
+            d[e] += of_column;
           }
         }
       }
+#pragma unroll
+      for (uint32_t e = 0; e < kPer; ++e) d[e] *= inv_t;
       if (empty) {
 #pragma unroll
         for (uint32_t e = 0; e < kPer; ++e) d[e] = 0.0f;

@@ -1,0 +1,40 @@
+"""The operators of include/sbw_step.h at the limits of their arguments."""
+import numpy as np
+import pytest
+import torch
+
+import step_reference as ref
+from test_gpu_step import DTYPES, close, given, sbw, upstream  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 3])
+@pytest.mark.parametrize("which", ["p", "l", "h", "plh"])
+@pytest.mark.parametrize("inv_t,scale", [(3e38, 1.0), (3e38, 1e-30), (1e37, 100.0), (1e-37, 1e36)])
+def test_gradient_of_extreme_products(sbw, dtype, n, which, inv_t, scale):  # noqa: F811
+    """Factors and upstream gradients whose product passes fp32's range: infinite where the gradient is, and
+    0 for the columns of probability 0."""
+    rng = np.random.default_rng(21)
+    B, V = 4, 3001
+    x = -np.abs(np.round(4 * rng.standard_normal((B, V)))).astype(np.float32)
+    x[1] -= 1
+    x[1, 77] = 0                               # one alone
+    x[2] = 0                                   # all alike
+    tokens = given(rng, B, V, n)
+    tokens[1, 0] = 77
+    t = torch.from_numpy(x).to(DTYPES[dtype]).cuda()
+    flat = torch.from_numpy(tokens[:, 0].copy() if n == 1 else tokens).cuda()
+    r = sbw.token_logprobs(t, flat, inv_t)
+    stats, H = r.stats.cpu().numpy(), r.entropy.cpu().numpy()
+    up = [np.float32(scale) * u if u is not None else None for u in upstream(rng, B, n, which)]
+    given_up = [u if u is not None else np.zeros((B, n) if i == 0 else B) for i, u in enumerate(up)]
+    want, tol = ref.gradient(x, tokens, inv_t, stats, H, *given_up, bf16=dtype == "bf16")
+    limit = float(torch.finfo(DTYPES[dtype]).max)
+    assert not ((np.abs(want) > 0.98 * limit) & (np.abs(want) < 1.02 * limit)).any()   # of the inputs
+    want = np.where(np.abs(want) > limit, np.copysign(np.inf, want), want)
+    dev = [torch.from_numpy(u).cuda() if u is not None else None for u in up]
+    if dev[0] is not None:
+        dev[0] = dev[0].view(flat.shape)
+    close(sbw.token_logprobs_grad(t, flat, r.stats, r.entropy, *dev, inv_t), want, tol, f"{which} n={n}")
