@@ -12,6 +12,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <c10/core/TensorImpl.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
@@ -363,6 +364,9 @@ struct Block {
   }
 };
 
+// Whether a gradient is asked for: the Python path refuses it for outputs that carry none.
+bool followed(const Tensor& t) { return t.requires_grad() && c10::GradMode::is_enabled(); }
+
 // logits and, unless None, tokens [rows] or [rows, n]
 bool tokens_call(PyObject* logits, PyObject* tokens, Call* c, const Tensor** ids, int64_t* n) {
   if (!matrix_of(logits, c) || (c->rows > 1 && c->row_stride < c->columns)) return false;
@@ -465,7 +469,7 @@ PyObject* top_candidates(PyObject*, PyObject* const* a, Py_ssize_t count) {
     const Tensor* none;
     int64_t n, k, v_offset;
     if (count != 3 || !tokens_call(a[0], Py_None, &c, &none, &n) || !integer(a[1], &k) || k < 1 ||
-        !integer(a[2], &v_offset) || k > SBW_STEP_MAX_TOKENS)
+        !integer(a[2], &v_offset) || k > SBW_STEP_MAX_TOKENS || followed(*c.matrix))
       Py_RETURN_NONE;
     Block block(sbw_top_candidates_workspace(c.rows, c.columns, k), 2 * c.rows * k, c);
     Tensor ids = block.take(at::kInt, {c.rows, k}), values = block.take(at::kFloat, {c.rows, k});
@@ -488,7 +492,7 @@ PyObject* head_logits(PyObject*, PyObject* const* a, Py_ssize_t count) {
   return guarded([&]() -> PyObject* {
     Call c;
     if (count != 4 || !matrix_of(a[0], &c) || c.matrix->scalar_type() != at::kBFloat16 || !PyBool_Check(a[3]) ||
-        (c.rows > 1 && c.row_stride < c.columns))
+        (c.rows > 1 && c.row_stride < c.columns) || followed(*c.matrix))
       Py_RETURN_NONE;
     const Tensor* codes = packed_of(a[1], at::kByte, c.device);
     if (codes == nullptr || codes->dim() != 2 || 2 * codes->size(1) != c.columns || codes->size(0) == 0)
@@ -501,7 +505,7 @@ PyObject* head_logits(PyObject*, PyObject* const* a, Py_ssize_t count) {
       scale_dtype = SBW_BF16;
     }
     if (scales == nullptr || scales->dim() != 2 || scales->size(0) != V || scales->size(1) == 0 ||
-        c.columns % scales->size(1) != 0)
+        c.columns % scales->size(1) != 0 || followed(*scales))
       Py_RETURN_NONE;
     const bool bf16 = a[3] == Py_True;
     Tensor logits = at::empty({c.rows, V}, c.matrix->options().dtype(bf16 ? at::kBFloat16 : at::kFloat)

@@ -101,6 +101,15 @@ def _vector(t: Optional[torch.Tensor], shape, dtype, name: str) -> Optional[int]
     return t.data_ptr()
 
 
+def _no_gradient(what: str, **tensors) -> None:
+    """Refuses inputs whose gradient a call would drop."""
+    if torch.is_grad_enabled():
+        for name, t in tensors.items():
+            if t.requires_grad:
+                raise ValueError(f"{what} carry no gradient to {name}: give {name}.detach(), or call under "
+                                 "torch.no_grad()")
+
+
 def _side(stream, device):
     """The torch stream of a stream argument that is not the current one, else None."""
     if stream is None or device.type != "cuda" or _stream(stream) == _stream(None):
@@ -241,7 +250,7 @@ def token_logprobs_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor], st
     """The gradient with respect to the logits, given that of token_logprobs()'s outputs: each
     grad_* is float32, shaped as its output, or None.  stats and entropy are what the forward call
     returned (entropy is needed with grad_entropy only).  ``out`` is like logits; it may be the
-    logits themselves."""
+    logits themselves.  The result carries no gradient of its own."""
     if stream is None and out is None:
         got = _native.token_logprobs_grad(logits, tokens, stats, entropy, grad_logprobs, grad_lse,
                                           grad_entropy, inv_temperature)
@@ -283,13 +292,16 @@ def top_candidates(logits: torch.Tensor, k: int, v_offset: int = 0,
     """The k <= 1024 largest logits of every row: (ids int32 [B, k], values float32 [B, k] or
     None), larger first, equal ones by their id, a NaN above every number.  Places beyond V hold
     -1 and -inf.  The ids are what ``watermark_candidates`` takes.  v_offset: the token id of
-    column 0 when the logits are a vocabulary shard."""
+    column 0 when the logits are a vocabulary shard.  The values carry no gradient: logits that require
+    one are refused unless it is off (torch.no_grad()) or the ids alone are asked for."""
     if stream is None and ids is None and values is None and workspace is None and with_values:
         got = _native.top_candidates(logits, k, v_offset)
         if type(got) is tuple:
             return got
         if got is not None:
             _check(got)
+    if with_values or values is not None:
+        _no_gradient("the values of top_candidates", logits=logits)
     dtype, B, V, row_stride = _matrix(logits, "logits")
     k = int(k)
     dev = logits.device
@@ -318,7 +330,8 @@ def head_logits(hidden: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
 
     hidden: bfloat16 [B, K], unit stride along K, K <= 8192.  codes: uint8 [V, K / 2] and scales:
     float32 or bfloat16 [V, K / group], contiguous; group is 32, 64 or 128.  V may be a shard
-    of the vocabulary.  dtype (of the logits): float32 or bfloat16.
+    of the vocabulary.  dtype (of the logits): float32 or bfloat16.  The logits carry no gradient: hidden
+    states or scales that require one are refused unless it is off (torch.no_grad()).
     """
     if stream is None and out is None and (dtype is torch.float32 or dtype is torch.bfloat16):
         got = _native.head_logits(hidden, codes, scales, dtype is torch.bfloat16)
@@ -326,6 +339,7 @@ def head_logits(hidden: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
             return got
         if got is not None:
             _check(got)
+    _no_gradient("the logits of head_logits", hidden=hidden, scales=scales)
     if hidden.dim() != 2 or hidden.dtype != torch.bfloat16:
         raise ValueError("hidden must be bfloat16 [B, K]")
     _, B, K, hidden_stride = _matrix(hidden, "hidden")

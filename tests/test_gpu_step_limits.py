@@ -38,3 +38,25 @@ def test_gradient_of_extreme_products(sbw, dtype, n, which, inv_t, scale):  # no
     if dev[0] is not None:
         dev[0] = dev[0].view(flat.shape)
     close(sbw.token_logprobs_grad(t, flat, r.stats, r.entropy, *dev, inv_t), want, tol, f"{which} n={n}")
+
+
+def test_what_requires_a_gradient(sbw):  # noqa: F811
+    """On the native path too: inputs that a call would drop the gradient of, and the calls that are right."""
+    x = torch.randn(3, 50, device="cuda", requires_grad=True)
+    h = torch.randn(3, 128, device="cuda").bfloat16().requires_grad_()
+    codes = torch.zeros((5, 64), dtype=torch.uint8, device="cuda")
+    scales = torch.ones((5, 1), device="cuda", requires_grad=True)
+    for call in (lambda: sbw.head_logits(h, codes, scales.detach()), lambda: sbw.head_logits(h.detach(), codes, scales),
+                 lambda: sbw.top_candidates(x, 4)):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+        with torch.no_grad():
+            call()
+    assert torch.equal(sbw.top_candidates(x, 4, with_values=False)[0], sbw.top_candidates(x.detach(), 4)[0])
+    ids = torch.zeros(3, dtype=torch.int32, device="cuda")
+    r = sbw.token_logprobs(x, ids)
+    assert r.logprobs.requires_grad
+    d = sbw.token_logprobs_grad(x, ids, r.stats, None, torch.ones(3, device="cuda"))   # a leaf's, by hand
+    assert not d.requires_grad
+    r.logprobs.sum().backward()
+    assert torch.equal(x.grad, d)
