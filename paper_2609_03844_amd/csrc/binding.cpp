@@ -364,14 +364,16 @@ struct Block {
   }
 };
 
-// Whether a gradient is asked for: the Python path refuses it for outputs that carry none.
+// Whether a gradient is asked for, or a tangent: the Python path refuses them for outputs that carry none.
 bool followed(const Tensor& t) { return t.requires_grad() && c10::GradMode::is_enabled(); }
+bool dual(const Tensor& t) { return t._fw_grad(0).defined(); }
 
 // logits and, unless None, tokens [rows] or [rows, n]
 bool tokens_call(PyObject* logits, PyObject* tokens, Call* c, const Tensor** ids, int64_t* n) {
   if (!matrix_of(logits, c) || (c->rows > 1 && c->row_stride < c->columns)) return false;
   if (c->matrix->scalar_type() == at::kBFloat16) c->dtype = SBW_BF16;
   else if (c->matrix->scalar_type() != at::kFloat) return false;
+  if (dual(*c->matrix)) return false;
   *ids = nullptr;
   *n = 0;
   if (tokens == Py_None) return true;
@@ -387,7 +389,7 @@ bool floats_of(PyObject* o, at::IntArrayRef shape, const Call& c, const float** 
   *out = nullptr;
   if (o == Py_None) return true;
   const Tensor* t = packed_of(o, at::kFloat, c.device);
-  if (t == nullptr || t->sizes() != shape) return false;
+  if (t == nullptr || t->sizes() != shape || dual(*t)) return false;
   *out = static_cast<const float*>(t->data_ptr());
   return true;
 }
@@ -492,7 +494,7 @@ PyObject* head_logits(PyObject*, PyObject* const* a, Py_ssize_t count) {
   return guarded([&]() -> PyObject* {
     Call c;
     if (count != 4 || !matrix_of(a[0], &c) || c.matrix->scalar_type() != at::kBFloat16 || !PyBool_Check(a[3]) ||
-        (c.rows > 1 && c.row_stride < c.columns) || followed(*c.matrix))
+        (c.rows > 1 && c.row_stride < c.columns) || followed(*c.matrix) || dual(*c.matrix))
       Py_RETURN_NONE;
     const Tensor* codes = packed_of(a[1], at::kByte, c.device);
     if (codes == nullptr || codes->dim() != 2 || 2 * codes->size(1) != c.columns || codes->size(0) == 0)
@@ -505,7 +507,7 @@ PyObject* head_logits(PyObject*, PyObject* const* a, Py_ssize_t count) {
       scale_dtype = SBW_BF16;
     }
     if (scales == nullptr || scales->dim() != 2 || scales->size(0) != V || scales->size(1) == 0 ||
-        c.columns % scales->size(1) != 0 || followed(*scales))
+        c.columns % scales->size(1) != 0 || followed(*scales) || dual(*scales))
       Py_RETURN_NONE;
     const bool bf16 = a[3] == Py_True;
     Tensor logits = at::empty({c.rows, V}, c.matrix->options().dtype(bf16 ? at::kBFloat16 : at::kFloat)

@@ -8,7 +8,8 @@
 Ordinary calls are marshalled in native code (``_binding.so``), the others here.  Same conventions
 as the watermark's calls: tensors on the current HIP device, unit stride
 along the vocabulary, rows padded or not, the current stream unless one is given, every step
-in the HIP kernels of ``libsbw.so``.
+in the HIP kernels of ``libsbw.so``.  token_logprobs carries a gradient; inputs with a forward-mode
+tangent are refused.
 """
 from __future__ import annotations
 
@@ -17,6 +18,7 @@ import functools
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd.forward_ad import unpack_dual
 from torch.autograd.function import once_differentiable
 
 from . import BF16, F32, _check, _native, _on_device, _stream, raw
@@ -68,8 +70,14 @@ def _dtype(t: torch.Tensor, name: str) -> int:
     raise TypeError(f"{name} must be float32 or bfloat16")
 
 
+def _no_tangent(t: torch.Tensor, name: str) -> None:
+    if unpack_dual(t).tangent is not None:
+        raise ValueError(f"{name} has a forward-mode tangent, which these operators do not carry")
+
+
 def _matrix(t: torch.Tensor, name: str):
     """(dtype, rows, columns, row stride) of a matrix with unit stride along its rows."""
+    _no_tangent(t, name)
     if t.dim() != 2:
         raise ValueError(f"{name} must be two-dimensional")
     dtype = _dtype(t, name)
@@ -98,6 +106,7 @@ def _vector(t: Optional[torch.Tensor], shape, dtype, name: str) -> Optional[int]
         return None
     if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous {dtype} {list(shape)}")
+    _no_tangent(t, name)
     return t.data_ptr()
 
 
@@ -347,6 +356,7 @@ def head_logits(hidden: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
         raise ValueError("codes must be contiguous uint8 [V, K / 2]")
     V = codes.shape[0]
     scale_dtype = _dtype(scales, "scales")
+    _no_tangent(scales, "scales")
     if scales.dim() != 2 or scales.shape[0] != V or not scales.is_contiguous():
         raise ValueError("scales must be contiguous [V, K / group]")
     groups = scales.shape[1]

@@ -60,3 +60,26 @@ def test_what_requires_a_gradient(sbw):  # noqa: F811
     assert not d.requires_grad
     r.logprobs.sum().backward()
     assert torch.equal(x.grad, d)
+
+
+def test_tangents_are_refused(sbw):  # noqa: F811
+    """A forward-mode tangent of any floating-point input, which no call carries, is named and not dropped."""
+    x = torch.randn(3, 50, device="cuda")
+    ids = torch.zeros(3, dtype=torch.int32, device="cuda")
+    h, codes = torch.randn(3, 128, device="cuda").bfloat16(), torch.zeros((5, 64), dtype=torch.uint8, device="cuda")
+    scales = torch.ones((5, 1), device="cuda")
+    r = sbw.token_logprobs(x, ids)
+    g = torch.ones(3, device="cuda")
+    calls = [(lambda a: sbw.token_logprobs(a, ids), x), (lambda a: sbw.top_candidates(a, 4), x),
+             (lambda a: sbw.top_candidates(a, 4, with_values=False), x),
+             (lambda a: sbw.head_logits(a, codes, scales), h), (lambda a: sbw.head_logits(h, codes, a), scales),
+             (lambda a: sbw.token_logprobs_grad(a, ids, r.stats, None, g), x),
+             (lambda a: sbw.token_logprobs_grad(x, ids, a, None, g), r.stats),
+             (lambda a: sbw.token_logprobs_grad(x, ids, r.stats, None, a), g),
+             (lambda a: sbw.token_logprobs_grad(x, ids, r.stats, a, None, g, g), r.entropy)]
+    with torch.autograd.forward_ad.dual_level():
+        for i, (call, t) in enumerate(calls):
+            call(t)
+            with pytest.raises(ValueError, match="tangent"):
+                call(torch.autograd.forward_ad.make_dual(t, torch.ones_like(t)))
+                print("call", i, "took a dual tensor", flush=True)
