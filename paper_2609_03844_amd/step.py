@@ -197,6 +197,8 @@ class _Differentiable(torch.autograd.Function):
         ctx.set_materialize_grads(False)
         ctx.save_for_backward(logits, tokens, out.stats, out.entropy)
         ctx.inv_temperature = inv_temperature
+        side = _side(stream, logits.device)
+        ctx.done = side.record_event() if side is not None else None
         ctx.mark_non_differentiable(*(t for t in out[3:] if t is not None))   # stats and alternatives
         return tuple(out)
 
@@ -207,8 +209,10 @@ class _Differentiable(torch.autograd.Function):
         if g_logprobs is None and g_lse is None and g_entropy is None:
             return (None,) * 6
         g = [t.contiguous() if t is not None else None for t in (g_logprobs, g_lse, g_entropy)]
-        # on autograd's stream, whatever the forward call's: it has waited for these gradients, and they came
-        # after the outputs that they are the gradients of
+        # on autograd's stream, whatever the forward call's: it has waited for these gradients, and waits for the
+        # statistics here, as gradients need not come from reading the outputs
+        if ctx.done is not None:
+            torch.cuda.current_stream().wait_event(ctx.done)
         grad = token_logprobs_grad(logits.detach(), tokens, stats, entropy, *g, ctx.inv_temperature)
         return grad, None, None, None, None, None
 

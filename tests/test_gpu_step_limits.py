@@ -83,3 +83,29 @@ def test_tangents_are_refused(sbw):  # noqa: F811
             with pytest.raises(ValueError, match="tangent"):
                 call(torch.autograd.forward_ad.make_dual(t, torch.ones_like(t)))
                 print("call", i, "took a dual tensor", flush=True)
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_backward_before_the_outputs_are_there(sbw, raw):  # noqa: F811
+    """Upstream gradients that read no output of a call on another, busy stream: the backward pass waits for what
+    the call left."""
+    rng = np.random.default_rng(22)
+    x = torch.randn(16, 4097, device="cuda")
+    ids = torch.from_numpy(given(rng, 16, 4097, 1)[:, 0].copy()).cuda()
+    up = [torch.randn(16, device="cuda") for _ in range(3)]
+    side, busy = torch.cuda.Stream(), torch.randn(4096, 4096, device="cuda")
+
+    def gradient(stream):
+        z = x.clone().requires_grad_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            work = busy
+            for _ in range(10):
+                work = work @ busy * 1e-3
+        r = sbw.token_logprobs(z, ids, stream=stream)
+        d, = torch.autograd.grad(r[:3], z, up)
+        torch.cuda.synchronize()
+        return d
+    want = gradient(None)
+    for _ in range(3):
+        assert torch.equal(gradient(side.cuda_stream if raw else side), want)
