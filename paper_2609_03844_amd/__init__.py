@@ -189,6 +189,28 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _side(stream, device):
+    """The torch stream of a stream argument that is not the current one, else None."""
+    if stream is None or device.type != "cuda" or _stream(stream) == _stream(None):
+        return None
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    return torch.cuda.ExternalStream(_stream(stream)) if _stream(stream) else torch.cuda.default_stream()
+
+
+def _empty(shape, dtype, device, side, kept=True) -> torch.Tensor:
+    """Memory for work on ``side`` comes from that stream's, so that its last use there is over and the
+    next one waits; what the caller keeps is known to the current stream too."""
+    if side is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    here = torch.cuda.current_stream()
+    with torch.cuda.stream(side):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if kept:
+        t.record_stream(here)
+    return t
+
+
 def _key(key: int) -> int:
     return int(key) & 0xFFFFFFFFFFFFFFFF
 
@@ -330,13 +352,14 @@ def watermark_argmax(logits: torch.Tensor, prev_tokens: torch.Tensor, key: int, 
         raise ValueError("logits must have unit stride along the vocabulary")
     context, width = _window(prev_tokens, B)
     dev = logits.device
+    side = _side(stream, dev)
     if tokens is None:
-        tokens = torch.empty(B, dtype=torch.int32, device=dev)
+        tokens = _empty(B, torch.int32, dev, side)
     if values is None and with_values:
-        values = torch.empty(B, dtype=torch.float32, device=dev)
+        values = _empty(B, torch.float32, dev, side)
     need = argmax_workspace_size(B, V)
     if workspace is None:
-        workspace = torch.empty(max(need, 1), dtype=torch.int64, device=dev)
+        workspace = _empty(max(need, 1), torch.int64, dev, side, kept=False)
     if tokens.shape != (B,) or tokens.dtype != torch.int32 or not tokens.is_contiguous():
         raise ValueError("tokens must be contiguous int32 [B]")
     if (workspace.dtype != torch.int64 or not workspace.is_contiguous()
@@ -385,10 +408,11 @@ def watermark_argmax_noalloc(logits: torch.Tensor, prev_tokens: torch.Tensor, ke
         raise ValueError("logits must have unit stride along the vocabulary")
     context, width = _window(prev_tokens, B)
     dev = logits.device
+    side = _side(stream, dev)
     if tokens is None:
-        tokens = torch.empty(B, dtype=torch.int32, device=dev)
+        tokens = _empty(B, torch.int32, dev, side)
     if values is None and with_values:
-        values = torch.empty(B, dtype=torch.float32, device=dev)
+        values = _empty(B, torch.float32, dev, side)
     if tokens.shape != (B,) or tokens.dtype != torch.int32 or not tokens.is_contiguous():
         raise ValueError("tokens must be contiguous int32 [B]")
     if values is not None and (values.shape != (B,) or values.dtype != torch.float32
@@ -433,13 +457,14 @@ def watermark_sample(logits: torch.Tensor, prev_tokens: torch.Tensor, key: int, 
         raise ValueError("seeds must be contiguous 64-bit integers [B]")
     context, width = _window(prev_tokens, B)
     dev = logits.device
+    side = _side(stream, dev)
     if tokens is None:
-        tokens = torch.empty(B, dtype=torch.int32, device=dev)
+        tokens = _empty(B, torch.int32, dev, side)
     if scores is None and with_scores:
-        scores = torch.empty(B, dtype=torch.float32, device=dev)
+        scores = _empty(B, torch.float32, dev, side)
     need = argmax_workspace_size(B, V)
     if workspace is None:
-        workspace = torch.empty(max(need, 1), dtype=torch.int64, device=dev)
+        workspace = _empty(max(need, 1), torch.int64, dev, side, kept=False)
     if tokens.shape != (B,) or tokens.dtype != torch.int32 or not tokens.is_contiguous():
         raise ValueError("tokens must be contiguous int32 [B]")
     if (workspace.dtype != torch.int64 or not workspace.is_contiguous()
@@ -506,7 +531,7 @@ def green_mask(prev_tokens: torch.Tensor, V: int, key: int, gamma: float, seedin
     context, width = _window(prev_tokens, B)
     words = (int(V) + 31) // 32
     if out is None:
-        out = torch.empty((B, words), dtype=torch.int32, device=prev_tokens.device)
+        out = _empty((B, words), torch.int32, prev_tokens.device, _side(stream, prev_tokens.device))
     elif out.shape != (B, words) or out.dtype != torch.int32 or not out.is_contiguous():
         raise ValueError("out must be contiguous int32 [B, ceil(V/32)]")
     _on_device(prev_tokens=context, out=out)
@@ -532,10 +557,11 @@ def detect(tokens: torch.Tensor, key: int, gamma: float, seeding="context",
     if N > 0 and L > 0 and tokens.stride(1) != 1:
         raise ValueError("tokens must have unit stride along L")
     dev = tokens.device
+    side = _side(stream, dev)
     if counts is None:
-        counts = torch.empty(N, dtype=torch.int32, device=dev)
+        counts = _empty(N, torch.int32, dev, side)
     if z is None:
-        z = torch.empty(N, dtype=torch.float64, device=dev)
+        z = _empty(N, torch.float64, dev, side)
     if counts.shape != (N,) or counts.dtype != torch.int32 or not counts.is_contiguous():
         raise ValueError("counts must be contiguous int32 [N]")
     if z.shape != (N,) or z.dtype != torch.float64 or not z.is_contiguous():
@@ -567,12 +593,13 @@ def detect_ex(tokens: torch.Tensor, key: int, gamma: float, seeding="context", w
     if N > 0 and L > 0 and tokens.stride(1) != 1:
         raise ValueError("tokens must have unit stride along L")
     dev = tokens.device
+    side = _side(stream, dev)
     if lengths is not None and (lengths.shape != (N,) or lengths.dtype != torch.int32
                                 or not lengths.is_contiguous()):
         raise ValueError("lengths must be contiguous int32 [N]")
-    counts = torch.empty(N, dtype=torch.int32, device=dev) if counts is None else counts
-    scored = torch.empty(N, dtype=torch.int32, device=dev) if scored is None else scored
-    z = torch.empty(N, dtype=torch.float64, device=dev) if z is None else z
+    counts = _empty(N, torch.int32, dev, side) if counts is None else counts
+    scored = _empty(N, torch.int32, dev, side) if scored is None else scored
+    z = _empty(N, torch.float64, dev, side) if z is None else z
     for name, t, dt in (("counts", counts, torch.int32), ("scored", scored, torch.int32),
                         ("z", z, torch.float64)):
         if t.shape != (N,) or t.dtype != dt or not t.is_contiguous():

@@ -21,7 +21,7 @@ import torch
 from torch.autograd.forward_ad import unpack_dual
 from torch.autograd.function import once_differentiable
 
-from . import BF16, F32, _check, _native, _on_device, _stream, raw
+from . import BF16, F32, _check, _empty, _native, _on_device, _side, _stream, raw
 
 MAX_STEP_TOKENS = 1024   # SBW_STEP_MAX_TOKENS
 HEAD_GROUPS = (32, 64, 128)
@@ -117,28 +117,6 @@ def _no_gradient(what: str, **tensors) -> None:
             if t.requires_grad:
                 raise ValueError(f"{what} carry no gradient to {name}: give {name}.detach(), or call under "
                                  "torch.no_grad()")
-
-
-def _side(stream, device):
-    """The torch stream of a stream argument that is not the current one, else None."""
-    if stream is None or device.type != "cuda" or _stream(stream) == _stream(None):
-        return None
-    if isinstance(stream, torch.cuda.Stream):
-        return stream
-    return torch.cuda.ExternalStream(_stream(stream)) if _stream(stream) else torch.cuda.default_stream()
-
-
-def _empty(shape, dtype, device, side, kept=True) -> torch.Tensor:
-    """Memory for work on ``side`` comes from that stream's, so that its last use there is over and the
-    next one waits; what the caller keeps is known to the current stream too."""
-    if side is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    here = torch.cuda.current_stream()
-    with torch.cuda.stream(side):
-        t = torch.empty(shape, dtype=dtype, device=device)
-    if kept:
-        t.record_stream(here)
-    return t
 
 
 def _scratch(workspace: Optional[torch.Tensor], need: int, device, side) -> torch.Tensor:
