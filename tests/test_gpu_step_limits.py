@@ -3,8 +3,9 @@ import numpy as np
 import pytest
 import torch
 
+import head_accuracy
 import step_reference as ref
-from test_gpu_step import DTYPES, close, given, sbw, upstream  # noqa: F401
+from test_gpu_step import DTYPES, close, given, packed, sbw, upstream  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -109,3 +110,38 @@ def test_backward_before_the_outputs_are_there(sbw, raw):  # noqa: F811
     want = gradient(None)
     for _ in range(3):
         assert torch.equal(gradient(side.cuda_stream if raw else side), want)
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("K", [1024, 2304, 4096])
+def test_head_accuracy(sbw, K, group):  # noqa: F811
+    """Nearer to the definition than weights held as 128 + q would come: bf16 holds 16 + q as exactly, and its sums
+    lose three bits less."""
+    rng = np.random.default_rng(K + group)
+    codes, s, exact_s = packed(rng, 512, K, group, "f32")
+    h = torch.from_numpy(rng.standard_normal((4, K)).astype(np.float32)).to(torch.bfloat16)
+    out = sbw.head_logits(h.cuda(), torch.from_numpy(codes).cuda(), s).double().cpu().numpy()
+    h = h.float().numpy()
+    want, _ = ref.head(h, codes, exact_s)
+    off, coarse = (head_accuracy.off(x, want) for x in (out, head_accuracy.simulated(h, codes, exact_s, 128)))
+    print(f"K={K} group={group}: {off / ref.U:.2f} u, held as 128 + q {coarse / ref.U:.2f} u", flush=True)
+    assert off < coarse
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("K", [512, 4224])
+def test_head_rows_without_a_number(sbw, K, group, dtype):  # noqa: F811
+    """A hidden state with an infinity or NaN, at any column, gives NaN for every row of the head; the others'
+    logits are as without it."""
+    rng = np.random.default_rng(K * group)
+    codes, s, _ = packed(rng, 101, K, group, "bf16")
+    codes = torch.from_numpy(codes).cuda()
+    h = torch.from_numpy(rng.standard_normal((18, K)).astype(np.float32)).to(torch.bfloat16).cuda()
+    want = sbw.head_logits(h, codes, s, dtype=DTYPES[dtype])
+    bad = {1: (0, np.inf), 4: (K - 1, -np.inf), 7: (K // 2 + 5, np.nan), 16: (77, np.inf), 17: (300, -np.inf)}
+    for row, (column, value) in bad.items():
+        h[row, column] = value
+    out = sbw.head_logits(h, codes, s, dtype=DTYPES[dtype])
+    for b in range(18):
+        assert torch.isnan(out[b]).all() if b in bad else torch.equal(out[b], want[b]), b
