@@ -22,7 +22,8 @@
  * Rows out of the ordinary.  A row whose every logit is -inf (a mask that leaves nothing) has
  * log sum -inf, log probabilities -inf, entropy 0 and gradient 0.  A row with a NaN or +inf has no
  * distribution: its log sum, log probabilities and entropy are NaN, and with them its gradient.
- * A logit of -inf or of the type's lowest value in any other row is a token of probability 0.
+ * A logit of -inf in any other row is a token of probability 0; so is one further below the row's largest than
+ * fp32's largest number, and the type's lowest value beside ordinary logits at ordinary temperatures.
  */
 #ifndef SBW_STEP_H
 #define SBW_STEP_H
@@ -42,7 +43,8 @@ extern "C" {
  *     logprob  = y_t - lse of each given token t
  *     entropy  = -sum_v p_v log p_v,  p_v = exp(y_v - lse)
  *     the `top` largest logits' columns and log probabilities, in order.
- * The logits are read once.  Sums are held in fp32 relative to the row's largest logit.
+ * The logits are read once, and those of a few parts of each row again where alternatives are asked
+ * for.  Sums are held in fp32 relative to the row's largest logit.
  *
  *   tokens       device, [B, n] int32.  An id outside [0, V) is padding: its log probability
  *                is 0.  May be NULL when n == 0.
@@ -75,7 +77,8 @@ int64_t sbw_top_candidates_workspace(int64_t B, int64_t V, int64_t k);
  * sbw_token_logprobs_grad -- the gradient of sbw_token_logprobs's outputs with respect to the
  * logits: for the upstream gradients g_j of logprob j, g_l of lse and g_H of entropy,
  *     d_v = inv_temperature * ( sum_j g_j [v = t_j] + p_v * (g_l - sum_j g_j - g_H (log p_v + H)) ).
- * Padding tokens take no part.  A token given twice adds both gradients, in order.
+ * Padding tokens take no part.  A token given twice adds both gradients, in order.  Only a gradient beyond the
+ * range of dtype is infinite, as long as the upstream gradients and their sums stay below 2^117.
  *
  *   tokens, n, inv_temperature   as for sbw_token_logprobs.
  *   stats, entropy  device, [B, 2] and [B] float, as sbw_token_logprobs wrote them (entropy may
@@ -114,7 +117,8 @@ sbw_status_t sbw_top_candidates(const void *logits, sbw_dtype_t dtype, int64_t B
  * with 4-bit q[v, c]: the low half of byte codes[v * K/2 + c/2] for even c, the high half for odd.
  *
  *   hidden       device, [B, hidden_stride] bfloat16, hidden_stride >= K.  A row that holds an
- *                infinity or NaN gives NaN logits.
+ *                infinity or NaN gives NaN logits; so may one with a magnitude of 2^115 or more, whose
+ *                sums on the way pass fp32's range.
  *   B            rows; the weights are read once for every 16 of them.
  *   K            length of a hidden state: a multiple of group, 0 < K <= 8192 (0 or not a
  *                multiple: SBW_ERR_INVALID_ARG; beyond 8192: SBW_ERR_UNSUPPORTED).

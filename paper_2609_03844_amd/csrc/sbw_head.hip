@@ -80,6 +80,8 @@ __device__ __forceinline__ void exchange(u32x4& w) {
 // sums for one head row, so a group's scale is one value a lane; a tile's scales are loaded side by side
 // and handed out through LDS.  The waves' sums meet in LDS.
 //
+// Every 16 states read the head again (64 states of 128256 x 4096: 211 us, 16 of them 61).
+//
 // Bound by HBM, less what a tile's barrier, sums and stores leave uncovered: one state through 128256 x 4096 in
 // groups of 128 49 us (5.5 TB/s), 16 states in groups of 64 59 us (5.1 TB/s; one state in
 // those groups 53; all-zero states are faster, 59 where others took 66 in the same run), groups of 32 for
@@ -253,8 +255,14 @@ void launch_head_shape(const void* hidden, int64_t B, uint32_t K, int64_t hidden
       static_cast<T*>(logits), row_stride, waves);
 }
 
-// Few columns are shared by few waves, so that a CU holds 16 waves (their hidden states fill its registers)
-// in 4, 2 or 1 workgroups.
+// Few columns are shared by few waves, so that a CU holds up to 16 waves (their hidden states fill its registers)
+// in 4, 2 or 1 workgroups: 16 where K is 1024, 2048, 4096 or 8192, as few as 9 between them (2304, 4608).  One state through
+// 128256 rows in groups of 128, from a graph: K = 1024 16.5 us (4.3 TB/s), 2048 28.5-29.8 (4.7-4.9), 2304 31.3-32.8 (4.8-5.0),
+// 2560 33.3 (5.2), 3584 45.7 (5.4), 4096 53-54 (5.2), 4608 63.8 (4.9), 5120 66.6 (5.3), 7168 88.1 (5.6), 8192 104.1 (5.4).
+// The forms against each other: two chunks a wave with sums for 16 waves instead of 4, K = 1024, 20.5 us; instead of 8, 2048,
+// 28.7.  Four chunks a wave: 1024 27.7, 2048 33.5, 3584 48.2, 4096 53.3, but 16 states in groups of 64 69.3 (two 61.4).  In
+// groups of 32 four chunks need 6 vector registers more than there are (28 bytes of scratch a lane): K = 4608 107 us,
+// 8192 152 (4.3 TB/s) where 4096 with two chunks takes 60 (5.5).
 template <typename S, typename T, int kGroup>
 void launch_head_group(const void* hidden, int64_t B, uint32_t K, int64_t hidden_stride, const uint8_t* codes,
                        const void* scales, uint32_t V, void* logits, int64_t row_stride, hipStream_t stream) {

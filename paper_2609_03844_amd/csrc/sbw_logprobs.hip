@@ -175,8 +175,9 @@ struct Sums {
   }
 };
 
-// The streaming pass: one read of every logit, bound by HBM (bf16 statistics: nearly as much by the ten
-// instructions a logit, four of them its exponential).  512 x 152064 fp32: 47.3 us, 6.6 TB/s; 256 x 152064 bf16, maxima
+// The streaming pass: one read of every logit, bound by HBM (bf16 statistics: as much by the ten
+// instructions a logit, four of them its exponential: with the second launch 1024 x 128256 take 49.9 us, 5.3 TB/s,
+// where 512 x 152064 fp32 move 5.8 to 6.1).  512 x 152064 fp32: 46.7-47.3 us, 6.6 TB/s; 256 x 152064 bf16, maxima
 // only: 13.7 us, 5.7 TB/s; one row of 32000: 2.6 us, a launch and a memory round trip.
 // A workgroup takes a segment of kThreads * kVecs
 // vectors of a row, a lane kVecs of them, kThreads vectors apart.  A wave writes the statistics
@@ -236,14 +237,17 @@ row_pass_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row
 // The k first logits of a row in order, by one workgroup, from the maxima of its groups.
 //
 // A chain of short dependent steps: threshold, groups, logits and order take 11-14 thousand cycles (the kernel
-// 5-7.5 us) for 5 to 50 of a row, 19 for 100; 1024 of 151936 take the kernel 18 us.
+// 5-8 us) for 5 to 50 of a row, 19 for 100; 1024 of 151936 take the kernel 18 us.
 // A threshold t with at least k group maxima at or above it has at least k logits there, all in
 // those groups; bisection stops at a t that leaves not many more than k groups.  Their logits
 // from t on are gathered as (key << 32 | ~column), which no two logits share, and sorted.
-// For a small k the blocks' maxima serve as well, a sixteenth as many: every wave bisects them by itself,
+// For a small k the blocks' maxima serve as well, a sixteenth as many: the first wave bisects them by itself,
 // without a barrier.
 // Where too many groups tie at t (a mask, equal logits), only what lies above t is gathered,
-// fewer than k groups, and the rest are the first columns that equal t.
+// fewer than k groups, and the rest are the first columns that equal t.  Those are looked for from column 0 on,
+// 256 vectors at a time, each time a memory round trip and a barrier: where a tenth of a row's last quarter ties for
+// its largest logit, 40 of 1 x 32000 fp32 take 24 us (7.6 without ties), of 1 x 152064 87 (9.5), of 256 x 152064 bf16 82
+// (21.9); logits clipped or rounded so that ties stand everywhere take no longer than others.
 // ---------------------------------------------------------------------------
 // Two sizes: a few hundred logits by 4 waves, up to 1024 by 16.
 template <bool kSmall_>
@@ -253,8 +257,13 @@ struct SelectionSize {
   static constexpr uint32_t kList = kSmall ? 1024 : 4096;     // gathered logits
   static constexpr uint32_t kGroups = kSmall ? 512 : 2048;    // listed groups
 };
-constexpr uint32_t kSmallMost = 256;     // k of the small size
-constexpr uint32_t kRankMost = 128;      // gathered logits that are ordered by counting all of them
+// k of the small size.  Us small and large: 16 x 151936 fp32 100 13.4 and 14.9, 256 17.0 and 16.6; 64 x 128256 bf16 100
+// 15.6 and 16.2, 256 20.3 and 17.6.  (Where the blocks do not suffice the large one is ahead sooner: 150 of 1 x 32000,
+// 256 blocks, 17-19 and 12.)
+constexpr uint32_t kSmallMost = 256;
+// Gathered logits, about 1.3 k, that are ordered by counting all of them.  Us by counting and by buckets, 16 x 151936
+// fp32: 40 11.0 and 11.7, 100 13.4 and 13.4, 160 15.5 and 14.7.
+constexpr uint32_t kRankMost = 128;
 constexpr uint32_t kBuckets = 256;       // the others are counted in their bucket of keys
 
 template <typename Size>
@@ -704,8 +713,13 @@ __device__ __forceinline__ const uint64_t* sorted(uint32_t taken, Selection<Size
 }
 
 // A function of its own, not part of its kernels: within them it has too few scalar registers and takes a third
-// longer (1024 of 16 x 151936: 33 us, 24 so).  Its pointers carry their address spaces, or every
-// access of LDS and memory would be a flat one.
+// longer (1024 of 16 x 151936 in one run: 33 us, 24 so; later steps took it to 20).  Its pointers carry their address
+// spaces, or every access of LDS and memory would be a flat one.
+//
+// The blocks' maxima are taken for k up to half of the blocks.  Us by blocks and by groups: 40 of 1 x 32000 fp32 7.4
+// and 17.0, of 1 x 152064 9.0 and 88, of 256 x 152064 bf16 21.9 and 35.6; beyond half of 256 blocks 140 11.2 and 19.5, 180 15.2
+// and 18.8, 200 23.2 and 18.5.  A form holds as few keys a lane as the row allows: 40 of 1 x 32000 7.4 us, 9.0
+// with room for 20; 1000 17.1 and 18.6.
 #define SBW_LDS __attribute__((address_space(3)))
 #define SBW_GLOBAL __attribute__((address_space(1)))
 template <typename T, int kVecs, typename Size>
@@ -842,8 +856,8 @@ select_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_s
 }
 
 // ---------------------------------------------------------------------------
-// Gradient: one read and one write of every logit, bound by HBM: 256 x 152064 fp32 49 us (6.3 TB/s),
-// 1024 x 128256 bf16 82 us (6.4).
+// Gradient: one read and one write of every logit, bound by HBM.  From a graph, into two gradients in turn: 256 x
+// 152064 fp32 50.6 us (6.2 TB/s), 1024 x 128256 bf16 with the entropy's 84-88 us (6.0-6.3).
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ void put_logit(float* p, float x) { *p = x; }
 __device__ __forceinline__ void put_logit(uint16_t* p, float x) {
@@ -879,7 +893,8 @@ struct RowGradient {
 };
 
 // Several tokens a row (kOne is false): the first wave lists those of the segment in their order and marks their
-// columns; a lane that meets a marked column adds up its gradients from the list.
+// columns; a lane that meets a marked column adds up its gradients from the list.  One token is compared with every
+// column instead: 256 x 152064 fp32 50.4 us (55.4 by the list), 1024 x 128256 bf16 84.7 (94.4).
 template <typename T, int kVecs, bool kOne>
 __global__ void __launch_bounds__(kThreads)
 token_logprobs_grad_kernel(const T* logits, int64_t B, uint32_t V, int64_t row_stride,
@@ -993,7 +1008,12 @@ constexpr int kShortVecs = sizeof(T) == 4 ? 2 : 1;
 constexpr int64_t kLongSegment = kThreads * 32, kShortSegment = kThreads * 8;
 
 // Whether the pass takes the long form: rows that make enough workgroups of it, and so many blocks that the
-// selection is left with few.  For a large k only with eight groups for each, as every vector of a listed group
+// selection is left with few.  Us of a call, long and short: 128256 columns, no alternatives, fp32 8 rows 6.2 and 6.6, 32
+// (512 workgroups) 8.4 and 8.8, 512 43.7 and 46.4, bf16 512 26.1 and 34.4; with 20 alternatives bf16 16 rows 9.9 and
+// 11.2, 64 12.8 and 15.0, 512 30.2 and 43.5.  32000 columns, fp32 16 rows 5.5 and 4.8, 128 (512 workgroups) 8.6 and 7.9, 1024
+// 24.9 and 26.2; with 20 alternatives 9.0 and 8.0, 12.4 and 11.7, 37.8 and 34.9.  So the length of a row would tell the
+// better form more often than the number of workgroups does, which is off by up to 1.3 us below 512 of them and 3
+// above.  For a large k only with eight groups for each, as every vector of a listed group
 // is another line to fetch, or where the lanes could not hold the short form's (1024 of 16 x 151936
 // fp32: 20.9 us short, 23.6 long; 500 of 100 x 150000 bf16, 24.7 and 22.3).
 bool long_segments(int64_t B, int64_t V, int64_t top) {
@@ -1056,8 +1076,8 @@ template <typename T>
 void launch_grad(const void* logits, int64_t B, uint32_t V, int64_t row_stride, const int32_t* tokens, uint32_t n,
                  const float* stats, const float* entropy, const float* grad_logprobs, const float* grad_lse,
                  const float* grad_entropy, float inv_t, void* grad, int64_t grad_stride, hipStream_t stream) {
-  // Two vectors a lane, past the caches both ways, into a buffer that the last call did not write.  fp32 256 x
-  // 152064: 50.8 us (four vectors 53.5, stores through the caches 56.6); bf16 1024 x 128256: 84.1 (one vector
+  // Two vectors a lane, past the caches both ways, into a buffer that the last call did not write.  In one run, fp32
+  // 256 x 152064: 50.8 us (four vectors 53.5, stores through the caches 56.6); bf16 1024 x 128256: 84.1 (one vector
   // 89.9, through the caches 91.2).
   constexpr int kVecs = 2;
   constexpr int64_t kSegment = kThreads * kVecs * kPerOf<T>;

@@ -10,6 +10,10 @@ as the watermark's calls: tensors on the current HIP device, unit stride
 along the vocabulary, rows padded or not, the current stream unless one is given, every step
 in the HIP kernels of ``libsbw.so``.  token_logprobs carries a gradient; inputs with a forward-mode
 tangent are refused.
+
+With ``stream`` the work is on that stream: what the caller passes must be ready there, and stay unchanged and
+alive until it has been read (``Tensor.record_stream``); what the call allocates does by itself, and its outputs are
+ready when that stream is.
 """
 from __future__ import annotations
 
@@ -219,6 +223,9 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor],
     token_logprobs_workspace_size(B, V, top) elements and ``out`` the tensors to write (both
     allocated here when not given).
 
+    Outputs that are allocated here may share one storage with each other and with a small workspace: clone() what
+    is kept for long or saved to a file.
+
     With logits that require a gradient, logprobs, lse and entropy carry one (through
     ``token_logprobs_grad``; ``out`` must not be given).  The logits must then keep their
     values until the backward pass: the in-place ``watermark`` does not tell torch of its writes.
@@ -282,7 +289,8 @@ def top_candidates(logits: torch.Tensor, k: int, v_offset: int = 0,
                    workspace: Optional[torch.Tensor] = None, with_values: bool = True, stream=None):
     """The k <= 1024 largest logits of every row: (ids int32 [B, k], values float32 [B, k] or
     None), larger first, equal ones by their id, a NaN above every number.  Places beyond V hold
-    -1 and -inf.  The ids are what ``watermark_candidates`` takes.  v_offset: the token id of
+    -1 and -inf.  The ids are what ``watermark_candidates`` takes.  Both may share one storage, as token_logprobs()'s
+    outputs do.  v_offset: the token id of
     column 0 when the logits are a vocabulary shard.  The values carry no gradient: logits that require
     one are refused unless it is off (torch.no_grad()) or the ids alone are asked for."""
     if stream is None and ids is None and values is None and workspace is None and with_values:
