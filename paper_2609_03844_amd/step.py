@@ -74,14 +74,17 @@ def _dtype(t: torch.Tensor, name: str) -> int:
     raise TypeError(f"{name} must be float32 or bfloat16")
 
 
-def _no_tangent(t: torch.Tensor, name: str) -> None:
+def _plain(t: torch.Tensor, name: str) -> None:
+    """Refuses what a tensor's memory does not show."""
+    if t.is_neg():
+        raise ValueError(f"{name} is a lazily negated view: give {name}.resolve_neg()")
     if unpack_dual(t).tangent is not None:
         raise ValueError(f"{name} has a forward-mode tangent, which these operators do not carry")
 
 
 def _matrix(t: torch.Tensor, name: str):
     """(dtype, rows, columns, row stride) of a matrix with unit stride along its rows."""
-    _no_tangent(t, name)
+    _plain(t, name)
     if t.dim() != 2:
         raise ValueError(f"{name} must be two-dimensional")
     dtype = _dtype(t, name)
@@ -110,7 +113,7 @@ def _vector(t: Optional[torch.Tensor], shape, dtype, name: str) -> Optional[int]
         return None
     if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous {dtype} {list(shape)}")
-    _no_tangent(t, name)
+    _plain(t, name)
     return t.data_ptr()
 
 
@@ -190,7 +193,7 @@ class _Differentiable(torch.autograd.Function):
         logits, tokens, stats, entropy = ctx.saved_tensors
         if g_logprobs is None and g_lse is None and g_entropy is None:
             return (None,) * 6
-        g = [t.contiguous() if t is not None else None for t in (g_logprobs, g_lse, g_entropy)]
+        g = [t.resolve_neg().contiguous() if t is not None else None for t in (g_logprobs, g_lse, g_entropy)]
         # on autograd's stream, whatever the forward call's: it has waited for these gradients, and waits for the
         # statistics here, as gradients need not come from reading the outputs
         if ctx.done is not None:
@@ -346,7 +349,7 @@ def head_logits(hidden: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
         raise ValueError("codes must be contiguous uint8 [V, K / 2]")
     V = codes.shape[0]
     scale_dtype = _dtype(scales, "scales")
-    _no_tangent(scales, "scales")
+    _plain(scales, "scales")
     if scales.dim() != 2 or scales.shape[0] != V or not scales.is_contiguous():
         raise ValueError("scales must be contiguous [V, K / group]")
     groups = scales.shape[1]

@@ -145,3 +145,27 @@ def test_head_rows_without_a_number(sbw, K, group, dtype):  # noqa: F811
     out = sbw.head_logits(h, codes, s, dtype=DTYPES[dtype])
     for b in range(18):
         assert torch.isnan(out[b]).all() if b in bad else torch.equal(out[b], want[b]), b
+
+
+def test_negated_views(sbw):  # noqa: F811
+    """Upstream gradients that torch hands over as lazily negated views (of one element, so contiguous) count with
+    their sign, and direct calls refuse such views."""
+    x = torch.randn(1, 50, device="cuda")
+    ids = torch.tensor([7], dtype=torch.int32, device="cuda")
+    zero = torch.zeros(1, device="cuda")
+
+    def gradient(f):
+        z = x.clone().requires_grad_()
+        f(sbw.token_logprobs(z, ids)).sum().backward()
+        return z.grad
+    want = gradient(lambda r: -r.logprobs)
+    got = gradient(lambda r: torch.complex(zero, r.logprobs).conj().imag)
+    assert torch.equal(got, want)
+    up = torch.complex(zero, zero + 1).conj().imag
+    assert up.is_neg() and up.is_contiguous()
+    r = sbw.token_logprobs(x, ids)
+    with pytest.raises(ValueError, match="resolve_neg"):
+        sbw.token_logprobs_grad(x, ids, r.stats, None, up)
+    assert torch.equal(sbw.token_logprobs_grad(x, ids, r.stats, None, up.resolve_neg()), want)
+    with pytest.raises(ValueError, match="resolve_neg"):
+        sbw.top_candidates(up[None], 1)
