@@ -9,7 +9,7 @@ Ordinary calls are marshalled in native code (``_binding.so``), the others here.
 as the watermark's calls: tensors on the current HIP device, unit stride
 along the vocabulary, rows padded or not, the current stream unless one is given, every step
 in the HIP kernels of ``libsbw.so``.  token_logprobs carries a gradient; inputs with a forward-mode
-tangent are refused.
+tangent and lazily negated views are refused.
 
 With ``stream`` the work is on that stream: what the caller passes must be ready there, and stay unchanged and
 alive until it has been read (``Tensor.record_stream``); what the call allocates does by itself, and its outputs are
