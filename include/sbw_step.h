@@ -11,6 +11,8 @@
  *   token_logprobs       log probabilities of given tokens, log sum, entropy and the most
  *                        likely alternatives: what a step answers beside its token
  *   token_logprobs_grad  the gradient of those with respect to the logits
+ *   quantize_fp8         a matrix in 8-bit floating point with a scale for each block of 128
+ *   matmul_fp8           the product of two such matrices
  *
  * Logits are [B, row_stride] of dtype, element (b, v) at logits[b * row_stride + v], v < V;
  * columns from V on are neither read nor written.  Rows may start at any element.  Limits on
@@ -133,6 +135,53 @@ sbw_status_t sbw_head_logits(const void *hidden, int64_t B, int64_t K, int64_t h
                              const uint8_t *codes, const void *scales, sbw_dtype_t scale_dtype,
                              int64_t group, int64_t V, void *logits, sbw_dtype_t dtype,
                              int64_t row_stride, void *stream);
+
+/* Kinds of scales of an 8-bit matrix. */
+typedef enum SBW_ENUM_TYPE {
+    SBW_SCALE_E8M0 = 0,     /* a power of two: one byte e for 2^(e - 127)  */
+    SBW_SCALE_F32 = 1       /* any positive binary32 number               */
+} sbw_scale_t;
+
+/*
+ * sbw_quantize_fp8 -- a matrix as e4m3 codes (OCP: 448 the largest, no infinity) with a scale for each block of
+ * block_rows x 128 elements (those at the ends may be smaller), and the same of its transpose, whose blocks lie
+ * along its own rows.  With a the largest finite magnitude of a block (0 if there is none)
+ *     E8M0   scale = the smallest 2^e, -127 <= e, with a <= 448 * 2^e
+ *     F32    scale = max(a / 448, 2^-126), rounded to binary32
+ *     code   = the element times 1 / scale (both rounded to binary32; exact for E8M0), rounded to the nearest
+ *              e4m3 value, ties to even.  An infinity or NaN becomes NaN.
+ *
+ *   x            device, [M, row_stride] of dtype, element (m, k) for k < K; read once.
+ *   block_rows   1 or 128 (else SBW_ERR_UNSUPPORTED).
+ *   codes        device, [M, codes_stride] bytes, written for k < K, or NULL.  scales: device,
+ *                [ceil(M / block_rows), ceil(K / 128)] bytes or float, written (NULL exactly when codes is).
+ *   codes_t      device, [K, codes_t_stride] bytes, written for m < M, or NULL.  scales_t: device,
+ *                [ceil(K / block_rows), ceil(M / 128)].  Both codes and codes_t NULL is SBW_ERR_INVALID_ARG.
+ */
+sbw_status_t sbw_quantize_fp8(const void *x, sbw_dtype_t dtype, int64_t M, int64_t K, int64_t row_stride,
+                              int64_t block_rows, sbw_scale_t scale_type, uint8_t *codes, int64_t codes_stride,
+                              void *scales, uint8_t *codes_t, int64_t codes_t_stride, void *scales_t,
+                              void *stream);
+
+/*
+ * sbw_matmul_fp8 -- out[m, n] = sum_k a(m, k) * b(n, k) of two matrices of e4m3 codes with scales, as
+ * sbw_quantize_fp8 writes them: a(m, k) = a[m * a_stride + k] * a_scales[m / a_block_rows, k / 128].
+ * An fp32 result is made of exact products and fp32 sums.  For a bf16 one each product may be cut off 13 bits below
+ * the power of two of the largest of its eight neighbours (columns 8 i .. 8 i + 7) on its way into the fp32 sum.
+ * The product of two blocks' scales is to lie in fp32's range.  out is rounded once.
+ *
+ *   a, b         device, [M, a_stride] and [N, b_stride] bytes, K columns of each row read; strides < 2^23.
+ *   a_scales, b_scales   device, [ceil(M / a_block_rows), ceil(K / 128)] and [ceil(N / b_block_rows),
+ *                ceil(K / 128)], both of scale_type; block_rows 1 or 128.
+ *   K            > 0 (else SBW_ERR_INVALID_ARG).  M < 2^23 - 128, N < 2^30 (else SBW_ERR_UNSUPPORTED).
+ *   out          device, [M, out_stride] of dtype (fp32 or bf16), written for n < N.
+ *   workspace    device, sbw_matmul_fp8_workspace(M, N, K) uint64 elements (may be NULL where that is 0).
+ */
+int64_t sbw_matmul_fp8_workspace(int64_t M, int64_t N, int64_t K);
+sbw_status_t sbw_matmul_fp8(const uint8_t *a, int64_t M, int64_t a_stride, const void *a_scales,
+                            int64_t a_block_rows, const uint8_t *b, int64_t N, int64_t b_stride,
+                            const void *b_scales, int64_t b_block_rows, int64_t K, sbw_scale_t scale_type,
+                            void *out, sbw_dtype_t dtype, int64_t out_stride, uint64_t *workspace, void *stream);
 
 #ifdef __cplusplus
 }

@@ -20,6 +20,12 @@ and the operators beside it in a decode or training step (``step.py``):
     token_logprobs(logits, tokens, inv_temperature, top) -> TokenLogprobs
     token_logprobs_grad(logits, tokens, stats, ...) -> gradient like logits
 
+and products in 8 bits with a scale for each block of 128 (``fp8.py``):
+
+    quantize_fp8(x) -> (codes, scales)
+    matmul_fp8(a, a_scales, b, b_scales) -> a b^T
+    linear_fp8(x, weight) -> x weight^T, with both gradients
+
 Tensors are torch tensors on the current HIP device; torch provides the memory
 and the stream, nothing else.
 
@@ -621,3 +627,7 @@ from .step import (EXPORTED_STEP, TokenLogprobs, head_logits, token_logprobs,  #
 __all__ += ["token_logprobs", "token_logprobs_grad", "top_candidates", "head_logits",
             "TokenLogprobs", "token_logprobs_workspace_size", "top_candidates_workspace_size",
             "EXPORTED_STEP"]
+
+from .fp8 import linear_fp8, matmul_fp8, matmul_fp8_workspace_size, quantize_fp8  # noqa: E402
+
+__all__ += ["quantize_fp8", "matmul_fp8", "matmul_fp8_workspace_size", "linear_fp8"]

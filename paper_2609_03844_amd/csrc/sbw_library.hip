@@ -3,3 +3,4 @@
 #include "sbw_kernels.hip"
 #include "sbw_logprobs.hip"
 #include "sbw_head.hip"
+#include "sbw_fp8.hip"

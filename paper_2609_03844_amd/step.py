@@ -33,7 +33,8 @@ MAX_HIDDEN = 8192
 
 #: C entry points of include/sbw_step.h.
 EXPORTED_STEP = ("sbw_token_logprobs", "sbw_token_logprobs_workspace", "sbw_token_logprobs_grad",
-                 "sbw_top_candidates", "sbw_top_candidates_workspace", "sbw_head_logits")
+                 "sbw_top_candidates", "sbw_top_candidates_workspace", "sbw_head_logits",
+                 "sbw_quantize_fp8", "sbw_matmul_fp8", "sbw_matmul_fp8_workspace")
 
 
 def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
