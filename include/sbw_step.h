@@ -11,6 +11,7 @@
  *   token_logprobs       log probabilities of given tokens, log sum, entropy and the most
  *                        likely alternatives: what a step answers beside its token
  *   token_logprobs_grad  the gradient of those with respect to the logits
+ *   sample_tokens        a token of every row by temperature, top-k, top-p and min-p
  *   quantize_fp8         a matrix in 8-bit floating point with a scale for each block of 128
  *   matmul_fp8           the product of two such matrices
  *
@@ -135,6 +136,37 @@ sbw_status_t sbw_head_logits(const void *hidden, int64_t B, int64_t K, int64_t h
                              const uint8_t *codes, const void *scales, sbw_dtype_t scale_dtype,
                              int64_t group, int64_t V, void *logits, sbw_dtype_t dtype,
                              int64_t row_stride, void *stream);
+
+/*
+ * sbw_sample_tokens -- one token of every row, drawn from what the filters keep of softmax(logits * inv_temperature).
+ * In the order of logits, with the weights e_v = exp((logits_v - largest) * inv_temperature):
+ *     top-k   the first top_k logits;
+ *     top-p   of those the ones before which the weights sum to less than top_p times the sum over all of them,
+ *             the first at least;
+ *     min-p   of those the ones with e_v >= min_p.
+ * The token is the one of the largest logits_v * inv_temperature + G_v (rounded in fp32 twice, the lower column of equal
+ * ones), G_v the noise of sbw_watermark_sample for column v under the row's seed: without filters it is that
+ * call's token with gamma = 0.  Sums of weights are exact to 2^-40 of the largest weight and do not depend on any order.
+ * A row with a NaN or +inf gives the first column of the order and NaN; one of -inf alone column 0 and -inf.
+ *
+ *   seeds            device, [B] uint64.
+ *   inv_temperatures device, [B] float, or NULL: inv_temperature for all rows (finite and > 0, else
+ *                    SBW_ERR_INVALID_ARG; a row whose own is not gives token -1 and NaN).
+ *   top_ks           device, [B] int32, or NULL: top_k for all rows.  0 and less, V and more keep all.
+ *   top_ps, min_ps   device, [B] float each, or NULL: top_p and min_p for all rows (not NaN, else
+ *                    SBW_ERR_INVALID_ARG).  top_p keeps all from 1 on (or NaN), min_p up to 0 (or NaN); a min_p beyond 1
+ *                    is 1.
+ *   tokens           device, [B] int32, written.
+ *   logprobs         device, [B] float, written (may be NULL): the token's log probability among the kept.
+ *   workspace        device, sbw_sample_tokens_workspace(B, V) uint64 elements, caller-owned; contents on entry do
+ *                    not matter.  Calls that share one must be ordered.
+ */
+int64_t sbw_sample_tokens_workspace(int64_t B, int64_t V);
+sbw_status_t sbw_sample_tokens(const void *logits, sbw_dtype_t dtype, int64_t B, int64_t V, int64_t row_stride,
+                               const uint64_t *seeds, const float *inv_temperatures, float inv_temperature,
+                               const int32_t *top_ks, int64_t top_k, const float *top_ps, float top_p,
+                               const float *min_ps, float min_p, int32_t *tokens, float *logprobs,
+                               uint64_t *workspace, void *stream);
 
 /* Kinds of scales of an 8-bit matrix. */
 typedef enum SBW_ENUM_TYPE {

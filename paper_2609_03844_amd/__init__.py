@@ -19,6 +19,7 @@ and the operators beside it in a decode or training step (``step.py``):
     top_candidates(logits, k) -> (ids [B, k], values [B, k])
     token_logprobs(logits, tokens, inv_temperature, top) -> TokenLogprobs
     token_logprobs_grad(logits, tokens, stats, ...) -> gradient like logits
+    sample_tokens(logits, seeds, inv_temperature, top_k, top_p, min_p) -> (tokens [B], logprobs [B])
 
 and products in 8 bits with a scale for each block of 128 (``fp8.py``):
 
@@ -620,13 +621,14 @@ def detect_ex(tokens: torch.Tensor, key: int, gamma: float, seeding="context", w
     return counts, scored, z
 
 
-from .step import (EXPORTED_STEP, TokenLogprobs, head_logits, token_logprobs,  # noqa: E402
+from .step import (EXPORTED_STEP, TokenLogprobs, head_logits, sample_tokens,  # noqa: E402
+                   sample_tokens_workspace_size, token_logprobs,
                    token_logprobs_grad, token_logprobs_workspace_size, top_candidates,
                    top_candidates_workspace_size)
 
 __all__ += ["token_logprobs", "token_logprobs_grad", "top_candidates", "head_logits",
             "TokenLogprobs", "token_logprobs_workspace_size", "top_candidates_workspace_size",
-            "EXPORTED_STEP"]
+            "EXPORTED_STEP", "sample_tokens", "sample_tokens_workspace_size"]
 
 from .fp8 import linear_fp8, matmul_fp8, matmul_fp8_workspace_size, quantize_fp8  # noqa: E402
 

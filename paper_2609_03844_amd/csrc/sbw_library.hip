@@ -3,4 +3,5 @@
 #include "sbw_kernels.hip"
 #include "sbw_logprobs.hip"
 #include "sbw_head.hip"
+#include "sbw_sample.hip"
 #include "sbw_fp8.hip"

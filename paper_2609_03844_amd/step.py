@@ -4,6 +4,7 @@
     top_candidates(logits, k) -> (ids int32 [B, k], values float32 [B, k])
     token_logprobs(logits, tokens, inv_temperature=1.0, top=0) -> TokenLogprobs
     token_logprobs_grad(logits, tokens, stats, ...) -> the gradient, like logits
+    sample_tokens(logits, seeds, inv_temperature=1.0, top_k=0, top_p=1.0, min_p=0.0) -> (tokens, logprobs)
 
 Ordinary calls are marshalled in native code (``_binding.so``), the others here.  Same conventions
 as the watermark's calls: tensors on the current HIP device, unit stride
@@ -34,7 +35,8 @@ MAX_HIDDEN = 8192
 #: C entry points of include/sbw_step.h.
 EXPORTED_STEP = ("sbw_token_logprobs", "sbw_token_logprobs_workspace", "sbw_token_logprobs_grad",
                  "sbw_top_candidates", "sbw_top_candidates_workspace", "sbw_head_logits",
-                 "sbw_quantize_fp8", "sbw_matmul_fp8", "sbw_matmul_fp8_workspace")
+                 "sbw_quantize_fp8", "sbw_matmul_fp8", "sbw_matmul_fp8_workspace",
+                 "sbw_sample_tokens", "sbw_sample_tokens_workspace")
 
 
 def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
@@ -49,6 +51,10 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.sbw_top_candidates.argtypes = [P, i32, i64, i64, i64, i64, i64, P, P, P, P]
     lib.sbw_top_candidates_workspace.restype = i64
     lib.sbw_top_candidates_workspace.argtypes = [i64, i64, i64]
+    lib.sbw_sample_tokens.restype = i32
+    lib.sbw_sample_tokens.argtypes = [P, i32, i64, i64, i64, P, P, f32, P, i64, P, f32, P, f32, P, P, P, P]
+    lib.sbw_sample_tokens_workspace.restype = i64
+    lib.sbw_sample_tokens_workspace.argtypes = [i64, i64]
     lib.sbw_head_logits.restype = i32
     lib.sbw_head_logits.argtypes = [P, i64, i64, i64, P, P, i32, i64, i64, P, i32, i64, P]
     return lib
@@ -366,3 +372,61 @@ def head_logits(hidden: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
                                 scales.data_ptr(), scale_dtype, K // groups, V, out.data_ptr(),
                                 out_dtype, row_stride, _stream(stream)))
     return out
+
+
+@functools.lru_cache(maxsize=1024)
+def sample_tokens_workspace_size(B: int, V: int) -> int:
+    """int64 elements of scratch that sample_tokens needs."""
+    return int(_lib.sbw_sample_tokens_workspace(int(B), int(V)))
+
+
+def _of_rows(value, B: int, dtype, name: str):
+    """(address of a parameter of every row or None, the one of all rows)."""
+    if not isinstance(value, torch.Tensor):
+        return None, value
+    return _vector(value, (B,), dtype, name), 0
+
+
+def sample_tokens(logits: torch.Tensor, seeds: torch.Tensor, inv_temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
+                  tokens: Optional[torch.Tensor] = None, logprobs: Optional[torch.Tensor] = None,
+                  workspace: Optional[torch.Tensor] = None, with_logprobs: bool = True, stream=None):
+    """One token of every row, drawn from what the filters keep of softmax(logits * inv_temperature): (tokens int32 [B],
+    their log probabilities among the kept, float32 [B], or None).
+
+    In the order of logits (larger first, equal ones by their id) top_k keeps the first k, top_p of those the ones before
+    which less than top_p of their probability lies (the first at least), min_p of those the ones with at least min_p times
+    the largest probability.  0, 1 and 0 keep all.  Each parameter is a number, or a tensor with one for every row:
+    float32 [B], top_k int32 [B].
+
+    logits: [B, V] float32 or bfloat16, for instance as ``watermark()`` left them.  seeds: int64 [B], random; the noise is
+    that of ``watermark_sample``, and without filters so is the token (with gamma 0).  A row with a NaN or +inf gives the
+    first column of its order with NaN, one of -inf alone column 0 with -inf, and a row whose inv_temperature in a tensor
+    is not finite and positive -1 with NaN.  ``workspace`` is an int64 scratch tensor of at least
+    sample_tokens_workspace_size(B, V) elements.  The log probabilities carry no gradient (token_logprobs' do): logits
+    that require one are refused unless it is off (torch.no_grad()) or the tokens alone are asked for."""
+    if with_logprobs or logprobs is not None:
+        _no_gradient("the log probabilities of sample_tokens", logits=logits)
+    dtype, B, V, row_stride = _matrix(logits, "logits")
+    dev = logits.device
+    side = _side(stream, dev)
+    if seeds.dtype != torch.int64 or tuple(seeds.shape) != (B,) or not seeds.is_contiguous():
+        raise ValueError("seeds must be contiguous int64 [B]")
+    inv_ts, inv_t = _of_rows(inv_temperature, B, torch.float32, "inv_temperature")
+    top_ks, k = _of_rows(top_k, B, torch.int32, "top_k")
+    top_ps, p = _of_rows(top_p, B, torch.float32, "top_p")
+    min_ps, least = _of_rows(min_p, B, torch.float32, "min_p")
+    if tokens is None:
+        tokens = _empty(B, torch.int32, dev, side)
+    if logprobs is None and with_logprobs:
+        logprobs = _empty(B, torch.float32, dev, side)
+    _vector(tokens, (B,), torch.int32, "tokens")
+    _vector(logprobs, (B,), torch.float32, "logprobs")
+    workspace = _scratch(workspace, sample_tokens_workspace_size(B, V), dev, side)
+    given = {name: t for name, t in (("inv_temperature", inv_temperature), ("top_k", top_k), ("top_p", top_p),
+                                     ("min_p", min_p)) if isinstance(t, torch.Tensor)}
+    _on_device(logits=logits, seeds=seeds, tokens=tokens, logprobs=logprobs, workspace=workspace, **given)
+    _check(_lib.sbw_sample_tokens(logits.data_ptr(), dtype, B, V, row_stride, seeds.data_ptr(), inv_ts, float(inv_t), top_ks,
+                                  int(k), top_ps, float(p), min_ps, float(least), tokens.data_ptr(),
+                                  logprobs.data_ptr() if logprobs is not None else None, workspace.data_ptr(),
+                                  _stream(stream)))
+    return tokens, logprobs
