@@ -2,6 +2,8 @@
 // (sbw_step.h).  Part of sbw_library.hip.
 #include "sbw_step.h"
 
+#include <algorithm>
+
 namespace sbw {
 namespace {
 
@@ -284,6 +286,27 @@ struct Side {
   uint32_t row_shift;      // log2 of block_rows
 };
 
+// Four neighbouring results of a row, those in front of column N.
+__device__ __forceinline__ void put_four(float* row, int64_t n, int64_t N, f32x4 v) {
+  if (n + 4 <= N) {
+    *reinterpret_cast<f32x4_memory*>(row + n) = v;
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (n + e < N) row[n + e] = v[e];
+}
+__device__ __forceinline__ void put_four(uint16_t* row, int64_t n, int64_t N, f32x4 v) {
+  const u32x2 w = {to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3])};
+  if (n + 4 <= N) {
+    *reinterpret_cast<u32x2_memory*>(row + n) = w;
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (n + e < N) row[n + e] = static_cast<uint16_t>(w[e / 2] >> e % 2 * 16);
+}
+
 // Sixteen codes of a row from column k on; 0 from column K on.
 __device__ __forceinline__ u32x4 load_codes(const uint8_t* row, int64_t k, int64_t K) {
   if (k + 16 <= K) return *reinterpret_cast<const u32x4_bytes*>(row + k);
@@ -442,10 +465,614 @@ product_any_kernel(Side a, Side b, int64_t K, Out* __restrict__ out, int64_t out
       }
 }
 
+// Aligned codes, powers of two, bf16 results: tiles of 256 x 256 by four waves of 128 x 128.
+// The workgroup's tile: each XCD takes neighbouring ones, in groups of up to eight rows of tiles.
+struct TileAt {
+  uint32_t m, n;
+};
+__device__ __forceinline__ TileAt tile_at(uint32_t id, uint32_t tiles_m, uint32_t tiles_n) {
+  const uint32_t total = tiles_m * tiles_n, each = total / 8, rest = total % 8, xcd = id % 8;
+  const uint32_t at = xcd * each + min(xcd, rest) + id / 8;
+  const uint32_t of_group = 8 * tiles_n, first = at / of_group * 8, in_group = at % of_group;
+  const uint32_t rows = min(8u, tiles_m - first);
+  return TileAt{first + in_group % rows, in_group / rows};
+}
+
+// From memory straight into LDS, 16 bytes a lane (or a word), the wave's side by side from `to` on; `at` from 2^31 on
+// fetches zeros.  Written as instructions: behind a fetch that it knows the compiler waits for all of them before any
+// read of LDS.  `arrived` waits for all but the newest `kNewer` fetches, and for the wave's own reads.
+typedef uint32_t Buffer __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ Buffer buffer_of(const void* p) {
+  const uint64_t at = reinterpret_cast<uint64_t>(p);
+  return Buffer{static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(at))),
+                static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(at >> 32))), 0x7FFFFFFFu, 0x00027000u};
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return __builtin_amdgcn_readfirstlane(static_cast<int>(reinterpret_cast<uintptr_t>((SBW_LDS const void*)p)));
+}
+__device__ __forceinline__ void fetch_to_lds(Buffer from, uint32_t at, uint32_t base, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+               :: "s"(to), "v"(at), "s"(from), "s"(base) : "memory");
+}
+__device__ __forceinline__ void fetch_word_to_lds(Buffer from, uint32_t at, uint32_t base, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds"
+               :: "s"(to), "v"(at), "s"(from), "s"(base) : "memory");
+}
+// A word a lane; of scales of one byte that byte.
+template <bool kByte>
+__device__ __forceinline__ void fetch_scale_to_lds(Buffer from, uint32_t at, uint32_t base, uint32_t to) {
+  if constexpr (kByte)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_ubyte %1, %2, %3 offen lds"
+                 :: "s"(to), "v"(at), "s"(from), "s"(base) : "memory");
+  else
+    fetch_word_to_lds(from, at, base, to);
+}
+template <int kNewer>
+__device__ __forceinline__ void arrived() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(kNewer) : "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Shape of a tiles kernel: waves of kM x kN instructions of 16 x 16, kDown x kAcross of them.
+template <int kM_, int kN_, int kDown_, int kAcross_>
+struct TileShape {
+  static constexpr int kM = kM_, kN = kN_, kDown = kDown_, kAcross = kAcross_;
+  static constexpr uint32_t kRowsA = kM * 16 * kDown, kRowsB = kN * 16 * kAcross, kThreadsHere = kDown * kAcross * kWave;
+  static constexpr uint32_t kFetchRows = kThreadsHere / 8;                      // that one fetch of every lane covers
+  static constexpr int kFetchA = kRowsA / kFetchRows, kFetchB = kRowsB / kFetchRows;
+  static constexpr int kFetches = kFetchA + kFetchB;                         // of a step
+  // whether fetch i of side a holds rows of the second half of a wave's instructions
+  static constexpr bool upper(int i) { return i * kFetchRows / (kM * 8) % 2 != 0; }
+};
+
+template <typename Out, typename Shape>
+__global__ void __launch_bounds__(Shape::kThreadsHere, 1)
+product_tiles_kernel(Side a, Side b, uint32_t K, uint32_t blocks_each, Out* __restrict__ out, int64_t out_stride, int64_t out_part,
+                     uint32_t tiles_m, uint32_t tiles_n) {
+  static_assert(Shape::kM * 8 % Shape::kFetchRows == 0, "a fetch holds rows of one half");
+  constexpr int kM = Shape::kM, kN = Shape::kN;
+  constexpr uint32_t kRowsA = Shape::kRowsA, kRowsB = Shape::kRowsB, kRows = kRowsA + kRowsB, kFetchRows = Shape::kFetchRows;
+  constexpr uint32_t kThreadsHere = Shape::kThreadsHere, kStage = kRows * 8;    // 16-byte parts of a step
+  __shared__ __attribute__((aligned(1024))) u32x4 codes[2][kStage];
+  __shared__ uint32_t tile_scales[2][kRows];                                    // four blocks' bytes
+  const uint32_t tid = threadIdx.x, lane = tid % kWave, r16 = lane % 16, quarter = lane / 16;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const TileAt tile = tile_at(blockIdx.x, tiles_m, tiles_n);
+  const int64_t m0 = static_cast<int64_t>(tile.m) * kRowsA, n0 = static_cast<int64_t>(tile.n) * kRowsB;
+  // the grid's second dimension: parts of K, of a multiple of four blocks
+  const uint32_t all_blocks = (K + kBlock - 1) / kBlock, block0 = blockIdx.y * blocks_each;
+  const uint32_t blocks = min(blocks_each, all_blocks - block0);
+  const auto from_a = buffer_of(a.codes + m0 * a.stride), from_b = buffer_of(b.codes + n0 * b.stride);
+  const uint32_t last_a = static_cast<uint32_t>(min(a.rows - m0, int64_t{kRowsA}) - 1), last_b = static_cast<uint32_t>(min(b.rows - n0, int64_t{kRowsB}) - 1);
+  // this lane's part of a row in each fetch: its place in LDS is fixed, so the part is permuted
+  const uint32_t part16 = (tid % 8 ^ (tid / 16 & 7u)) * 16;
+  uint32_t at_a[Shape::kFetchA], at_b[Shape::kFetchB];
+#pragma unroll
+  for (int i = 0; i < Shape::kFetchA; ++i) at_a[i] = min(tid / 8 + i * kFetchRows, last_a) * static_cast<uint32_t>(a.stride) + part16;
+#pragma unroll
+  for (int i = 0; i < Shape::kFetchB; ++i) at_b[i] = min(tid / 8 + i * kFetchRows, last_b) * static_cast<uint32_t>(b.stride) + part16;
+  const uint32_t lds_codes = lds_address(&codes[0][0]) + wave * 1024, lds_scales = lds_address(&tile_scales[0][0]) + wave * 256;
+  const auto fetch = [&](uint32_t block, uint32_t turn, bool upper) {
+    const uint32_t k = (block0 + block) * kBlock, beyond = block < blocks && k + part16 < K ? 0u : 0x80000000u, to = lds_codes + turn * (kStage * 16);
+#pragma unroll
+    for (int i = 0; i < Shape::kFetchA; ++i)
+      if (Shape::upper(i) == upper) fetch_to_lds(from_a, at_a[i] | beyond, k, to + i * kFetchRows * 128);
+    if (upper) return;
+#pragma unroll
+    for (int i = 0; i < Shape::kFetchB; ++i) fetch_to_lds(from_b, at_b[i] | beyond, k, to + (kRowsA + i * kFetchRows) * 128);
+  };
+  // Four blocks' scales of a row are a word of LDS; those of blocks behind the last are never used with codes but 0, and
+  // are the last block's.  Words of memory are fetched like the codes; others are put together.
+  constexpr int kScaleRows = (kRows + kThreadsHere - 1) / kThreadsHere;
+  const bool words = all_blocks % 4 == 0 && (reinterpret_cast<uintptr_t>(a.scales) | reinterpret_cast<uintptr_t>(b.scales)) % 4 == 0;
+  const auto bring_scales = [&](uint32_t block) {
+    const uint32_t turn = block / 4 & 1;
+#pragma unroll
+    for (int i = 0; i < kScaleRows; ++i) {
+      const uint32_t r = tid + i * kThreadsHere;
+      if (kRows % kThreadsHere != 0 && r >= kRows) continue;
+      const bool of_a = r < kRowsA;
+      const Side& s = of_a ? a : b;
+      const int64_t row = (min(of_a ? m0 + r : n0 + r - kRowsA, s.rows - 1) >> s.row_shift) - ((of_a ? m0 : n0) >> s.row_shift);
+      const uint8_t* first = static_cast<const uint8_t*>(s.scales) + ((of_a ? m0 : n0) >> s.row_shift) * all_blocks;
+      if (words) {
+        fetch_word_to_lds(buffer_of(first), static_cast<uint32_t>(row) * all_blocks, min(block0 + block, all_blocks - 4),
+                          lds_scales + (turn * kRows + i * kThreadsHere) * 4);
+      } else {
+        uint32_t w = 0;
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) w |= static_cast<uint32_t>(first[row * all_blocks + min(block0 + block + e, all_blocks - 1)]) << e * 8;
+        tile_scales[turn][r] = w;
+      }
+    }
+  };
+  const uint32_t row_a = wave / Shape::kAcross * (kM * 16), row_b = wave % Shape::kAcross * (kN * 16);
+  // this lane's two parts of a row; other rows and the other step lie at fixed distances
+  uint32_t at_x[2], at_y[2];
+#pragma unroll
+  for (uint32_t c = 0; c < 2; ++c) {
+    at_x[c] = place_of(row_a + r16, quarter * 2 + c);
+    at_y[c] = place_of(kRowsA + row_b + r16, quarter * 2 + c);
+  }
+  const u32x4* const stage = &codes[0][0];
+  f32x4 total[kM][kN] = {};
+  constexpr int kAhead = 4;        // rows of instructions whose codes are held
+  Codes x[kAhead], y[kN];
+  uint32_t sx[kM], sy[kN];
+  const auto read_x = [&](int i) { x[i % kAhead] = Codes{stage[at_x[0] + i * 128], stage[at_x[1] + i * 128]}; };
+  const auto read_y = [&](int j) { y[j] = Codes{stage[at_y[0] + j * 128], stage[at_y[1] + j * 128]}; };
+  const auto read_scales = [&](uint32_t block) {   // four blocks' bytes, of which an instruction takes the lowest
+#pragma unroll
+    for (int t = 0; t < kM; ++t) sx[t] = tile_scales[block / 4 & 1][row_a + t * 16 + r16];
+#pragma unroll
+    for (int t = 0; t < kN; ++t) sy[t] = tile_scales[block / 4 & 1][kRowsA + row_b + t * 16 + r16];
+  };
+  const auto multiply = [&](int i, int j) {
+    total[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(as_operand(y[j]), as_operand(x[i % kAhead]), total[i][j], 0,
+                                                                   0, 0, sy[j], 0, sx[i]);
+  };
+  // The codes of a step are fetched in two parts, each as soon as every wave has read the one that stood in its place, two
+  // steps before: b and the lower halves of a's rows in the first quarter of a step, the upper halves in the last.  Whatever
+  // is waited for has had a whole step, as only what the newest step fetched may be still on its way.
+  constexpr int kOfStep = Shape::kFetchA + Shape::kFetchB, kUpper = Shape::kFetchA / 2;
+  bring_scales(0);
+  fetch(0, 0, false);
+  fetch(0, 0, true);
+  fetch(1, 1, false);
+  fetch(1, 1, true);
+  arrived<kOfStep + kUpper>();
+  read_scales(0);
+  read_x(0);
+  read_x(1);
+#pragma unroll
+  for (int j = 0; j < kN; ++j) read_y(j);
+  for (uint32_t block = 0; block < blocks; ++block) {
+#pragma unroll
+    for (int i = 0; i < kM; ++i) {
+      if (i == kM / 2 - 2) {
+        arrived<kOfStep>();
+        fetch(block + 2, block & 1, false);
+        if (block % 4 == 0) bring_scales(block + 4);
+      }
+      if (i == kM - 2) {
+        arrived<kOfStep>();
+        fetch(block + 2, block & 1, true);
+        const uint32_t other = block & 1 ? -kStage : kStage;
+        at_x[0] += other, at_x[1] += other, at_y[0] += other, at_y[1] += other;
+      }
+      read_x((i + 2) % kM);
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        multiply(i, j);
+        if (i == kM - 1) read_y(j);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // the instructions stay in front of the branch
+#pragma unroll
+    for (int i = 0; i < kM; ++i)
+#pragma unroll
+      for (int j = 0; j < kN; ++j) asm volatile("" : "+v"(total[i][j]));
+    if (block % 4 == 3) {
+      read_scales(block + 1);
+    } else {
+#pragma unroll
+      for (int t = 0; t < kM; ++t) sx[t] >>= 8;
+#pragma unroll
+      for (int t = 0; t < kN; ++t) sy[t] >>= 8;
+    }
+  }
+  arrived<0>();
+  if constexpr (sizeof(Out) == 4) {
+    out += blockIdx.y * out_part;
+#pragma unroll
+    for (int i = 0; i < kM; ++i) {
+      const int64_t m = m0 + row_a + i * 16 + r16;
+      if (m >= a.rows) continue;
+#pragma unroll
+      for (int j = 0; j < kN; ++j) put_four(out + m * out_stride, n0 + row_b + j * 16 + quarter * 4, b.rows, total[i][j]);
+    }
+    return;
+  }
+  // a wave's results, turned in LDS: 8 bytes of a row and four neighbouring columns a lane, in places permuted
+  // by the row; then 16 bytes a lane, whole rows
+  constexpr uint32_t kWide = kN * 4;       // places of 8 bytes in a row
+  auto* const turned = reinterpret_cast<u32x2*>(&codes[0][0]) + wave * (kM * 16 * kWide);
+#pragma unroll
+  for (int i = 0; i < kM; ++i)
+#pragma unroll
+    for (int j = 0; j < kN; ++j)
+      turned[(i * 16 + r16) * kWide + ((j * 4 + quarter) ^ (i * 16 + r16) % kWide)] =
+          u32x2{to_bf16x2(total[i][j][0], total[i][j][1]), to_bf16x2(total[i][j][2], total[i][j][3])};
+  __builtin_amdgcn_wave_barrier();
+  constexpr uint32_t kLanes = kWide / 2;   // of a row
+  const int64_t n = n0 + row_b + lane % kLanes * 8;
+#pragma unroll 4
+  for (uint32_t p = 0; p < kM * 16 * kLanes / kWave; ++p) {
+    const uint32_t r = p * (kWave / kLanes) + lane / kLanes;
+    const int64_t m = m0 + row_a + r;
+    const u32x4 w = reinterpret_cast<const u32x4*>(turned)[r * kLanes + (lane % kLanes ^ (r % kWide >> 1))];
+    const u32x4 v = r & 1 ? u32x4{w.z, w.w, w.x, w.y} : w;
+    if (m >= a.rows) continue;
+    auto* to = reinterpret_cast<uint16_t*>(out) + m * out_stride + n;
+    if (n + 8 <= b.rows) {
+      *reinterpret_cast<u32x4_memory*>(to) = v;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (n + e < b.rows) to[e] = static_cast<uint16_t>(v[e / 2] >> e % 2 * 16);
+    }
+  }
+}
+
+// Few rows of a (up to kMt * 16): the rows of b stream past them once.  The waves of a workgroup share the columns, kSteps
+// blocks each, and keep their part of a in registers; a wave's part of 16 * kTn rows of b goes from memory into registers and
+// into the instructions (a's rows as rows, b's as columns).  The waves' sums meet in LDS.  Any alignment.
+template <typename Out, bool kE8, int kMt, int kSteps, int kTn>
+__global__ void __launch_bounds__(1024)
+product_rows_kernel(Side a, Side b, uint32_t K, Out* __restrict__ out, int64_t out_stride, uint32_t waves) {
+  constexpr bool kExact = sizeof(Out) == 4, kInside = kE8 && !kExact;
+  constexpr uint32_t kSums = kTn * kMt * 256;               // of a wave
+  // sixteen sums of a row side by side, rows 4 apart (of the wave's four quarters) in other banks
+  const auto place_of_sum = [](uint32_t row, uint32_t c) { return row / 4 * 64 + ((row ^ row / 4) % 4) * 16 + c; };
+  extern __shared__ float shared[];
+  float* const sums[2] = {shared, shared + waves * kSums};
+  float* const row_scales = shared + 2 * waves * kSums;     // [wave][step][kMt * 16]
+  const uint32_t tid = threadIdx.x, lane = tid % kWave, r16 = lane % 16, quarter = lane / 16, threads = waves * kWave;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const uint32_t blocks = (K + kBlock - 1) / kBlock, first = wave * kSteps;
+  const int64_t tiles = (b.rows + 16 * kTn - 1) / (16 * kTn);
+  // a lane's 32 columns of step s: two parts of 16, those of a row 64 apart, so that four lanes take a line
+  const auto column = [&](int s, int h) { return (first + s) * kBlock + h * 64 + quarter * 16; };
+
+  Codes words[kTn][kSteps];
+  uint32_t scale[kTn][kSteps];
+  const bool ragged = (first + kSteps) * kBlock > K;        // some part of this wave's lies beyond K
+  const auto load = [&](int64_t tile) {
+#pragma unroll
+    for (int t = 0; t < kTn; ++t) {
+      const int64_t n = min(tile * (16 * kTn) + t * 16 + r16, b.rows - 1);
+      const uint8_t* row = b.codes + n * b.stride;
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        if (!ragged) {
+          words[t][s].lo = *reinterpret_cast<const u32x4_bytes*>(row + column(s, 0));
+          words[t][s].hi = *reinterpret_cast<const u32x4_bytes*>(row + column(s, 1));
+        } else {
+          words[t][s] = Codes{load_codes(row, column(s, 0), K), load_codes(row, column(s, 1), K)};
+        }
+        scale[t][s] = load_scale<kE8, kE8>(b, n, min(first + s, blocks - 1), blocks);
+      }
+    }
+  };
+  const auto next_of = [&](int64_t tile) { return tile + gridDim.x < tiles ? tile + gridDim.x : tile; };
+  load(blockIdx.x);
+
+  Codes x[kMt][kSteps];
+  uint32_t sx[kMt][kSteps];
+#pragma unroll
+  for (int i = 0; i < kMt; ++i)
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const int64_t m = i * 16 + r16;
+      const uint8_t* row = a.codes + min(m, a.rows - 1) * a.stride;
+      x[i][s] = Codes{load_codes(row, column(s, 0), K), load_codes(row, column(s, 1), K)};
+      sx[i][s] = load_scale<kE8, kInside>(a, m, min(first + s, blocks - 1), blocks);
+      if (!kInside && quarter == 0) row_scales[(wave * kSteps + s) * (kMt * 16) + m] = __uint_as_float(sx[i][s]);
+    }
+  __syncthreads();
+
+  uint32_t turn = 0;
+  for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+#pragma unroll
+    for (int t = 0; t < kTn; ++t) {
+      f32x4 total[kMt] = {};
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        if constexpr (kInside) {
+#pragma unroll
+          for (int i = 0; i < kMt; ++i)
+            total[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(as_operand(x[i][s]), as_operand(words[t][s]), total[i], 0, 0,
+                                                                        0, sx[i][s], 0, scale[t][s]);
+        } else {
+          const float sb = kE8 ? power_of(scale[t][s]) : __uint_as_float(scale[t][s]);
+          Widened wide;
+          if constexpr (kExact) wide = widened(words[t][s]);
+#pragma unroll
+          for (int i = 0; i < kMt; ++i) {
+            f32x4 part = {};
+            if constexpr (kExact) {
+              Codes c = x[i][s];
+              if (kMt * kSteps > 2) asm volatile("" : "+v"(c.lo), "+v"(c.hi));   // widened each time: there is no room to keep them
+              const Widened wx = widened(c);
+#pragma unroll
+              for (int h = 0; h < 4; ++h) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wx.part[h], wide.part[h], part, 0, 0, 0);
+            } else {
+              part = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(as_operand(x[i][s]), as_operand(words[t][s]), part, 0, 0, 0,
+                                                                      0x7F7F7F7F, 0, 0x7F7F7F7F);
+            }
+            const f32x4 sa = *reinterpret_cast<const f32x4*>(&row_scales[(wave * kSteps + s) * (kMt * 16) + i * 16 + quarter * 4]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) total[i][e] = __builtin_fmaf(part[e], sa[e] * sb, total[i][e]);
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kMt; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          sums[turn][wave * kSums + place_of_sum((t * kMt + i) * 16 + quarter * 4 + e, r16)] = total[i][e];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    load(next_of(tile));
+    __builtin_amdgcn_sched_barrier(0);
+    // the waves' reads of these sums are done when they meet here again, one tile later
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    for (uint32_t i = tid; i < kTn * kMt * 256; i += threads) {
+      const uint32_t row = i / 16, c = i % 16;               // row: a tile of 16 rows of b, a row of a
+      const int64_t m = row % (kMt * 16), n = tile * (16 * kTn) + row / (kMt * 16) * 16 + c;
+      if (m >= a.rows || n >= b.rows) continue;
+      float sum = sums[turn][place_of_sum(row, c)];
+      for (uint32_t w = 1; w < waves; ++w) sum += sums[turn][w * kSums + place_of_sum(row, c)];
+      put_logit(out + m * out_stride + n, sum);
+    }
+    turn ^= 1;
+  }
+}
+
+template <typename Out, bool kE8, int kMt, int kSteps, int kTn>
+void launch_rows_of(Side a, Side b, int64_t K, void* out, int64_t out_stride, hipStream_t stream) {
+  const auto waves = static_cast<uint32_t>((blocks_of(K) + kSteps - 1) / kSteps);
+  const int64_t tiles = (b.rows + 16 * kTn - 1) / (16 * kTn);
+  const int64_t resident = 256 * (16 / waves);
+  const uint32_t lds = (2 * waves * kTn * kMt * 256 + waves * kSteps * kMt * 16) * sizeof(float);
+  product_rows_kernel<Out, kE8, kMt, kSteps, kTn><<<static_cast<uint32_t>(tiles < resident ? tiles : resident), waves * kWave, lds, stream>>>(
+      a, b, static_cast<uint32_t>(K), static_cast<Out*>(out), out_stride, waves);
+}
+
+// Aligned codes, any scales and results: tiles whose steps stand in kStages places of LDS, all but one of them on their way.
+// One barrier a step: behind it the step's codes and scales have arrived, and the place of the step before is free.
+template <typename Shape, int kStages>
+struct StreamLds {
+  static constexpr uint32_t kRows = Shape::kRowsA + Shape::kRowsB;
+  static constexpr uint32_t kScalePlaces = (kRows + Shape::kThreadsHere - 1) / Shape::kThreadsHere * Shape::kThreadsHere;
+  static constexpr uint32_t kStage = kRows * kBlock + kScalePlaces * 4;      // bytes
+  static constexpr uint32_t kBytes = kStages * kStage;
+};
+template <typename Out, bool kE8, bool kExact, typename Shape, int kStages>
+__global__ void __launch_bounds__(Shape::kThreadsHere)
+product_stream_kernel(Side a, Side b, uint32_t K, uint32_t blocks_each, Out* __restrict__ out, int64_t out_stride, int64_t out_part,
+                      uint32_t tiles_m, uint32_t tiles_n) {
+  using Lds = StreamLds<Shape, kStages>;
+  constexpr bool kInside = kE8 && !kExact;
+  constexpr int kM = Shape::kM, kN = Shape::kN, kWords = Lds::kScalePlaces / Shape::kThreadsHere;
+  constexpr uint32_t kRowsA = Shape::kRowsA, kRows = Lds::kRows, kFetchRows = Shape::kFetchRows;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t stages[];
+  const uint32_t tid = threadIdx.x, lane = tid % kWave, r16 = lane % 16, quarter = lane / 16;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const TileAt tile = tile_at(blockIdx.x, tiles_m, tiles_n);
+  const int64_t m0 = static_cast<int64_t>(tile.m) * kRowsA, n0 = static_cast<int64_t>(tile.n) * Shape::kRowsB;
+  const uint32_t all_blocks = (K + kBlock - 1) / kBlock, block0 = blockIdx.y * blocks_each;
+  const uint32_t blocks = min(blocks_each, all_blocks - block0);
+  const Buffer from_a = buffer_of(a.codes + m0 * a.stride), from_b = buffer_of(b.codes + n0 * b.stride);
+  const uint32_t last_a = static_cast<uint32_t>(min(a.rows - m0, int64_t{kRowsA}) - 1), last_b = static_cast<uint32_t>(min(b.rows - n0, int64_t{Shape::kRowsB}) - 1);
+  const uint32_t part16 = (tid % 8 ^ (tid / 16 & 7u)) * 16;
+  uint32_t at_a[Shape::kFetchA], at_b[Shape::kFetchB], at_scale[kWords];
+#pragma unroll
+  for (int i = 0; i < Shape::kFetchA; ++i) at_a[i] = min(tid / 8 + i * kFetchRows, last_a) * static_cast<uint32_t>(a.stride) + part16;
+#pragma unroll
+  for (int i = 0; i < Shape::kFetchB; ++i) at_b[i] = min(tid / 8 + i * kFetchRows, last_b) * static_cast<uint32_t>(b.stride) + part16;
+  // scales: whole waves look after rows of one side
+  static_assert(kRowsA % kWave == 0 && Shape::kRowsB % kWave == 0, "a wave's rows are of one side");
+  constexpr uint32_t kSize = kE8 ? 1 : 4;
+  const uint8_t* first_scale[2] = {static_cast<const uint8_t*>(a.scales) + (m0 >> a.row_shift) * all_blocks * kSize,
+                                   static_cast<const uint8_t*>(b.scales) + (n0 >> b.row_shift) * all_blocks * kSize};
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) {
+    const uint32_t r = min(tid + i * Shape::kThreadsHere, kRows - 1);
+    const int64_t row = r < kRowsA ? (min(m0 + r, a.rows - 1) >> a.row_shift) - (m0 >> a.row_shift)
+                                   : (min(n0 + r - kRowsA, b.rows - 1) >> b.row_shift) - (n0 >> b.row_shift);
+    at_scale[i] = static_cast<uint32_t>(row) * all_blocks * kSize;
+  }
+  const uint32_t lds = lds_address(stages);
+  const auto fetch = [&](uint32_t step, uint32_t stage) {
+    const uint32_t block = block0 + step, k = block * kBlock, to = lds + stage * Lds::kStage + wave * 1024;
+    const uint32_t beyond = step < blocks && k + part16 < K ? 0u : 0x80000000u;
+#pragma unroll
+    for (int i = 0; i < Shape::kFetchA; ++i) fetch_to_lds(from_a, at_a[i] | beyond, k, to + i * kFetchRows * kBlock);
+#pragma unroll
+    for (int i = 0; i < Shape::kFetchB; ++i) fetch_to_lds(from_b, at_b[i] | beyond, k, to + (kRowsA + i * kFetchRows) * kBlock);
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      const uint32_t r = wave * kWave + i * Shape::kThreadsHere;
+      fetch_scale_to_lds<kE8>(buffer_of(first_scale[r < kRowsA ? 0 : 1]), at_scale[i], min(block, all_blocks - 1) * kSize,
+                              lds + stage * Lds::kStage + kRows * kBlock + r * 4);
+    }
+  };
+  constexpr int kOfStep = Shape::kFetchA + Shape::kFetchB + kWords;
+  const uint32_t row_a = wave / Shape::kAcross * (kM * 16), row_b = kRowsA + wave % Shape::kAcross * (kN * 16);
+  const uint32_t lo = place_of(r16, quarter * 2) * 16, hi = place_of(r16, quarter * 2 + 1) * 16;   // in any sixteen rows
+  f32x4 total[kM][kN] = {};
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s) fetch(s, s);
+  uint32_t stage = 0;
+  for (uint32_t step = 0; step < blocks; ++step) {
+    arrived<(kStages - 2) * kOfStep>();
+    fetch(step + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
+    const uint8_t* at = stages + stage * Lds::kStage;
+    const auto read = [&](uint32_t row) {
+      return Codes{*reinterpret_cast<const u32x4*>(at + row * kBlock + lo), *reinterpret_cast<const u32x4*>(at + row * kBlock + hi)};
+    };
+    const auto* scales = reinterpret_cast<const uint32_t*>(at + kRows * kBlock);
+    const auto as_scale = [&](uint32_t w) { return kE8 ? power_of(w & 0xFFu) : __uint_as_float(w); };
+    if constexpr (kExact) {
+      Widened y[kN];
+      f32x4 sb[kN];
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        y[j] = widened(read(row_b + j * 16));
+        const u32x4 w = *reinterpret_cast<const u32x4*>(scales + row_b + j * 16 + quarter * 4);
+        sb[j] = f32x4{as_scale(w.x), as_scale(w.y), as_scale(w.z), as_scale(w.w)};
+      }
+#pragma unroll
+      for (int i = 0; i < kM; ++i) {
+        const Widened x = widened(read(row_a + i * 16));
+        const float sa = as_scale(scales[row_a + i * 16 + r16]);
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+          f32x4 part = {};
+#pragma unroll
+          for (int h = 0; h < 4; ++h) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[j].part[h], x.part[h], part, 0, 0, 0);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) total[i][j][e] = __builtin_fmaf(part[e], sa * sb[j][e], total[i][j][e]);
+        }
+      }
+    } else {
+      Codes y[kN];
+      uint32_t sy[kN];
+      f32x4 sb[kN];
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        y[j] = read(row_b + j * 16);
+        if constexpr (kInside) {
+          sy[j] = scales[row_b + j * 16 + r16];
+        } else {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(scales + row_b + j * 16 + quarter * 4);
+          sb[j] = f32x4{as_scale(w.x), as_scale(w.y), as_scale(w.z), as_scale(w.w)};
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kM; ++i) {
+        const Codes x = read(row_a + i * 16);
+        const uint32_t sx = scales[row_a + i * 16 + r16];
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+          if constexpr (kInside) {
+            total[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(as_operand(y[j]), as_operand(x), total[i][j], 0, 0, 0,
+                                                                           sy[j], 0, sx);
+          } else {
+            const f32x4 none = {};
+            const f32x4 part = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(as_operand(y[j]), as_operand(x), none, 0, 0, 0,
+                                                                                0x7F7F7F7F, 0, 0x7F7F7F7F);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) total[i][j][e] = __builtin_fmaf(part[e], as_scale(sx) * sb[j][e], total[i][j][e]);
+          }
+        }
+      }
+    }
+    stage = stage + 1 == kStages ? 0 : stage + 1;
+  }
+  // fetches that nothing waited for end before the workgroup does
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  out += blockIdx.y * out_part;
+#pragma unroll
+  for (int i = 0; i < kM; ++i) {
+    const int64_t m = m0 + row_a + i * 16 + r16;
+    if (m >= a.rows) continue;
+#pragma unroll
+    for (int j = 0; j < kN; ++j) put_four(out + m * out_stride, n0 + row_b - kRowsA + j * 16 + quarter * 4, b.rows, total[i][j]);
+  }
+}
+
+// Sums of the parts of K, in their order.
+template <typename Out>
+__global__ void __launch_bounds__(kThreads)
+product_join_kernel(const float* __restrict__ parts, int64_t M, int64_t N, int64_t pitch, uint32_t count, Out* __restrict__ out,
+                    int64_t out_stride) {
+  const int64_t n = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) * 4;
+  if (n >= N) return;
+  for (int64_t m = blockIdx.y; m < M; m += gridDim.y) {
+    const float* at = parts + m * pitch + n;
+    f32x4 sum = *reinterpret_cast<const f32x4*>(at);
+    for (uint32_t p = 1; p < count; ++p) sum += *reinterpret_cast<const f32x4*>(at + p * M * pitch);
+    put_four(out + m * out_stride, n, N, sum);
+  }
+}
+
+// How a product is computed.
+using Tiles64 = TileShape<4, 1, 1, 8>;      // of a row of tiles only; 128 rows of b
+using Tiles128 = TileShape<4, 4, 2, 2>;
+using Tiles256 = TileShape<8, 4, 2, 4>;
+enum class Form { kRows, k64, k128, k256 };
+struct Plan {
+  Form form;
+  int64_t parts;            // of K
+};
+Plan plan_of(int64_t M, int64_t N, int64_t K) {
+  const int64_t blocks = blocks_of(K);
+  if (M <= 16 && blocks <= 64) return Plan{Form::kRows, 1};
+  const auto tiles = [&](int64_t size) { return (M + size - 1) / size * ((N + size - 1) / size); };
+  // parts of at least `least` blocks where the tiles alone leave compute units idle
+  const auto parts = [&](int64_t count, int64_t least) {
+    const int64_t most = std::min(256 / std::max(count, int64_t{1}), blocks / least);
+    return count >= 200 || most < 2 ? int64_t{1} : most;
+  };
+  if (M <= 64) return Plan{Form::k64, parts((N + 127) / 128, 4)};
+  const int64_t large = tiles(256), of_large = parts(large, 16);
+  if (large * of_large >= 200 && large * 256 * 256 * 4 <= tiles(128) * 128 * 128 * 5) return Plan{Form::k256, of_large};
+  return Plan{Form::k128, parts(tiles(128), 4)};
+}
+int64_t part_pitch(int64_t N) { return (N + 3) / 4 * 4; }
+
+template <typename Out, bool kE8, bool kExact, typename Shape, int kStages>
+void launch_stream(Side a, Side b, int64_t K, int64_t blocks_each, Out* out, int64_t out_stride, int64_t out_part, hipStream_t stream) {
+  const auto tiles_m = static_cast<uint32_t>((a.rows + Shape::kRowsA - 1) / Shape::kRowsA);
+  const auto tiles_n = static_cast<uint32_t>((b.rows + Shape::kRowsB - 1) / Shape::kRowsB);
+  const dim3 grid(tiles_m * tiles_n, static_cast<uint32_t>((blocks_of(K) + blocks_each - 1) / blocks_each));
+  product_stream_kernel<Out, kE8, kExact, Shape, kStages><<<grid, Shape::kThreadsHere, StreamLds<Shape, kStages>::kBytes, stream>>>(
+      a, b, static_cast<uint32_t>(K), static_cast<uint32_t>(blocks_each), out, out_stride, out_part, tiles_m, tiles_n);
+}
+
+// Tiles of one form into `out`, of type Out: the result, or the parts' sums.
+template <typename Out, bool kE8, bool kExact>
+void launch_tiles(Form form, Side a, Side b, int64_t K, int64_t blocks_each, Out* out, int64_t out_stride, int64_t out_part,
+                  hipStream_t stream) {
+  if (form == Form::k64) {
+    launch_stream<Out, kE8, kExact, Tiles64, 3>(a, b, K, blocks_each, out, out_stride, out_part, stream);
+  } else if (form == Form::k128) {
+    if (blocks_of(a.rows) * blocks_of(b.rows) >= 512) launch_stream<Out, kE8, kExact, Tiles128, 2>(a, b, K, blocks_each, out, out_stride, out_part, stream);
+    else launch_stream<Out, kE8, kExact, Tiles128, 3>(a, b, K, blocks_each, out, out_stride, out_part, stream);
+  } else if constexpr (kE8 && !kExact) {
+    const auto tiles_m = static_cast<uint32_t>((a.rows + 255) / 256), tiles_n = static_cast<uint32_t>((b.rows + 255) / 256);
+    const dim3 grid(tiles_m * tiles_n, static_cast<uint32_t>((blocks_of(K) + blocks_each - 1) / blocks_each));
+    product_tiles_kernel<Out, Tiles256><<<grid, Tiles256::kThreadsHere, 0, stream>>>(
+        a, b, static_cast<uint32_t>(K), static_cast<uint32_t>(blocks_each), out, out_stride, out_part, tiles_m, tiles_n);
+  } else {
+    launch_stream<Out, kE8, kExact, Tiles256, 2>(a, b, K, blocks_each, out, out_stride, out_part, stream);
+  }
+}
+
 template <typename Out, bool kE8>
-void launch_product(Side a, Side b, int64_t K, void* out, int64_t out_stride, hipStream_t stream) {
-  const dim3 grid(static_cast<uint32_t>(blocks_of(b.rows)), static_cast<uint32_t>(blocks_of(a.rows)));
-  product_any_kernel<Out, kE8><<<grid, kThreads, 0, stream>>>(a, b, K, static_cast<Out*>(out), out_stride);
+void launch_product(Side a, Side b, int64_t K, void* out_, int64_t out_stride, uint64_t* workspace, hipStream_t stream) {
+  constexpr bool kExact = sizeof(Out) == 4;
+  auto* out = static_cast<Out*>(out_);
+  const Plan plan = plan_of(a.rows, b.rows, K);
+  const int64_t blocks = blocks_of(K);
+  if (plan.form == Form::kRows) {
+    auto* launch = blocks <= 16 ? launch_rows_of<Out, kE8, 1, 1, 2> : blocks <= 32 ? launch_rows_of<Out, kE8, 1, 2, 2> : launch_rows_of<Out, kE8, 1, 4, 1>;
+    launch(a, b, K, out, out_stride, stream);
+    return;
+  }
+  const auto aligned = [&](const Side& s) {
+    return (reinterpret_cast<uintptr_t>(s.codes) | static_cast<uintptr_t>(s.stride) | static_cast<uintptr_t>(K)) % 16 == 0;
+  };
+  if (!aligned(a) || !aligned(b)) {
+    const dim3 grid(static_cast<uint32_t>(blocks_of(b.rows)), static_cast<uint32_t>(blocks_of(a.rows)));
+    product_any_kernel<Out, kE8><<<grid, kThreads, 0, stream>>>(a, b, K, out, out_stride);
+    return;
+  }
+  if (plan.parts == 1) {
+    launch_tiles<Out, kE8, kExact>(plan.form, a, b, K, blocks, out, out_stride, 0, stream);
+    return;
+  }
+  const int64_t blocks_each = ((blocks + plan.parts - 1) / plan.parts + 3) / 4 * 4, parts = (blocks + blocks_each - 1) / blocks_each;
+  const int64_t pitch = part_pitch(b.rows);
+  auto* sums = reinterpret_cast<float*>(workspace);
+  launch_tiles<float, kE8, kExact>(plan.form, a, b, K, blocks_each, sums, pitch, a.rows * pitch, stream);
+  const dim3 grid(static_cast<uint32_t>((b.rows + 4 * kThreads - 1) / (4 * kThreads)),
+                  static_cast<uint32_t>(a.rows < kMaxGridY ? a.rows : kMaxGridY));
+  product_join_kernel<Out><<<grid, kThreads, 0, stream>>>(sums, a.rows, b.rows, pitch, static_cast<uint32_t>(parts), out, out_stride);
 }
 
 }  // namespace
@@ -480,8 +1107,9 @@ sbw_status_t sbw_quantize_fp8(const void* x, sbw_dtype_t dtype, int64_t M, int64
 }
 
 int64_t sbw_matmul_fp8_workspace(int64_t M, int64_t N, int64_t K) {
-  if (M <= 0 || N <= 0 || K <= 0) return 0;
-  return 0;
+  if (M <= 0 || N <= 0 || K <= 0 || M > kMostRows || N > kMostRows || K > kMostStride) return 0;
+  const Plan plan = plan_of(M, N, K);
+  return plan.parts == 1 ? 0 : plan.parts * M * part_pitch(N) / 2;
 }
 
 sbw_status_t sbw_matmul_fp8(const uint8_t* a, int64_t M, int64_t a_stride, const void* a_scales, int64_t a_block_rows,
@@ -507,7 +1135,7 @@ sbw_status_t sbw_matmul_fp8(const uint8_t* a, int64_t M, int64_t a_stride, const
   auto* launch = scale_type == SBW_SCALE_E8M0
                      ? (dtype == SBW_F32 ? launch_product<float, true> : launch_product<uint16_t, true>)
                      : (dtype == SBW_F32 ? launch_product<float, false> : launch_product<uint16_t, false>);
-  launch(left, right, K, out, out_stride, static_cast<hipStream_t>(stream));
+  launch(left, right, K, out, out_stride, workspace, static_cast<hipStream_t>(stream));
   return after_launch();
 }
 

@@ -166,6 +166,46 @@ def test_product(sbw, M, N, K, scales):
         assert (pad[:, 0] == 5).all() and (pad[:, N + 1:] == 5).all()
 
 
+# many tiles, few tiles with long rows (parts of K), columns that end inside a block, blocks not a multiple of four
+LARGE = [(512, 25700, 272), (513, 25601, 400), (1024, 4096, 8208), (300, 300, 8192), (40, 520, 4096), (64, 30000, 1040),
+         (17, 130, 20000), (1000, 1000, 4112), (16, 70, 20000), (129, 40000, 528), (2, 100, 8320)]
+
+
+@pytest.mark.parametrize("scales", ["e8m0", "f32"])
+@pytest.mark.parametrize("M,N,K", LARGE)
+def test_large_products(sbw, M, N, K, scales):
+    rng = np.random.default_rng(M + N + K)
+    rows = np.unique(np.concatenate([[0, M - 1], rng.integers(0, M, 6)]))
+    columns = np.unique(np.concatenate([np.arange(min(N, 300)), np.arange(max(0, N - 300), N), rng.integers(0, N, 400)]))
+    for rows_b, contiguous, dtype in ((1, True, "bf16"), (128, False, "bf16"), (128, False, "f32")):
+        say(f"large product {scales} {M}x{N}x{K} blocks {rows_b} contiguous={contiguous} {dtype}")
+        a, sa, a_, sa_ = matrices(rng, M, K, 1, scales, contiguous)
+        b, sb, b_, sb_ = matrices(rng, N, K, rows_b, scales, contiguous)
+        sb_ = ref.spread(sb_, N, K)[:, ::128]                       # a scale for each row
+        want, tol = ref.product(a_[rows], sa_[rows], b_[columns], sb_[columns], dtype == "bf16")
+        got = sbw.matmul_fp8(a, sa, b, sb, dtype=DTYPES[dtype])
+        assert torch.isfinite(got).all()
+        close(got[torch.from_numpy(rows).cuda()][:, torch.from_numpy(columns).cuda()], want, tol, (M, N, K))
+        workspace = torch.full((sbw.matmul_fp8_workspace_size(M, N, K) + 1,), -1, dtype=torch.int64, device="cuda")
+        again = torch.full((M, N + 8), 7.0, dtype=DTYPES[dtype], device="cuda")
+        sbw.matmul_fp8(a, sa, b, sb, dtype=DTYPES[dtype], out=again[:, 3:3 + N], workspace=workspace)
+        assert torch.equal(again[:, 3:3 + N], got) and workspace[-1] == -1
+        assert (again[:, :3] == 7).all() and (again[:, 3 + N:] == 7).all()
+
+
+def test_every_row_of_a_large_product(sbw):
+    """Codes of one value a row, so that each result is known: no tile or part misses or repeats."""
+    for M, N, K in ((600, 26000, 256), (1024, 4096, 8192), (48, 1000, 4096), (130, 513, 2048)):
+        x = torch.exp2((torch.arange(M, device="cuda") % 5).float())[:, None].expand(M, K).contiguous()
+        w = torch.exp2((torch.arange(N, device="cuda") % 7).float())[:, None].expand(N, K).contiguous()
+        for scales in SCALES.values():
+            a, b = sbw.quantize_fp8(x, scale_dtype=scales), sbw.quantize_fp8(w, scale_dtype=scales)
+            for dtype in DTYPES.values():
+                got = sbw.matmul_fp8(*a, *b, dtype=dtype).float()
+                want = x[:, :1] * w[:, 0] * K
+                assert ((got - want).abs() <= want * 2.0 ** -7).all(), (M, N, K, dtype)
+
+
 @pytest.mark.parametrize("M", [1, 40, 200])
 def test_product_of_nan_codes(sbw, M):
     rng = np.random.default_rng(M)
