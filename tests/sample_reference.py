@@ -1,10 +1,10 @@
 """The plain 64-bit definition of sbw_sample_tokens, on the CPU; the noise is the oracle's, which other tests pin.
 
-The token is exact: scores are two fp32 operations.  Where the sums' own rounding decides whether a logit is kept
-(the kernel's weights are whole numbers of 2^-44 and more, a row's sum of V of them is off by V 2^-44 at most, these here by V 2^-53),
-either answer is right: rows are taken with top_p a little smaller and a little larger.  A log probability is off by
-4 u |y| from its score, a rounding of itself, and the weights' sum, which fp32 holds to `adds` as for log
-probabilities."""
+The token is exact: scores are two fp32 operations.  Where the rounding of sums decides whether a logit is kept either answer
+is right: rows are taken with top_p a little smaller and a little larger.  How little: the kernel's sum of all weights is
+made as that of the log probabilities is, so off by u (adds + 4 E|y|) of itself, and the sums it is compared with are of V
+whole numbers of 2^-30 at most, each off by half of one.  A log probability is off by 4 u |y| from its score, a rounding of
+itself, and the weights' sum."""
 import numpy as np
 
 import oracle
@@ -44,10 +44,14 @@ def sample(row, seed, inv_t, top_k=0, top_p=1.0, min_p=0.0):
     first = ref.order(row)[0]
     if not np.isfinite(row[first]):
         return [(int(first), -np.inf if row[first] == -np.inf else np.nan, 0.0)]
-    with np.errstate(over="ignore", invalid="ignore"):
+    with np.errstate(over="ignore", invalid="ignore"):      # -inf times 0 where a weight is 0
         scores = (row * inv32).astype(np.float32) + noise(row.size, seed)
     answers = []
-    for p in sorted({top_p, top_p * (1 - 2.0 ** -24), min(top_p * (1 + 2.0 ** -24), 1.0)} if 0 < top_p < 1 else {top_p}):
+    y_all = (row.astype(np.float64) - float(row[first])) * inv_t
+    e_all = np.exp(y_all)
+    S = e_all.sum()
+    off = U * (ref.adds(row.size) + 4 * (e_all * np.abs(y_all))[e_all > 0].sum() / S) + row.size * 2.0 ** -31 / S
+    for p in sorted({top_p, top_p * (1 - off), min(top_p * (1 + off), 1.0)} if 0 < top_p < 1 else {top_p}):
         columns, e = kept_columns(row, inv_t, top_k, p, min_p)
         best = scores[columns].max()
         token = int(columns[scores[columns] == best].min())
