@@ -256,6 +256,7 @@ struct SelectionSize {
   static constexpr int kT = kSmall ? 256 : 1024;
   static constexpr uint32_t kList = kSmall ? 1024 : 4096;     // gathered logits
   static constexpr uint32_t kGroups = kSmall ? 512 : 2048;    // listed groups
+  static constexpr int kHeld = 8;                             // groups' keys of a lane of the small size
 };
 // k of the small size.  Us small and large: 16 x 151936 fp32 100 13.4 and 14.9, 256 17.0 and 16.6; 64 x 128256 bf16 100
 // 15.6 and 16.2, 256 20.3 and 17.6.  (Where the blocks do not suffice the large one is ahead sooner: 150 of 1 x 32000,
@@ -742,7 +743,7 @@ __device__ __noinline__ const uint64_t* select_row(const SBW_GLOBAL T* row_, uin
   }
   if (r.taken > Size::kList) {
     const uint32_t count = segments * kThreads;
-    if constexpr (Size::kSmall) r = gather_any<T, kVecs, 8, Size>(row, V, maxima.groups, count, k, s);
+    if constexpr (Size::kSmall) r = gather_any<T, kVecs, Size::kHeld, Size>(row, V, maxima.groups, count, k, s);
     else if (count <= 5 * Size::kT) r = gather_any<T, kVecs, 5, Size>(row, V, maxima.groups, count, k, s);
     else r = gather_any<T, kVecs, 20, Size>(row, V, maxima.groups, count, k, s);
   }

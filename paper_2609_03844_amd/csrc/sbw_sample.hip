@@ -263,16 +263,14 @@ sample_any_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t r
 // workgroups share the wide rows' logits in both steps.
 // ---------------------------------------------------------------------------
 constexpr uint32_t kSmallTop = kSmallMost;      // top-k that a row's first logits in order are gathered for
+// As many keys a lane as a row of 160000 logits has groups: 200 and fewer of 256 x 152064 29 us with 8, 24 so.
+struct SampledSize : SelectionSize<true> {
+  static constexpr int kHeld = 20;
+};
 constexpr uint32_t kBins = 2048;
 constexpr uint32_t kListed = SelectionSize<false>::kList;
 constexpr int kWeightBits = 30;                 // of a weight in the histogram
 
-// A wide row between the steps, in the workspace (cleared by the first one).
-struct WideRow {
-  uint64_t bins[kBins];
-  uint64_t list[kListed];                       // key << 32 | ~column
-  uint32_t listed, unused;
-};
 struct PartBest {
   uint64_t best;                                // score's key << 32 | ~column, of the kept ones of a part
   uint64_t total;                               // their weights
@@ -299,14 +297,22 @@ __device__ __forceinline__ WidePlan wide_plan(const RowFilter& f, uint32_t V, St
   p.least = f.min_p > 0.0f ? float_from(static_cast<double>(r.m) + log(static_cast<double>(f.min_p)) / static_cast<double>(f.inv_t)) : -INFINITY;
   if (p.cut) {
     // logits so far below the largest that all of them together cannot reach what is left out lie behind the end
-    const double left = p.by_count ? 1.0 / (4.0 * V) : fmax((1.0 - static_cast<double>(f.top_p)) * p.S / V * 0.999, 1e-12);
-    p.scale = static_cast<float>(kBins * static_cast<double>(f.inv_t) / (-log(fmin(left, 0.5))));
+    const float left = p.by_count ? 0.25f / static_cast<float>(V)
+                                  : fmaxf((1.0f - f.top_p) * r.S / static_cast<float>(V) * 0.999f, 1e-12f);
+    p.scale = static_cast<float>(kBins) * f.inv_t / -logf(fminf(left, 0.5f));
     p.target = p.by_count ? static_cast<double>(f.top_k)
                           : ceil(static_cast<double>(f.top_p) * p.S * static_cast<double>(1u << kWeightBits));
     if (!(p.scale > 1e-30f) || !(p.scale < 1e30f)) p.slow = true;
   }
   return p;
 }
+// A wide row between the steps, in the workspace (cleared by the first one).
+struct WideRow {
+  WidePlan plan;
+  uint64_t bins[kBins];
+  uint64_t list[kListed];                       // key << 32 | ~column
+  uint32_t listed, unused;
+};
 // The bin of a logit (kBins and more: behind all); larger logits have smaller bins.
 __device__ __forceinline__ uint32_t bin_of(const WidePlan& p, float x) {
   return static_cast<uint32_t>(fminf((p.m - x) * p.scale, 2.0f * kBins));
@@ -359,12 +365,24 @@ sample_pass_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t 
   }
 }
 
+// The plans of wide rows, a wave each (in the steps that go by them it took 2 us of each workgroup).
+__global__ void __launch_bounds__(kThreads)
+sample_plan_kernel(int64_t B, uint32_t V, uint32_t segments, const Stats* __restrict__ parts, Filters filters, WideRow* __restrict__ wide) {
+  const uint32_t count = segments * (kThreads / kWave);
+  const int64_t b = static_cast<int64_t>(blockIdx.x) * (kThreads / kWave) + threadIdx.x / kWave;
+  if (b >= B) return;
+  const RowFilter f = row_filter(filters, b, V);
+  if (is_small(f, V)) return;
+  const WidePlan p = wide_plan(f, V, join_parts(parts + b * count, count, score_factor(f.inv_t)));
+  if (threadIdx.x % kWave == 0) wide[b].plan = p;
+}
+
 // A small top-k: the first logits in order, their weights' sums, the draw among those that are kept; a lane for each.
 template <typename T, int kVecs>
 __global__ void __launch_bounds__(kThreads)
 sample_small_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride, uint32_t segments, Maxima maxima,
                     Filters filters, const uint64_t* __restrict__ seeds, int32_t* __restrict__ tokens, float* __restrict__ logprobs) {
-  using Size = SelectionSize<true>;
+  using Size = SampledSize;
   static_assert(Size::kT == kThreads && kSmallTop == kThreads, "a lane for each of the first logits");
   constexpr int kWaves = kThreads / kWave;
   __shared__ Selection<Size> s;
@@ -435,37 +453,55 @@ sample_small_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t
   }
 }
 
+// The workgroup's groups that a step looks at, side by side; their number.
+__device__ __forceinline__ uint32_t list_groups(bool some, uint16_t* list, uint32_t* counts) {
+  const uint64_t mask = __ballot(some);
+  if (threadIdx.x % kWave == 0) counts[threadIdx.x / kWave] = __popcll(mask);
+  __syncthreads();
+  uint32_t at = __popcll(mask & ((uint64_t{1} << threadIdx.x % kWave) - 1u)), total = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / kWave; ++w) {
+    if (w < static_cast<int>(threadIdx.x / kWave)) at += counts[w];
+    total += counts[w];
+  }
+  if (some) list[at] = static_cast<uint16_t>(threadIdx.x);
+  __syncthreads();
+  return total;
+}
+
 // The histogram of a wide row with top-p or a large top-k.
 template <typename T, int kVecs>
 __global__ void __launch_bounds__(kThreads)
-sample_bins_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride, const Stats* __restrict__ parts,
-                   const uint32_t* __restrict__ groups, Filters filters, WideRow* __restrict__ wide) {
+sample_bins_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride, const uint32_t* __restrict__ groups,
+                   Filters filters, WideRow* __restrict__ wide) {
   constexpr uint32_t kPer = kPerOf<T>;
   __shared__ uint64_t bins[kBins];
-  const uint32_t j0 = blockIdx.x * (kThreads * kVecs) + threadIdx.x, count = gridDim.x * (kThreads / kWave);
+  __shared__ uint16_t listed[kThreads];
+  __shared__ uint32_t counts[kThreads / kWave];
+  const uint32_t j0 = blockIdx.x * (kThreads * kVecs);
   for (int64_t b = blockIdx.y; b < B; b += gridDim.y) {
     const RowFilter f = row_filter(filters, b, V);
     if (is_small(f, V) || (f.top_k >= V && f.top_p >= 1.0f)) continue;
-    const WidePlan p = wide_plan(f, V, join_parts(parts + b * count, count, score_factor(f.inv_t)));
+    const WidePlan p = wide[b].plan;
     if (!p.plain || p.slow) continue;
     const T* row = logits + b * row_stride;
     const bool near = bin_of(p, logit_of_key(groups[(b * gridDim.x + blockIdx.x) * kThreads + threadIdx.x])) < kBins;
+    const uint32_t items = list_groups(near, listed, counts) * kVecs;
+    if (items == 0) continue;
     for (uint32_t i = threadIdx.x; i < kBins; i += kThreads) bins[i] = 0;
     __syncthreads();
-    if (near) {
-      typename VecOf<T>::Value x[kVecs];
+#pragma unroll 2
+    for (uint32_t i = threadIdx.x; i < items; i += kThreads) {
+      const uint32_t j = j0 + listed[i / kVecs] + i % kVecs * kThreads;
+      const auto x = load_any(row, V, j);
 #pragma unroll
-      for (int u = 0; u < kVecs; ++u) x[u] = load_any(row, V, j0 + u * kThreads);
-#pragma unroll
-      for (int u = 0; u < kVecs; ++u)
-#pragma unroll
-        for (uint32_t e = 0; e < kPer; ++e) {
-          const float v = elem(x[u], e);
-          const uint32_t bin = bin_of(p, v);
-          if (bin >= kBins || (j0 + u * kThreads) * kPer + e >= V) continue;
-          const uint32_t w = p.by_count ? 1u : static_cast<uint32_t>(__builtin_fmaf(weight_of(p, v), static_cast<float>(1u << kWeightBits), 0.5f));
-          atomicAdd(reinterpret_cast<unsigned long long*>(&bins[bin]), static_cast<unsigned long long>(w));
-        }
+      for (uint32_t e = 0; e < kPer; ++e) {
+        const float v = elem(x, e);
+        const uint32_t bin = bin_of(p, v);
+        if (bin >= kBins || j * kPer + e >= V) continue;
+        const uint32_t w = p.by_count ? 1u : static_cast<uint32_t>(__builtin_fmaf(weight_of(p, v), static_cast<float>(1u << kWeightBits), 0.5f));
+        atomicAdd(reinterpret_cast<unsigned long long*>(&bins[bin]), static_cast<unsigned long long>(w));
+      }
     }
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < kBins; i += kThreads)
@@ -510,21 +546,31 @@ __device__ __forceinline__ CutBin cut_bin(const uint64_t* bins, double target, u
 }
 
 // The kept logits of a wide row: the largest score of those in front of the bin where the filter ends, their weights' sum,
-// and the list of that bin's.
+// and the list of that bin's.  A kept logit's noise is first bounded from both sides by its draw's bits; only where its
+// upper bound reaches the largest lower one so far, about one of a wave's vector, it is queued and its noise computed.  (All
+// in registers and unrolled, without a queue, the code was as long as 32 logarithms and took 58 us for 64 x 128256.)
+// The bin's logits gather in LDS first: one atomic a workgroup reserves their places (one for each logit: 24 us, so 16).
+constexpr uint32_t kQueued = 1024, kCutListed = 1024;
 template <typename T, int kVecs>
 __global__ void __launch_bounds__(kThreads)
-sample_wide_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride, const Stats* __restrict__ parts,
-                   const uint32_t* __restrict__ groups, Filters filters, const uint64_t* __restrict__ seeds,
+sample_wide_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride, const uint32_t* __restrict__ groups,
+                   Filters filters, const uint64_t* __restrict__ seeds,
                    WideRow* __restrict__ wide, PartBest* __restrict__ bests) {
   constexpr uint32_t kPer = kPerOf<T>;
   constexpr int kWaves = kThreads / kWave;
   __shared__ uint64_t sums[kWaves];
   __shared__ CutBin found;
-  const uint32_t tid = threadIdx.x, j0 = blockIdx.x * (kThreads * kVecs) + tid, count = gridDim.x * kWaves;
+  __shared__ uint16_t listed[kThreads];
+  __shared__ uint32_t counts[kWaves];
+  __shared__ uint32_t queued_column[kWaves][kQueued];
+  __shared__ float queued_logit[kWaves][kQueued];
+  __shared__ uint64_t cut_list[kCutListed];
+  __shared__ uint32_t cut_listed, cut_place;
+  const uint32_t tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, j0 = blockIdx.x * (kThreads * kVecs);
   for (int64_t b = blockIdx.y; b < B; b += gridDim.y) {
     const RowFilter f = row_filter(filters, b, V);
     if (is_small(f, V)) continue;
-    const WidePlan p = wide_plan(f, V, join_parts(parts + b * count, count, score_factor(f.inv_t)));
+    const WidePlan p = wide[b].plan;
     if (!p.plain || p.slow) continue;
     const T* row = logits + b * row_stride;
     const float of_group = logit_of_key(groups[(b * gridDim.x + blockIdx.x) * kThreads + tid]);
@@ -532,67 +578,98 @@ sample_wide_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t 
     // whatever stands this far below the largest cannot be drawn: the noise lies in (-2.82, 16.64)
     const float highest = p.m * f.inv_t, lowest = __builtin_fmaf(-fabsf(highest), 9.5367431640625e-7f, highest - 20.0f);
     const auto wanted = [&](float x) { return (!p.cut || bin_of(p, x) <= cut.bin) && x >= p.least; };
+    const bool summed = p.cut || p.least > -INFINITY;     // else the sum of all is known
     const Key seed = key_of(seeds[b]);
     uint64_t best = 0, total = 0;
-    const bool some = cut.bin < kBins && wanted(of_group);
-    if (__any(some)) {
-      typename VecOf<T>::Value x[kVecs];
-      float upper[kVecs][kPer];
-      float most = -INFINITY;
-#pragma unroll
-      for (int u = 0; u < kVecs; ++u) {
-        const uint32_t j = j0 + u * kThreads;
-        x[u] = some ? load_any(row, V, j) : lowest_vec(typename VecOf<T>::Value{});
+    float most = highest + kGumbelLo;                     // that the best score reaches
+    uint32_t queue = 0;
+    const auto flush = [&] {
+      for (uint32_t i = lane; i < queue; i += kWave) {
+        const uint32_t v = queued_column[wave][i];
+        const Block words = philox_block(v / 4, seed);
+        const uint32_t word = v % 4 == 0 ? words.w0 : v % 4 == 1 ? words.w1 : v % 4 == 2 ? words.w2 : words.w3;
+        best = max(best, static_cast<uint64_t>(order_key(queued_logit[wave][i] * f.inv_t + gumbel_of(word))) << 32 | ~v);
+      }
+      queue = 0;
+    };
+    if (tid == 0) cut_listed = 0;
+    const uint32_t items = list_groups(cut.bin < kBins && wanted(of_group), listed, counts) * kVecs;
+    const auto vector_of = [&](uint32_t i) { return j0 + listed[min(i, items - 1) / kVecs] + min(i, items - 1) % kVecs * kThreads; };
+    if (items > wave * kWave) {
+      uint32_t j = vector_of(tid);
+      auto next = load_any(row, V, j);
+#pragma unroll 1
+      for (uint32_t i0 = wave * kWave; i0 < items; i0 += kThreads) {
+        const uint32_t i = i0 + lane, of_next = vector_of(i + kThreads);
+        auto x = next;
+        if (i0 + kThreads < items) next = load_any(row, V, of_next);
+        if (i >= items) x = lowest_vec(typename VecOf<T>::Value{});
 #pragma unroll
         for (uint32_t q = 0; q < kPer / 4; ++q) {
-          bool drawn[4], any = false;
+          float upper[4];
+          bool any = false;
 #pragma unroll
           for (uint32_t e = 0; e < 4; ++e) {
-            const uint32_t at = q * 4 + e, v = j * kPer + at;
-            const float y = elem(x[u], at);
-            bool kept = v < V && wanted(y);
+            const uint32_t v = j * kPer + q * 4 + e;
+            const float y = elem(x, q * 4 + e);
+            bool kept = i < items && v < V && wanted(y);
             if (kept && p.cut && bin_of(p, y) == cut.bin) {
-              const uint32_t n = atomicAdd(&wide[b].listed, 1u);
-              if (n < kListed) wide[b].list[n] = static_cast<uint64_t>(order_key(y)) << 32 | ~v;
+              const uint64_t entry = static_cast<uint64_t>(order_key(y)) << 32 | ~v;
+              const uint32_t n = count_one(cut_listed);
+              if (n < kCutListed) {
+                cut_list[n] = entry;
+              } else {
+                const uint32_t at = atomicAdd(&wide[b].listed, 1u);
+                if (at < kListed) wide[b].list[at] = entry;
+              }
               kept = false;
             }
-            if (kept) total += static_cast<uint64_t>(weight_of(p, y) * 1099511627776.0f);   // 2^40
-            drawn[e] = kept && y * f.inv_t >= lowest;
-            any |= drawn[e];
-            upper[u][at] = -INFINITY;
+            if (summed && kept) total += static_cast<uint64_t>(weight_of(p, y) * 1099511627776.0f);   // 2^40
+            const bool drawn = kept && y * f.inv_t >= lowest;
+            any |= drawn;
+            upper[e] = drawn ? 0.0f : -INFINITY;
           }
           if (!__any(any)) continue;
           const Block words = philox_block(j * (kPer / 4) + q, seed);
           const uint32_t word[4] = {words.w0, words.w1, words.w2, words.w3};
+          float lower = -INFINITY;
 #pragma unroll
           for (uint32_t e = 0; e < 4; ++e) {
-            if (!drawn[e]) continue;
-            // between what bounds the noise from both sides
-            const float y = elem(x[u], q * 4 + e) * f.inv_t;
+            const float y = elem(x, q * 4 + e) * f.inv_t;
             const float above = __builtin_fmaf(-kNoiseBitsScale, noise_bits(word[e]), kNoiseBitsOffset);
-            upper[u][q * 4 + e] = y + above;
-            most = fmaxf(most, y + (above > kNoiseUpperRange ? above - kNoiseGap : kGumbelLo));
+            const bool drawn = upper[e] == 0.0f;
+            upper[e] = drawn ? y + above : -INFINITY;
+            lower = fmaxf(lower, drawn ? y + (above > kNoiseUpperRange ? above - kNoiseGap : kGumbelLo) : -INFINITY);
+          }
+          if (__any(lower > most)) most = fmaxf(most, wave_reduce(lower, -INFINITY, [](float a, float c) { return fmaxf(a, c); }));
+#pragma unroll
+          for (uint32_t e = 0; e < 4; ++e) {
+            const uint64_t can = __ballot(upper[e] >= most);
+            if (can == 0) continue;
+            if (queue + kWave > kQueued) flush();
+            if (upper[e] >= most) {
+              const uint32_t at = queue + __popcll(can & ((uint64_t{1} << lane) - 1u));
+              queued_column[wave][at] = j * kPer + q * 4 + e;
+              queued_logit[wave][at] = elem(x, q * 4 + e);
+            }
+            queue += __popcll(can);
           }
         }
+        j = of_next;
       }
-      most = wave_reduce(most, -INFINITY, [](float a, float c) { return fmaxf(a, c); });
-#pragma unroll
-      for (int u = 0; u < kVecs; ++u)
-#pragma unroll
-        for (uint32_t e = 0; e < kPer; ++e) {
-          const bool can = upper[u][e] >= most && upper[u][e] > -INFINITY;
-          if (!__any(can)) continue;
-          if (can) {
-            const uint32_t v = (j0 + u * kThreads) * kPer + e;
-            const Block words = philox_block(v / 4, seed);
-            const uint32_t word = v % 4 == 0 ? words.w0 : v % 4 == 1 ? words.w1 : v % 4 == 2 ? words.w2 : words.w3;
-            best = max(best, static_cast<uint64_t>(order_key(elem(x[u], e) * f.inv_t + gumbel_of(word))) << 32 | ~v);
-          }
-        }
+      flush();
     }
     best = wave_most64(best);
-    total = wave_sum64(total);
-    if (tid % kWave == 0) bests[(b * gridDim.x + blockIdx.x) * kWaves + tid / kWave] = PartBest{best, total};
+    if (summed) total = wave_sum64(total);
+    if (lane == 0) bests[(b * gridDim.x + blockIdx.x) * kWaves + wave] = PartBest{best, total};
+    __syncthreads();
+    const uint32_t own = min(cut_listed, kCutListed);
+    if (own != 0) {
+      if (tid == 0) cut_place = atomicAdd(&wide[b].listed, own);
+      __syncthreads();
+      for (uint32_t i = tid; i < own; i += kThreads)
+        if (cut_place + i < kListed) wide[b].list[cut_place + i] = cut_list[i];
+    }
     __syncthreads();
   }
 }
@@ -601,9 +678,8 @@ sample_wide_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t 
 template <typename T>
 __global__ void __launch_bounds__(kAnyThreads)
 sample_join_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride, uint32_t segments,
-                   const Stats* __restrict__ parts, Filters filters, const uint64_t* __restrict__ seeds,
-                   const WideRow* __restrict__ wide, const PartBest* __restrict__ bests, int32_t* __restrict__ tokens,
-                   float* __restrict__ logprobs) {
+                   Filters filters, const uint64_t* __restrict__ seeds, const WideRow* __restrict__ wide, const PartBest* __restrict__ bests,
+                   int32_t* __restrict__ tokens, float* __restrict__ logprobs) {
   using Size = SelectionSize<false>;
   static_assert(Size::kT == kAnyThreads, "one workgroup");
   constexpr int kWaves = kAnyThreads / kWave;
@@ -619,7 +695,15 @@ sample_join_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t 
     const RowFilter f = row_filter(filters, b, V);
     if (is_small(f, V)) continue;
     const T* row = logits + b * row_stride;
-    const WidePlan p = wide_plan(f, V, join_parts(parts + b * count, count, score_factor(f.inv_t)));
+    const WidePlan p = wide[b].plan;
+    const bool valid = f.inv_t > 0.0f && !isinf(f.inv_t);
+    if (!valid || p.m == -INFINITY) {          // no parameter, or no logit
+      if (tid == 0) {
+        tokens[b] = valid ? 0 : -1;
+        if (logprobs != nullptr) logprobs[b] = valid ? -INFINITY : __uint_as_float(0x7FC00000u);
+      }
+      continue;
+    }
     bool alone = !p.plain || p.slow;
     CutBin cut{0, 0};
     uint32_t listed = 0;
@@ -741,12 +825,13 @@ void launch_long_rows(const T* logits, int64_t B, uint32_t V, int64_t row_stride
   auto* pass = all_small ? sample_pass_kernel<T, kVecs, false, true>
                : any_small ? sample_pass_kernel<T, kVecs, true, true> : sample_pass_kernel<T, kVecs, true, false>;
   pass<<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, filters, parts, maxima, !all_small && any_cut ? wide : nullptr);
+  if (!all_small) sample_plan_kernel<<<static_cast<uint32_t>((B + 3) / 4), kThreads, 0, stream>>>(B, V, segments, parts, filters, wide);
   if (any_small)
     sample_small_kernel<T, kVecs><<<rows, kThreads, 0, stream>>>(logits, B, V, row_stride, segments, maxima, filters, seeds, tokens, logprobs);
   if (all_small) return;
-  if (any_cut) sample_bins_kernel<T, kVecs><<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, parts, maxima.groups, filters, wide);
-  sample_wide_kernel<T, kVecs><<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, parts, maxima.groups, filters, seeds, wide, bests);
-  sample_join_kernel<T><<<rows, kAnyThreads, 0, stream>>>(logits, B, V, row_stride, segments, parts, filters, seeds, wide, bests, tokens, logprobs);
+  if (any_cut) sample_bins_kernel<T, kVecs><<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, maxima.groups, filters, wide);
+  sample_wide_kernel<T, kVecs><<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, maxima.groups, filters, seeds, wide, bests);
+  sample_join_kernel<T><<<rows, kAnyThreads, 0, stream>>>(logits, B, V, row_stride, segments, filters, seeds, wide, bests, tokens, logprobs);
 }
 
 template <typename T>
