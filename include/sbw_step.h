@@ -203,7 +203,9 @@ sbw_status_t sbw_quantize_fp8(const void *x, sbw_dtype_t dtype, int64_t M, int64
  * the power of two of the largest of its eight neighbours (columns 8 i .. 8 i + 7) on its way into the fp32 sum.
  * The product of two blocks' scales is to lie in fp32's range.  out is rounded once.
  *
- *   a, b         device, [M, a_stride] and [N, b_stride] bytes, K columns of each row read; strides < 2^23.
+ *   a, b         device, [M, a_stride] and [N, b_stride] bytes, K columns of each row; strides < 2^23.  Where both start
+ *                at multiples of 16 with strides that are, bytes that share an aligned 16 with a row's last
+ *                columns are read too, and have no effect.
  *   a_scales, b_scales   device, [ceil(M / a_block_rows), ceil(K / 128)] and [ceil(N / b_block_rows),
  *                ceil(K / 128)], both of scale_type; block_rows 1 or 128.
  *   K            > 0 (else SBW_ERR_INVALID_ARG).  M < 2^23 - 128, N < 2^30 (else SBW_ERR_UNSUPPORTED).

@@ -51,46 +51,84 @@ __device__ __forceinline__ uint32_t finite_size(float x) {
   const uint32_t b = __float_as_uint(x) & 0x7FFFFFFFu;
   return b < 0x7F800000u ? b : 0u;
 }
-__device__ __forceinline__ float scaled_value(float x, float inverse) {
-  return finite_size(x) == 0u && x != 0.0f ? __uint_as_float(0x7FC00000u) : x * inverse;
-}
+// Infinities and NaN become NaN.
 __device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d, float inverse) {
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(scaled_value(a, inverse), scaled_value(b, inverse), 0, false);
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(scaled_value(c, inverse), scaled_value(d, inverse), w, true);
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inverse, b * inverse, 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(c * inverse, d * inverse, w, true);
   return static_cast<uint32_t>(w);
 }
 
-// Eight neighbours of a row; those from `columns` on are 0.
-struct Eight {
-  float x[8];
+// Eight neighbours of a row as they stand in memory; those from `columns` on are 0.  Sizes are magnitudes as integers, which
+// order like them: of bf16 two to a word.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+template <typename T>
+struct Eight;
+template <>
+struct Eight<float> {
+  f32x4 lo, hi;
+  static constexpr int kSizes = 8;       // words of sizes
+  __device__ __forceinline__ float operator[](int e) const { return e < 4 ? lo[e] : hi[e - 4]; }
+  __device__ __forceinline__ uint32_t size(int i) const { return __float_as_uint((*this)[i]) & 0x7FFFFFFFu; }
+  static __device__ __forceinline__ uint32_t larger_size(uint32_t a, uint32_t b) { return max(a, b); }
+  static __device__ __forceinline__ uint32_t bits_of(uint32_t size, int) { return size; }
+  static __device__ __forceinline__ uint32_t largest(uint32_t size) { return size; }
 };
-__device__ __forceinline__ Eight load_eight(const float* p, int64_t columns) {
-  Eight v;
-  if (columns >= 8) {
-    const f32x4 lo = *reinterpret_cast<const f32x4_memory*>(p), hi = *reinterpret_cast<const f32x4_memory*>(p + 4);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v.x[e] = lo[e], v.x[e + 4] = hi[e];
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v.x[e] = e < columns ? p[e] : 0.0f;
+template <>
+struct Eight<uint16_t> {
+  u32x4 w;
+  static constexpr int kSizes = 4;
+  __device__ __forceinline__ float operator[](int e) const { return __uint_as_float(e % 2 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16); }
+  __device__ __forceinline__ uint32_t size(int i) const { return w[i] & 0x7FFF7FFFu; }
+  static __device__ __forceinline__ uint32_t larger_size(uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
   }
+  static __device__ __forceinline__ uint32_t bits_of(uint32_t size, int e) { return e % 2 ? size & 0xFFFF0000u : size << 16; }
+  static __device__ __forceinline__ uint32_t largest(uint32_t size) { return max(size & 0xFFFF0000u, size << 16); }
+};
+__device__ __forceinline__ Eight<float> load_eight(const float* p, int64_t columns) {
+  if (columns >= 8) return Eight<float>{*reinterpret_cast<const f32x4_memory*>(p), *reinterpret_cast<const f32x4_memory*>(p + 4)};
+  Eight<float> v{};
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e < columns) (e < 4 ? v.lo : v.hi)[e % 4] = p[e];
   return v;
 }
-__device__ __forceinline__ Eight load_eight(const uint16_t* p, int64_t columns) {
-  Eight v;
-  if (columns >= 8) {
-    const u32x4 w = *reinterpret_cast<const u32x4_memory*>(p);
+__device__ __forceinline__ Eight<uint16_t> load_eight(const uint16_t* p, int64_t columns) {
+  if (columns >= 8) return Eight<uint16_t>{*reinterpret_cast<const u32x4_memory*>(p)};
+  Eight<uint16_t> v{};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v.x[2 * e] = __uint_as_float(w[e] << 16), v.x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+  for (int e = 0; e < 8; ++e)
+    if (e < columns) v.w[e / 2] |= static_cast<uint32_t>(p[e]) << e % 2 * 16;
+  return v;
+}
+// Bits of the largest magnitude; where that is no number, of the largest finite one.
+template <typename T>
+__device__ __forceinline__ uint32_t largest_size(const Eight<T>& v, bool finite) {
+  uint32_t s = 0;
+  if (finite) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = max(s, finite_size(v[e]));
+    return s;
+  }
+#pragma unroll
+  for (int i = 0; i < Eight<T>::kSizes; ++i) s = Eight<T>::larger_size(s, v.size(i));
+  return Eight<T>::largest(s);
+}
+template <typename T>
+__device__ __forceinline__ void put_eight(uint8_t* to, int64_t columns, const Eight<T>& v, float inverse) {
+  const u32x2 w = {codes_of(v[0], v[1], v[2], v[3], inverse), codes_of(v[4], v[5], v[6], v[7], inverse)};
+  if (columns >= 8) {
+    *reinterpret_cast<u32x2_bytes*>(to) = w;
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v.x[e] = e < columns ? logit_of(p[e]) : 0.0f;
+    for (int e = 0; e < 8; ++e)
+      if (e < columns) to[e] = static_cast<uint8_t>(w[e / 4] >> e % 4 * 8);
   }
-  return v;
 }
 
-// Blocks of one row: sixteen lanes a block, eight values a lane.  `across` (a power of two, at most 16) of a
-// workgroup's sixteen groups of lanes take neighbouring blocks of a row, the others the next rows.
+// Blocks of one row: sixteen lanes a block, eight values a lane, kRowsEach rows on their way together.  `across` (a power of
+// two, at most 16) of a workgroup's sixteen groups of lanes take neighbouring blocks of a row, the others the next rows.
+constexpr int kRowsEach = 4;
 template <typename T, bool kE8>
 __global__ void __launch_bounds__(kThreads)
 quantize_rows_kernel(const T* __restrict__ x, int64_t M, int64_t K, int64_t row_stride, uint32_t across,
@@ -99,23 +137,24 @@ quantize_rows_kernel(const T* __restrict__ x, int64_t M, int64_t K, int64_t row_
   const int64_t block = static_cast<int64_t>(blockIdx.x) * across + group % across;
   const int64_t blocks = (K + kBlock - 1) / kBlock, column = block * kBlock + at;
   if (block >= blocks) return;                    // whole groups of sixteen lanes
-  const int64_t rows = kThreads / 16 / across;    // of a workgroup
-  for (int64_t row = blockIdx.y * rows + group / across; row < M; row += gridDim.y * rows) {
-    const Eight v = load_eight(x + row * row_stride + column, K - column);
-    uint32_t largest = 0;
+  const int64_t rows = kThreads / 16 / across;    // of a workgroup at a time
+  for (int64_t row0 = blockIdx.y * (rows * kRowsEach) + group / across; row0 < M; row0 += gridDim.y * (rows * kRowsEach)) {
+    Eight<T> v[kRowsEach];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) largest = max(largest, finite_size(v.x[e]));
-    const BlockScale s = scale_of<kE8>(row_largest(largest));
-    const u32x2 w = {codes_of(v.x[0], v.x[1], v.x[2], v.x[3], s.inverse), codes_of(v.x[4], v.x[5], v.x[6], v.x[7], s.inverse)};
-    uint8_t* to = codes + row * codes_stride + column;
-    if (column + 8 <= K) {
-      *reinterpret_cast<u32x2_bytes*>(to) = w;
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (column + e < K) to[e] = static_cast<uint8_t>(w[e / 4] >> e % 4 * 8);
+    for (int i = 0; i < kRowsEach; ++i) {
+      const int64_t row = row0 + i * rows;
+      v[i] = load_eight(x + min(row, M - 1) * row_stride + min(column, K - 1), K - column);
     }
-    if (at == 0) put_scale<kE8>(scales, row * blocks + block, s.stored);
+#pragma unroll
+    for (int i = 0; i < kRowsEach; ++i) {
+      const int64_t row = row0 + i * rows;
+      uint32_t largest = row_largest(largest_size(v[i], false));
+      if (__any(largest >= 0x7F800000u)) largest = row_largest(largest_size(v[i], true));
+      const BlockScale s = scale_of<kE8>(largest);
+      if (row >= M) continue;
+      put_eight(codes + row * codes_stride + column, K - column, v[i], s.inverse);
+      if (at == 0) put_scale<kE8>(scales, row * blocks + block, s.stored);
+    }
   }
 }
 
@@ -129,7 +168,7 @@ struct Quantized {
 // Tiles of 128 x 128: blocks of 128 rows, and the transposed orientation.  A lane holds eight neighbouring
 // columns of four neighbouring rows, twice, so that four rows' codes of a column make a word of LDS.
 template <typename T, bool kE8, bool kSquare>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : kSquare ? 4 : 3)
 quantize_tiles_kernel(const T* __restrict__ x, int64_t M, int64_t K, int64_t row_stride, Quantized straight,
                       Quantized transposed) {
   constexpr uint32_t kStride = 33;                // words of a column in LDS: lanes 8 columns apart meet in pairs of banks
@@ -141,24 +180,34 @@ quantize_tiles_kernel(const T* __restrict__ x, int64_t M, int64_t K, int64_t row
   const auto row_of = [&](int i) { return static_cast<int64_t>(group * 4 + i / 4 * 64 + i % 4); };
   for (int64_t row_block = blockIdx.y; row_block < row_blocks; row_block += gridDim.y) {
     const int64_t row0 = row_block * kBlock;
-    Eight v[8];
+    Eight<T> v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int64_t row = row0 + row_of(i);
       v[i] = load_eight(x + (row < M ? row : M - 1) * row_stride + min(column, K - 1), row < M ? K - column : 0);
     }
+    // the largest of each of a lane's columns, and of all
+    uint32_t of_columns[Eight<T>::kSizes], of_lane = 0;
+#pragma unroll
+    for (int j = 0; j < Eight<T>::kSizes; ++j) {
+      of_columns[j] = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) of_columns[j] = Eight<T>::larger_size(of_columns[j], v[i].size(j));
+      of_lane = Eight<T>::larger_size(of_lane, of_columns[j]);
+    }
+    of_lane = Eight<T>::largest(of_lane);
+    const bool odd = __syncthreads_or(of_lane >= 0x7F800000u);     // some value is no number
     BlockScale square;
     if (kSquare) {
-      uint32_t largest = 0;
+      if (odd) {
+        of_lane = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) largest = max(largest, finite_size(v[i].x[e]));
-      largest = wave_highest(largest);
-      if (threadIdx.x % kWave == 0) largest_of[wave][0] = largest;
+        for (int i = 0; i < 8; ++i) of_lane = max(of_lane, largest_size(v[i], true));
+      }
+      of_lane = wave_highest(of_lane);
+      if (threadIdx.x % kWave == 0) largest_of[wave][0] = of_lane;
       __syncthreads();
-      largest = max(max(largest_of[0][0], largest_of[1][0]), max(largest_of[2][0], largest_of[3][0]));
-      square = scale_of<kE8>(largest);
+      square = scale_of<kE8>(max(max(largest_of[0][0], largest_of[1][0]), max(largest_of[2][0], largest_of[3][0])));
       if (threadIdx.x == 0) {
         if (straight.codes != nullptr) put_scale<kE8>(straight.scales, row_block * column_blocks + blockIdx.x, square.stored);
         if (transposed.codes != nullptr) put_scale<kE8>(transposed.scales, blockIdx.x * row_blocks + row_block, square.stored);
@@ -169,23 +218,9 @@ quantize_tiles_kernel(const T* __restrict__ x, int64_t M, int64_t K, int64_t row
       for (int i = 0; i < 8; ++i) {
         const int64_t row = row0 + row_of(i);
         BlockScale s = square;
-        if (!kSquare) {
-          uint32_t largest = 0;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) largest = max(largest, finite_size(v[i].x[e]));
-          s = scale_of<kE8>(row_largest(largest));
-        }
+        if (!kSquare) s = scale_of<kE8>(row_largest(largest_size(v[i], odd)));
         if (row >= M || column >= K) continue;
-        const u32x2 w = {codes_of(v[i].x[0], v[i].x[1], v[i].x[2], v[i].x[3], s.inverse),
-                         codes_of(v[i].x[4], v[i].x[5], v[i].x[6], v[i].x[7], s.inverse)};
-        uint8_t* to = straight.codes + row * straight.stride + column;
-        if (column + 8 <= K) {
-          *reinterpret_cast<u32x2_bytes*>(to) = w;
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (column + e < K) to[e] = static_cast<uint8_t>(w[e / 4] >> e % 4 * 8);
-        }
+        put_eight(straight.codes + row * straight.stride + column, K - column, v[i], s.inverse);
         if (!kSquare && lane16 == 0) put_scale<kE8>(straight.scales, row * column_blocks + blockIdx.x, s.stored);
       }
     }
@@ -193,15 +228,17 @@ quantize_tiles_kernel(const T* __restrict__ x, int64_t M, int64_t K, int64_t row
       float inverse[8];
       if (!kSquare) {
         // a column's largest: a lane's eight rows, the wave's four groups of lanes, the four waves
-        uint32_t largest[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          largest[e] = 0;
+          uint32_t largest = Eight<T>::bits_of(of_columns[e * Eight<T>::kSizes / 8], e);
+          if (odd) {
+            largest = 0;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) largest[e] = max(largest[e], finite_size(v[i].x[e]));
-          largest[e] = max(largest[e], __shfl_xor(largest[e], 16));
-          largest[e] = max(largest[e], __shfl_xor(largest[e], 32));
-          if (threadIdx.x % kWave < 16) largest_of[wave][lane16 * 8 + e] = largest[e];
+            for (int i = 0; i < 8; ++i) largest = max(largest, finite_size(v[i][e]));
+          }
+          largest = max(largest, __shfl_xor(largest, 16));
+          largest = max(largest, __shfl_xor(largest, 32));
+          if (threadIdx.x % kWave < 16) largest_of[wave][lane16 * 8 + e] = largest;
         }
         __syncthreads();
 #pragma unroll
@@ -220,7 +257,7 @@ quantize_tiles_kernel(const T* __restrict__ x, int64_t M, int64_t K, int64_t row
 #pragma unroll
         for (int h = 0; h < 2; ++h)
           turned[(lane16 * 8 + e) * kStride + group + h * 16] =
-              codes_of(v[4 * h].x[e], v[4 * h + 1].x[e], v[4 * h + 2].x[e], v[4 * h + 3].x[e], inverse[e]);
+              codes_of(v[4 * h][e], v[4 * h + 1][e], v[4 * h + 2][e], v[4 * h + 3][e], inverse[e]);
       __syncthreads();
 #pragma unroll
       for (int p = 0; p < 4; ++p) {
@@ -240,7 +277,7 @@ quantize_tiles_kernel(const T* __restrict__ x, int64_t M, int64_t K, int64_t row
         }
       }
     }
-    __syncthreads();
+    if (gridDim.y < row_blocks) __syncthreads();
   }
 }
 
@@ -252,7 +289,7 @@ void launch_quantize(const void* x_, int64_t M, int64_t K, int64_t row_stride, b
   if (!square && transposed.codes == nullptr) {
     uint32_t across = 1;
     while (across < 16 && across < blocks) across *= 2;
-    const int64_t rows = 16 / across, groups = (M + rows - 1) / rows;
+    const int64_t rows = 16 / across * kRowsEach, groups = (M + rows - 1) / rows;
     const dim3 grid(static_cast<uint32_t>((blocks + across - 1) / across),
                     static_cast<uint32_t>(groups < kMaxGridY ? groups : kMaxGridY));
     quantize_rows_kernel<T, kE8><<<grid, kThreads, 0, stream>>>(x, M, K, row_stride, across, straight.codes,
@@ -374,13 +411,26 @@ product_any_kernel(Side a, Side b, int64_t K, Out* __restrict__ out, int64_t out
   const int64_t blocks = (K + kBlock - 1) / kBlock;
   u32x4 held[2][4];
   uint32_t held_scale;
-  const auto load = [&](int64_t block) {
+  const uint8_t *row_of_a[4], *row_of_b[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t r = threadIdx.x / 8 + i * 32, c = threadIdx.x % 8;
-      const int64_t k = block * kBlock + c * 16;
-      held[0][i] = load_codes(a.codes + min(m0 + r, a.rows - 1) * a.stride, k, K);
-      held[1][i] = load_codes(b.codes + min(n0 + r, b.rows - 1) * b.stride, k, K);
+  for (int i = 0; i < 4; ++i) {
+    row_of_a[i] = a.codes + min(m0 + threadIdx.x / 8 + i * 32, a.rows - 1) * a.stride;
+    row_of_b[i] = b.codes + min(n0 + threadIdx.x / 8 + i * 32, b.rows - 1) * b.stride;
+  }
+  const auto load = [&](int64_t block) {
+    const int64_t k = block * kBlock + threadIdx.x % 8 * 16;
+    if ((block + 1) * kBlock <= K) {        // of the whole workgroup
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        held[0][i] = *reinterpret_cast<const u32x4_bytes*>(row_of_a[i] + k);
+        held[1][i] = *reinterpret_cast<const u32x4_bytes*>(row_of_b[i] + k);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        held[0][i] = load_codes(row_of_a[i], k, K);
+        held[1][i] = load_codes(row_of_b[i], k, K);
+      }
     }
     held_scale = threadIdx.x < kTile ? load_scale<kE8, kInside>(a, m0 + threadIdx.x, block, blocks)
                                      : load_scale<kE8, kInside>(b, n0 + threadIdx.x - kTile, block, blocks);
@@ -506,6 +556,18 @@ __device__ __forceinline__ void fetch_scale_to_lds(Buffer from, uint32_t at, uin
                  :: "s"(to), "v"(at), "s"(from), "s"(base) : "memory");
   else
     fetch_word_to_lds(from, at, base, to);
+}
+// Columns from K on that share their last 16 bytes with a row's last columns, in LDS: 0 instead of whatever stands there.
+// `rows` rows of a step that holds column K; every lane of the workgroup comes here, behind a barrier and in front of one.
+template <uint32_t kThreadsHere>
+__device__ __forceinline__ void clear_behind(u32x4* step, uint32_t rows, uint32_t K) {
+  const uint32_t c = K % kBlock / 16, kept = K % 16;
+  for (uint32_t r = threadIdx.x; r < rows; r += kThreadsHere) {
+    u32x4 w = step[place_of(r, c)];
+#pragma unroll
+    for (uint32_t d = 0; d < 4; ++d) w[d] &= kept >= d * 4 + 4 ? 0xFFFFFFFFu : kept > d * 4 ? (1u << (kept - d * 4) * 8) - 1u : 0u;
+    step[place_of(r, c)] = w;
+  }
 }
 template <int kNewer>
 __device__ __forceinline__ void arrived() {
@@ -899,6 +961,10 @@ product_stream_kernel(Side a, Side b, uint32_t K, uint32_t blocks_each, Out* __r
   uint32_t stage = 0;
   for (uint32_t step = 0; step < blocks; ++step) {
     arrived<(kStages - 2) * kOfStep>();
+    if (K % 16 != 0 && block0 + step + 1 == all_blocks) {
+      clear_behind<Shape::kThreadsHere>(reinterpret_cast<u32x4*>(stages + stage * Lds::kStage), kRows, K);
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
     fetch(step + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
     const uint8_t* at = stages + stage * Lds::kStage;
     const auto read = [&](uint32_t row) {
@@ -1033,13 +1099,13 @@ void launch_tiles(Form form, Side a, Side b, int64_t K, int64_t blocks_each, Out
   } else if (form == Form::k128) {
     if (blocks_of(a.rows) * blocks_of(b.rows) >= 512) launch_stream<Out, kE8, kExact, Tiles128, 2>(a, b, K, blocks_each, out, out_stride, out_part, stream);
     else launch_stream<Out, kE8, kExact, Tiles128, 3>(a, b, K, blocks_each, out, out_stride, out_part, stream);
+  } else if (!kE8 || kExact || K % 16 != 0) {
+    launch_stream<Out, kE8, kExact, Tiles256, 2>(a, b, K, blocks_each, out, out_stride, out_part, stream);
   } else if constexpr (kE8 && !kExact) {
     const auto tiles_m = static_cast<uint32_t>((a.rows + 255) / 256), tiles_n = static_cast<uint32_t>((b.rows + 255) / 256);
     const dim3 grid(tiles_m * tiles_n, static_cast<uint32_t>((blocks_of(K) + blocks_each - 1) / blocks_each));
     product_tiles_kernel<Out, Tiles256><<<grid, Tiles256::kThreadsHere, 0, stream>>>(
         a, b, static_cast<uint32_t>(K), static_cast<uint32_t>(blocks_each), out, out_stride, out_part, tiles_m, tiles_n);
-  } else {
-    launch_stream<Out, kE8, kExact, Tiles256, 2>(a, b, K, blocks_each, out, out_stride, out_part, stream);
   }
 }
 
@@ -1055,7 +1121,7 @@ void launch_product(Side a, Side b, int64_t K, void* out_, int64_t out_stride, u
     return;
   }
   const auto aligned = [&](const Side& s) {
-    return (reinterpret_cast<uintptr_t>(s.codes) | static_cast<uintptr_t>(s.stride) | static_cast<uintptr_t>(K)) % 16 == 0;
+    return (reinterpret_cast<uintptr_t>(s.codes) | static_cast<uintptr_t>(s.stride)) % 16 == 0;
   };
   if (!aligned(a) || !aligned(b)) {
     const dim3 grid(static_cast<uint32_t>(blocks_of(b.rows)), static_cast<uint32_t>(blocks_of(a.rows)));
