@@ -527,6 +527,159 @@ PyObject* head_logits(PyObject*, PyObject* const* a, Py_ssize_t count) {
   });
 }
 
+// A parameter of every row, or one of all.
+bool of_rows(PyObject* o, at::ScalarType type, const Call& c, const void** each, double* one) {
+  *each = nullptr;
+  *one = 0.0;
+  if (!THPVariable_CheckExact(o)) return number(o, one);
+  const Tensor* t = packed_of(o, type, c.device);
+  if (t == nullptr || t->dim() != 1 || t->size(0) != c.rows || dual(*t)) return false;
+  *each = t->data_ptr();
+  return true;
+}
+
+// sample_tokens(logits, seeds, inv_temperature, top_k, top_p, min_p): tokens and log probabilities
+PyObject* sample_tokens(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  return guarded([&]() -> PyObject* {
+    Call c;
+    const Tensor* none;
+    int64_t n, top_k = 0;
+    const void *inv_ts, *top_ks = nullptr, *top_ps, *min_ps;
+    double inv_t, top_p, min_p, unused;
+    if (count != 6 || !tokens_call(a[0], Py_None, &c, &none, &n) || followed(*c.matrix)) Py_RETURN_NONE;
+    const Tensor* seeds = packed_of(a[1], at::kLong, c.device);
+    if (seeds == nullptr || seeds->dim() != 1 || seeds->size(0) != c.rows || !of_rows(a[2], at::kFloat, c, &inv_ts, &inv_t) ||
+        !(integer(a[3], &top_k) || (THPVariable_CheckExact(a[3]) && of_rows(a[3], at::kInt, c, &top_ks, &unused))) ||
+        !of_rows(a[4], at::kFloat, c, &top_ps, &top_p) || !of_rows(a[5], at::kFloat, c, &min_ps, &min_p))
+      Py_RETURN_NONE;
+    Block block(sbw_sample_tokens_workspace(c.rows, c.columns), 2 * c.rows, c);
+    Tensor tokens = block.take(at::kInt, {c.rows}), logprobs = block.take(at::kFloat, {c.rows});
+    const void* logits = c.matrix->data_ptr();
+    const auto* seed = static_cast<const uint64_t*>(seeds->data_ptr());
+    auto* token = static_cast<int32_t*>(tokens.data_ptr());
+    auto* logprob = static_cast<float*>(logprobs.data_ptr());
+    uint64_t* scratch = block.workspace();
+    void* stream = stream_of(c);
+    PyObject* result = tuple_of(THPVariable_Wrap(tokens), THPVariable_Wrap(logprobs), nullptr);
+    if (result == nullptr) return nullptr;
+    return outputs_or_status(result, unlocked([&] {
+      return sbw_sample_tokens(logits, c.dtype, c.rows, c.columns, c.row_stride, seed, static_cast<const float*>(inv_ts),
+                               static_cast<float>(inv_t), static_cast<const int32_t*>(top_ks), top_k,
+                               static_cast<const float*>(top_ps), static_cast<float>(top_p), static_cast<const float*>(min_ps),
+                               static_cast<float>(min_p), token, logprob, scratch, stream);
+    }));
+  });
+}
+
+// ---- matrices in 8 bits ------------------------------------------------------------------
+
+int64_t blocks_of(int64_t n) { return (n + 127) / 128; }
+
+// quantize_fp8(x, block_rows, whether straight, whether transposed, whether scales are powers of two): codes and scales of
+// both, None where they are not asked for
+PyObject* quantize_fp8(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  return guarded([&]() -> PyObject* {
+    Call c;
+    const Tensor* none;
+    int64_t n, block_rows;
+    if (count != 5 || !tokens_call(a[0], Py_None, &c, &none, &n) || followed(*c.matrix) || !integer(a[1], &block_rows) ||
+        (block_rows != 1 && block_rows != 128) || !PyBool_Check(a[2]) || !PyBool_Check(a[3]) || !PyBool_Check(a[4]))
+      Py_RETURN_NONE;
+    const bool e8m0 = a[4] == Py_True;
+    const auto options = c.matrix->options().requires_grad(false);
+    Tensor codes[2], scales[2];
+    int64_t stride[2] = {0, 0};
+    PyObject* objects[4] = {};
+    for (int i = 0; i < 2; ++i) {
+      if (a[2 + i] != Py_True) continue;
+      const int64_t rows = i == 0 ? c.rows : c.columns, columns = i == 0 ? c.columns : c.rows;
+      stride[i] = blocks_of(columns) * 128;
+      const Tensor whole = at::empty({rows, stride[i]}, options.dtype(at::kFloat8_e4m3fn));
+      if (stride[i] == columns) {
+        codes[i] = whole;
+      } else {
+        auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(whole.storage()), whole.key_set(), whole.dtype());
+        impl->set_sizes_and_strides(at::IntArrayRef({rows, columns}), at::IntArrayRef({stride[i], 1}));
+        codes[i] = Tensor(std::move(impl));
+      }
+      scales[i] = at::empty({(rows + block_rows - 1) / block_rows, blocks_of(columns)},
+                            options.dtype(e8m0 ? at::kFloat8_e8m0fnu : at::kFloat));
+    }
+    const void* x = c.matrix->data_ptr();
+    void* stream = stream_of(c);
+    const auto code_address = [&](int i) { return codes[i].defined() ? static_cast<uint8_t*>(codes[i].data_ptr()) : nullptr; };
+    const auto scale_address = [&](int i) { return scales[i].defined() ? scales[i].data_ptr() : nullptr; };
+    uint8_t *straight = code_address(0), *turned = code_address(1);
+    void *of_straight = scale_address(0), *of_turned = scale_address(1);
+    for (int i = 0; i < 2; ++i)
+      if (codes[i].defined()) {
+        objects[2 * i] = THPVariable_Wrap(codes[i]);
+        objects[2 * i + 1] = THPVariable_Wrap(scales[i]);
+      }
+    PyObject* result = tuple_of(objects);
+    if (result == nullptr) return nullptr;
+    return outputs_or_status(result, unlocked([&] {
+      return sbw_quantize_fp8(x, c.dtype, c.rows, c.columns, c.row_stride, block_rows, e8m0 ? SBW_SCALE_E8M0 : SBW_SCALE_F32,
+                              straight, stride[0], of_straight, turned, stride[1], of_turned, stream);
+    }));
+  });
+}
+
+// A matrix of codes with its scales.
+struct CodedSide {
+  const Tensor* codes;
+  int64_t rows, columns, stride, block_rows;
+  const void* scales;
+};
+bool side_of(PyObject* codes, PyObject* scales, at::ScalarType type, c10::DeviceIndex device, CodedSide* s) {
+  const Tensor* t = tensor_of(codes, device);
+  if (t == nullptr || t->scalar_type() != at::kFloat8_e4m3fn || t->dim() != 2 || t->numel() == 0 || t->stride(1) != 1 ||
+      followed(*t) || dual(*t))
+    return false;
+  s->codes = t;
+  s->rows = t->size(0);
+  s->columns = t->size(1);
+  s->stride = s->rows > 1 ? t->stride(0) : std::max(s->columns, t->stride(0));
+  if (s->stride < s->columns) return false;
+  const Tensor* f = packed_of(scales, type, device);
+  if (f == nullptr || f->dim() != 2 || f->size(1) != blocks_of(s->columns) || followed(*f) || dual(*f)) return false;
+  if (f->size(0) == s->rows) s->block_rows = 1;
+  else if (f->size(0) == blocks_of(s->rows)) s->block_rows = 128;
+  else return false;
+  s->scales = f->data_ptr();
+  return true;
+}
+
+// matmul_fp8(a, a_scales, b, b_scales, whether the product is bfloat16): the product
+PyObject* matmul_fp8(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  return guarded([&]() -> PyObject* {
+    if (count != 5 || !PyBool_Check(a[4]) || !THPVariable_CheckExact(a[1])) Py_RETURN_NONE;
+    const auto device = c10::hip::current_device();
+    const at::ScalarType type = THPVariable_Unpack(a[1]).scalar_type();
+    CodedSide left, right;
+    if ((type != at::kFloat8_e8m0fnu && type != at::kFloat) || !side_of(a[0], a[1], type, device, &left) ||
+        !side_of(a[2], a[3], type, device, &right) || left.columns != right.columns)
+      Py_RETURN_NONE;
+    const bool bf16 = a[4] == Py_True;
+    const auto options = left.codes->options().requires_grad(false);
+    Tensor out = at::empty({left.rows, right.rows}, options.dtype(bf16 ? at::kBFloat16 : at::kFloat)), workspace;
+    const int64_t need = sbw_matmul_fp8_workspace(left.rows, right.rows, left.columns);
+    if (need > 0) workspace = at::empty({need}, options.dtype(at::kLong));
+    const auto* x = static_cast<const uint8_t*>(left.codes->data_ptr());
+    const auto* y = static_cast<const uint8_t*>(right.codes->data_ptr());
+    void* to = out.data_ptr();
+    auto* scratch = need > 0 ? static_cast<uint64_t*>(workspace.data_ptr()) : nullptr;
+    void* stream = c10::hip::getCurrentHIPStream(device).stream();
+    PyObject* result = THPVariable_Wrap(out);
+    if (result == nullptr) return nullptr;
+    return outputs_or_status(result, unlocked([&] {
+      return sbw_matmul_fp8(x, left.rows, left.stride, left.scales, left.block_rows, y, right.rows, right.stride, right.scales,
+                            right.block_rows, left.columns, type == at::kFloat ? SBW_SCALE_F32 : SBW_SCALE_E8M0, to,
+                            bf16 ? SBW_BF16 : SBW_F32, right.rows, scratch, stream);
+    }));
+  });
+}
+
 PyCFunction fast(PyObject* (*f)(PyObject*, PyObject* const*, Py_ssize_t)) {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f));
 }
@@ -540,6 +693,9 @@ PyMethodDef methods[] = {
     {"token_logprobs_grad", fast(token_logprobs_grad), METH_FASTCALL, nullptr},
     {"top_candidates", fast(top_candidates), METH_FASTCALL, nullptr},
     {"head_logits", fast(head_logits), METH_FASTCALL, nullptr},
+    {"sample_tokens", fast(sample_tokens), METH_FASTCALL, nullptr},
+    {"quantize_fp8", fast(quantize_fp8), METH_FASTCALL, nullptr},
+    {"matmul_fp8", fast(matmul_fp8), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods,

@@ -70,6 +70,13 @@ def _new_codes(rows: int, columns: int, device, side) -> torch.Tensor:
 
 def _quantized(x, block_rows, scale_dtype, straight, transposed, stream=None):
     """Both orientations, each a pair (codes, scales) to write, True for a new one, or None."""
+    if stream is None and scale_dtype in _SCALE_TYPES and (straight is None or straight is True) and \
+            (transposed is None or transposed is True):
+        got = _native.quantize_fp8(x, block_rows, straight is True, transposed is True, scale_dtype is torch.float8_e8m0fnu)
+        if type(got) is tuple:
+            return [got[:2] if straight else None, got[2:] if transposed else None]
+        if got is not None:
+            _check(got)
     dtype, M, K, row_stride = _matrix(x, "x")
     kind = _scale_type(scale_dtype)
     block_rows = int(block_rows)
@@ -112,7 +119,7 @@ def quantize_fp8(x: torch.Tensor, block_rows: int = 1, transposed: bool = False,
     NaN become NaN.  Codes that are allocated here have rows padded to whole blocks (a view).  They carry no gradient:
     an x that requires one is refused unless it is off (torch.no_grad())."""
     _no_gradient("the codes of quantize_fp8", x=x)
-    given = (codes, scales)
+    given = (codes, scales) if codes is not None or scales is not None else True
     straight, turned = _quantized(x, block_rows, scale_dtype, None if transposed else given, given if transposed else None,
                                   stream)
     return turned if transposed else straight
@@ -144,6 +151,12 @@ def matmul_fp8(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scale
     dtype (of the product): float32 or bfloat16, rounded once from sums in float32.  The product carries no
     gradient (linear_fp8() does): scales that require one are refused unless it is off.  ``workspace`` is an int64
     scratch tensor of at least matmul_fp8_workspace_size(M, N, K) elements (allocated here when not given)."""
+    if stream is None and out is None and workspace is None and (dtype is torch.float32 or dtype is torch.bfloat16):
+        got = _native.matmul_fp8(a, a_scales, b, b_scales, dtype is torch.bfloat16)
+        if type(got) is torch.Tensor:
+            return got
+        if got is not None:
+            _check(got)
     _no_gradient("the products of matmul_fp8", a=a, a_scales=a_scales, b=b, b_scales=b_scales)
     M, K, a_stride = _codes(a, "a")
     N, b_columns, b_stride = _codes(b, "b")
