@@ -515,7 +515,15 @@ product_any_kernel(Side a, Side b, int64_t K, Out* __restrict__ out, int64_t out
       }
 }
 
-// Aligned codes, powers of two, bf16 results: tiles of 256 x 256 by four waves of 128 x 128.
+// Aligned codes, powers of two, bf16 results, tiles of 256 x 256 by eight waves of 128 x 64.
+//
+// What bounds it: the matrix cores (3.9 PFLOP/s of these instructions alone on random codes, at the clock that the card's
+// power leaves; 32x32x64 reaches 3.2), LDS reads and fetches into LDS share a step of 128 columns: alone they take 1.1, 0.8 and
+// 1.0 us of a compute unit, together 1.65.  8192^3: 439 us, 2.5 PFLOP/s; 1024 x 128256 x 4096: 495 us, 2.2, a share of it the 263 MB of
+// the result; 32000 x 4096 x 1024, of eight steps a tile, 155 us, 1.7.  Measured on the way, 8192^3: 32x32x64 by four waves of
+// 128 x 128 with both steps' fetches waited for at one barrier 571 us; 16x16x128 by eight waves so 527; fetches that
+// the compiler does not wait for in front of reads of LDS, two barriers a step 460; scales as words, shifted each step, instead of
+// bytes read each step 444; the XCDs' starts turned 440 and one wave of a SIMD ahead of the other 439.
 // The workgroup's tile: each XCD takes neighbouring ones, in groups of up to eight rows of tiles.
 struct TileAt {
   uint32_t m, n;
@@ -614,9 +622,12 @@ product_tiles_kernel(Side a, Side b, uint32_t K, uint32_t blocks_each, Out* __re
   for (int i = 0; i < Shape::kFetchA; ++i) at_a[i] = min(tid / 8 + i * kFetchRows, last_a) * static_cast<uint32_t>(a.stride) + part16;
 #pragma unroll
   for (int i = 0; i < Shape::kFetchB; ++i) at_b[i] = min(tid / 8 + i * kFetchRows, last_b) * static_cast<uint32_t>(b.stride) + part16;
+  // the XCDs start at different blocks: rows a power of two apart would all be fetched from the same channels at a time
+  const uint32_t rotation = blocks % 4 == 0 ? blockIdx.x % 8 * (blocks / 32) * 4 : 0;
+  const auto physical = [&](uint32_t block) { return block + rotation >= blocks ? block + rotation - blocks : block + rotation; };
   const uint32_t lds_codes = lds_address(&codes[0][0]) + wave * 1024, lds_scales = lds_address(&tile_scales[0][0]) + wave * 256;
   const auto fetch = [&](uint32_t block, uint32_t turn, bool upper) {
-    const uint32_t k = (block0 + block) * kBlock, beyond = block < blocks && k + part16 < K ? 0u : 0x80000000u, to = lds_codes + turn * (kStage * 16);
+    const uint32_t k = (block0 + physical(block)) * kBlock, beyond = block < blocks && k + part16 < K ? 0u : 0x80000000u, to = lds_codes + turn * (kStage * 16);
 #pragma unroll
     for (int i = 0; i < Shape::kFetchA; ++i)
       if (Shape::upper(i) == upper) fetch_to_lds(from_a, at_a[i] | beyond, k, to + i * kFetchRows * 128);
@@ -639,12 +650,12 @@ product_tiles_kernel(Side a, Side b, uint32_t K, uint32_t blocks_each, Out* __re
       const int64_t row = (min(of_a ? m0 + r : n0 + r - kRowsA, s.rows - 1) >> s.row_shift) - ((of_a ? m0 : n0) >> s.row_shift);
       const uint8_t* first = static_cast<const uint8_t*>(s.scales) + ((of_a ? m0 : n0) >> s.row_shift) * all_blocks;
       if (words) {
-        fetch_word_to_lds(buffer_of(first), static_cast<uint32_t>(row) * all_blocks, min(block0 + block, all_blocks - 4),
+        fetch_word_to_lds(buffer_of(first), static_cast<uint32_t>(row) * all_blocks, min(block0 + physical(block), all_blocks - 4),
                           lds_scales + (turn * kRows + i * kThreadsHere) * 4);
       } else {
         uint32_t w = 0;
 #pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) w |= static_cast<uint32_t>(first[row * all_blocks + min(block0 + block + e, all_blocks - 1)]) << e * 8;
+        for (uint32_t e = 0; e < 4; ++e) w |= static_cast<uint32_t>(first[row * all_blocks + min(block0 + physical(block) + e, all_blocks - 1)]) << e * 8;
         tile_scales[turn][r] = w;
       }
     }
@@ -689,6 +700,7 @@ product_tiles_kernel(Side a, Side b, uint32_t K, uint32_t blocks_each, Out* __re
   read_x(1);
 #pragma unroll
   for (int j = 0; j < kN; ++j) read_y(j);
+  if (wave / 4 != 0) __builtin_amdgcn_s_setprio(1);   // a SIMD's two waves drift apart: one multiplies while the other waits
   for (uint32_t block = 0; block < blocks; ++block) {
 #pragma unroll
     for (int i = 0; i < kM; ++i) {
@@ -938,8 +950,12 @@ product_stream_kernel(Side a, Side b, uint32_t K, uint32_t blocks_each, Out* __r
     at_scale[i] = static_cast<uint32_t>(row) * all_blocks * kSize;
   }
   const uint32_t lds = lds_address(stages);
+  // tiles start at different blocks: at one block, rows a power of two apart come from few channels (64 x 128256 x 4096 with
+  // fp32 scales: 129 us so, 118 with the start turned; with 128 columns to eight waves, 110 with 128 to four)
+  const uint32_t rotation = tile.n % blocks;
   const auto fetch = [&](uint32_t step, uint32_t stage) {
-    const uint32_t block = block0 + step, k = block * kBlock, to = lds + stage * Lds::kStage + wave * 1024;
+    const uint32_t turned = step + rotation, block = block0 + (turned >= blocks ? turned - blocks : turned), k = block * kBlock;
+    const uint32_t to = lds + stage * Lds::kStage + wave * 1024;
     const uint32_t beyond = step < blocks && k + part16 < K ? 0u : 0x80000000u;
 #pragma unroll
     for (int i = 0; i < Shape::kFetchA; ++i) fetch_to_lds(from_a, at_a[i] | beyond, k, to + i * kFetchRows * kBlock);
@@ -961,7 +977,7 @@ product_stream_kernel(Side a, Side b, uint32_t K, uint32_t blocks_each, Out* __r
   uint32_t stage = 0;
   for (uint32_t step = 0; step < blocks; ++step) {
     arrived<(kStages - 2) * kOfStep>();
-    if (K % 16 != 0 && block0 + step + 1 == all_blocks) {
+    if (K % 16 != 0 && block0 + (step + rotation >= blocks ? step + rotation - blocks : step + rotation) + 1 == all_blocks) {
       clear_behind<Shape::kThreadsHere>(reinterpret_cast<u32x4*>(stages + stage * Lds::kStage), kRows, K);
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
@@ -1057,7 +1073,7 @@ product_join_kernel(const float* __restrict__ parts, int64_t M, int64_t N, int64
 }
 
 // How a product is computed.
-using Tiles64 = TileShape<4, 1, 1, 8>;      // of a row of tiles only; 128 rows of b
+using Tiles64 = TileShape<4, 2, 1, 4>;      // of a row of tiles only; 128 rows of b
 using Tiles128 = TileShape<4, 4, 2, 2>;
 using Tiles256 = TileShape<8, 4, 2, 4>;
 enum class Form { kRows, k64, k128, k256 };

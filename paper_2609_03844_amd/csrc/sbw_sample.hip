@@ -273,7 +273,7 @@ constexpr int kWeightBits = 30;                 // of a weight in the histogram
 
 struct PartBest {
   uint64_t best;                                // score's key << 32 | ~column, of the kept ones of a part
-  uint64_t total;                               // their weights
+  double total;                                 // their weights' sum
 };
 
 // How a row is sampled.
@@ -580,7 +580,8 @@ sample_wide_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t 
     const auto wanted = [&](float x) { return (!p.cut || bin_of(p, x) <= cut.bin) && x >= p.least; };
     const bool summed = p.cut || p.least > -INFINITY;     // else the sum of all is known
     const Key seed = key_of(seeds[b]);
-    uint64_t best = 0, total = 0;
+    uint64_t best = 0;
+    float total = 0.0f;                                   // of a lane's logits, in the order of the list
     float most = highest + kGumbelLo;                     // that the best score reaches
     uint32_t queue = 0;
     const auto flush = [&] {
@@ -624,7 +625,7 @@ sample_wide_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t 
               }
               kept = false;
             }
-            if (summed && kept) total += static_cast<uint64_t>(weight_of(p, y) * 1099511627776.0f);   // 2^40
+            if (summed && kept) total += weight_of(p, y);
             const bool drawn = kept && y * f.inv_t >= lowest;
             any |= drawn;
             upper[e] = drawn ? 0.0f : -INFINITY;
@@ -660,8 +661,8 @@ sample_wide_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t 
       flush();
     }
     best = wave_most64(best);
-    if (summed) total = wave_sum64(total);
-    if (lane == 0) bests[(b * gridDim.x + blockIdx.x) * kWaves + wave] = PartBest{best, total};
+    if (summed) total = wave_sum(total);
+    if (lane == 0) bests[(b * gridDim.x + blockIdx.x) * kWaves + wave] = PartBest{best, static_cast<double>(total)};
     __syncthreads();
     const uint32_t own = min(cut_listed, kCutListed);
     if (own != 0) {
@@ -718,7 +719,8 @@ sample_join_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t 
       continue;
     }
     const double inv_t = static_cast<double>(f.inv_t);
-    uint64_t best = 0, whole = 0;
+    uint64_t best = 0;
+    double whole = 0.0;
     for (uint32_t i = tid; i < count; i += kAnyThreads) {
       const PartBest part = bests[b * count + i];
       best = max(best, part.best);
@@ -764,22 +766,21 @@ sample_join_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t 
       }
     }
     best = wave_most64(best);
-    whole = wave_sum64(whole);
+    own += whole;
 #pragma unroll
     for (int d = kWave / 2; d > 0; d /= 2) own += __shfl_xor(own, d);
-    if (tid % kWave == 0) most[wave] = best, sums[wave] = whole, weights[1][wave] = own;
+    if (tid % kWave == 0) most[wave] = best, weights[1][wave] = own;
     __syncthreads();
     if (tid == 0) {
       for (int w = 1; w < kWaves; ++w) {
         best = max(best, most[w]);
-        whole += sums[w];
         own += weights[1][w];
       }
       const uint32_t token = min(~static_cast<uint32_t>(best), V - 1);
       tokens[b] = static_cast<int32_t>(token);
       if (logprobs != nullptr) {
         const bool all = !p.cut && f.min_p <= 0.0f;
-        const double total = all ? p.S : own + static_cast<double>(whole) / 1099511627776.0;
+        const double total = all ? p.S : own;
         logprobs[b] = static_cast<float>((static_cast<double>(logit_of(row[token])) - static_cast<double>(p.m)) * inv_t - log(total));
       }
     }
