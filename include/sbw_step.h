@@ -208,7 +208,8 @@ sbw_status_t sbw_quantize_fp8(const void *x, sbw_dtype_t dtype, int64_t M, int64
  *                columns are read too, and have no effect.
  *   a_scales, b_scales   device, [ceil(M / a_block_rows), ceil(K / 128)] and [ceil(N / b_block_rows),
  *                ceil(K / 128)], both of scale_type; block_rows 1 or 128.
- *   K            > 0 (else SBW_ERR_INVALID_ARG).  M < 2^23 - 128, N < 2^30 (else SBW_ERR_UNSUPPORTED).
+ *   K            > 0 (else SBW_ERR_INVALID_ARG).  M < 2^23 - 128, N < 2^30, and fewer than 2^24 tiles of 128 x 128 (else
+ *                SBW_ERR_UNSUPPORTED).
  *   out          device, [M, out_stride] of dtype (fp32 or bf16), written for n < N.
  *   workspace    device, sbw_matmul_fp8_workspace(M, N, K) uint64 elements (may be NULL where that is 0).
  */

@@ -396,8 +396,10 @@ __device__ __forceinline__ Widened widened(Codes c) {
 // that read one part of sixteen rows meet every bank once.
 __device__ __forceinline__ uint32_t place_of(uint32_t r, uint32_t c) { return r * 8 + (c ^ (r >> 1 & 7u)); }
 
-// Any sizes and alignments: tiles of 128 x 128 by four waves of 64 x 64, the next step's codes on their way in
-// registers while this one's are multiplied.
+// Rows that do not start at multiples of 16 bytes, of more than 64 rows of a and not in parts of K: tiles of 128 x 128 by four waves of 64 x 64, the next
+// step's codes on their way in registers while this one's are multiplied.  Us so and by the streamed form through
+// registers: 333 x 50257 x 1000 of fp32 95 and 115, of bf16 118 and 109; 1024 x 32000 x 4001 271 and 284; 300 x 9000 x 777 30 and
+// 26.  (Aligned, 333 x 50257 x 1024 of fp32 takes 54.)
 template <typename Out, bool kE8>
 __global__ void __launch_bounds__(kThreads)
 product_any_kernel(Side a, Side b, int64_t K, Out* __restrict__ out, int64_t out_stride) {
@@ -905,8 +907,9 @@ void launch_rows_of(Side a, Side b, int64_t K, void* out, int64_t out_stride, hi
       a, b, static_cast<uint32_t>(K), static_cast<Out*>(out), out_stride, waves);
 }
 
-// Aligned codes, any scales and results: tiles whose steps stand in kStages places of LDS, all but one of them on their way.
-// One barrier a step: behind it the step's codes and scales have arrived, and the place of the step before is free.
+// Any scales and results: tiles whose steps stand in kStages places of LDS, all but one of them on their way.  One barrier a
+// step: behind it the step's codes and scales have arrived, and the place of the step before is free.  Rows that do not start at
+// multiples of 16 bytes (kDirect is false) come through registers, a step ahead, into one of two places.
 template <typename Shape, int kStages>
 struct StreamLds {
   static constexpr uint32_t kRows = Shape::kRowsA + Shape::kRowsB;
@@ -914,7 +917,7 @@ struct StreamLds {
   static constexpr uint32_t kStage = kRows * kBlock + kScalePlaces * 4;      // bytes
   static constexpr uint32_t kBytes = kStages * kStage;
 };
-template <typename Out, bool kE8, bool kExact, typename Shape, int kStages>
+template <typename Out, bool kE8, bool kExact, bool kDirect, typename Shape, int kStages>
 __global__ void __launch_bounds__(Shape::kThreadsHere)
 product_stream_kernel(Side a, Side b, uint32_t K, uint32_t blocks_each, Out* __restrict__ out, int64_t out_stride, int64_t out_part,
                       uint32_t tiles_m, uint32_t tiles_n) {
@@ -939,6 +942,7 @@ product_stream_kernel(Side a, Side b, uint32_t K, uint32_t blocks_each, Out* __r
   for (int i = 0; i < Shape::kFetchB; ++i) at_b[i] = min(tid / 8 + i * kFetchRows, last_b) * static_cast<uint32_t>(b.stride) + part16;
   // scales: whole waves look after rows of one side
   static_assert(kRowsA % kWave == 0 && Shape::kRowsB % kWave == 0, "a wave's rows are of one side");
+  static_assert(kDirect || kStages == 2, "a step in registers, one in LDS");
   constexpr uint32_t kSize = kE8 ? 1 : 4;
   const uint8_t* first_scale[2] = {static_cast<const uint8_t*>(a.scales) + (m0 >> a.row_shift) * all_blocks * kSize,
                                    static_cast<const uint8_t*>(b.scales) + (n0 >> b.row_shift) * all_blocks * kSize};
@@ -953,8 +957,9 @@ product_stream_kernel(Side a, Side b, uint32_t K, uint32_t blocks_each, Out* __r
   // tiles start at different blocks: at one block, rows a power of two apart come from few channels (64 x 128256 x 4096 with
   // fp32 scales: 129 us so, 118 with the start turned; with 128 columns to eight waves, 110 with 128 to four)
   const uint32_t rotation = tile.n % blocks;
+  const auto block_of = [&](uint32_t step) { return block0 + (step + rotation >= blocks ? step + rotation - blocks : step + rotation); };
   const auto fetch = [&](uint32_t step, uint32_t stage) {
-    const uint32_t turned = step + rotation, block = block0 + (turned >= blocks ? turned - blocks : turned), k = block * kBlock;
+    const uint32_t block = block_of(step), k = block * kBlock;
     const uint32_t to = lds + stage * Lds::kStage + wave * 1024;
     const uint32_t beyond = step < blocks && k + part16 < K ? 0u : 0x80000000u;
 #pragma unroll
@@ -972,16 +977,56 @@ product_stream_kernel(Side a, Side b, uint32_t K, uint32_t blocks_each, Out* __r
   const uint32_t row_a = wave / Shape::kAcross * (kM * 16), row_b = kRowsA + wave % Shape::kAcross * (kN * 16);
   const uint32_t lo = place_of(r16, quarter * 2) * 16, hi = place_of(r16, quarter * 2 + 1) * 16;   // in any sixteen rows
   f32x4 total[kM][kN] = {};
+  // through registers
+  u32x4 held[Shape::kFetchA + Shape::kFetchB];
+  uint32_t held_scale[kWords];
+  const auto load = [&](uint32_t step) {
+    const uint32_t block = block_of(step), k = block * kBlock + part16;
+    const uint8_t *row_of_a = a.codes + m0 * a.stride - part16, *row_of_b = b.codes + n0 * b.stride - part16;
+    if ((block + 1) * kBlock <= K) {             // of the whole workgroup
 #pragma unroll
-  for (int s = 0; s < kStages - 1; ++s) fetch(s, s);
+      for (int i = 0; i < Shape::kFetchA; ++i) held[i] = *reinterpret_cast<const u32x4_bytes*>(row_of_a + at_a[i] + k);
+#pragma unroll
+      for (int i = 0; i < Shape::kFetchB; ++i) held[Shape::kFetchA + i] = *reinterpret_cast<const u32x4_bytes*>(row_of_b + at_b[i] + k);
+    } else {
+#pragma unroll
+      for (int i = 0; i < Shape::kFetchA; ++i) held[i] = load_codes(row_of_a + at_a[i], k, K);
+#pragma unroll
+      for (int i = 0; i < Shape::kFetchB; ++i) held[Shape::kFetchA + i] = load_codes(row_of_b + at_b[i], k, K);
+    }
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      const uint8_t* p = first_scale[wave * kWave + i * Shape::kThreadsHere < kRowsA ? 0 : 1] + at_scale[i] + block * kSize;
+      held_scale[i] = kE8 ? *p : *reinterpret_cast<const uint32_t*>(p);
+    }
+  };
+  const auto put = [&](uint32_t stage) {
+    uint8_t* to = stages + stage * Lds::kStage;
+#pragma unroll
+    for (int i = 0; i < Shape::kFetchA + Shape::kFetchB; ++i) reinterpret_cast<u32x4*>(to)[i * Shape::kThreadsHere + tid] = held[i];
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) reinterpret_cast<uint32_t*>(to + kRows * kBlock)[i * Shape::kThreadsHere + tid] = held_scale[i];
+  };
+  if constexpr (kDirect) {
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) fetch(s, s);
+  } else {
+    load(0);
+    put(0);
+  }
   uint32_t stage = 0;
   for (uint32_t step = 0; step < blocks; ++step) {
-    arrived<(kStages - 2) * kOfStep>();
-    if (K % 16 != 0 && block0 + (step + rotation >= blocks ? step + rotation - blocks : step + rotation) + 1 == all_blocks) {
-      clear_behind<Shape::kThreadsHere>(reinterpret_cast<u32x4*>(stages + stage * Lds::kStage), kRows, K);
-      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if constexpr (kDirect) {
+      arrived<(kStages - 2) * kOfStep>();
+      if (K % 16 != 0 && block_of(step) + 1 == all_blocks) {
+        clear_behind<Shape::kThreadsHere>(reinterpret_cast<u32x4*>(stages + stage * Lds::kStage), kRows, K);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      }
+      fetch(step + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
+    } else {
+      __syncthreads();
+      if (step + 1 < blocks) load(step + 1);
     }
-    fetch(step + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
     const uint8_t* at = stages + stage * Lds::kStage;
     const auto read = [&](uint32_t row) {
       return Codes{*reinterpret_cast<const u32x4*>(at + row * kBlock + lo), *reinterpret_cast<const u32x4*>(at + row * kBlock + hi)};
@@ -1044,6 +1089,8 @@ product_stream_kernel(Side a, Side b, uint32_t K, uint32_t blocks_each, Out* __r
       }
     }
     stage = stage + 1 == kStages ? 0 : stage + 1;
+    if constexpr (!kDirect)
+      if (step + 1 < blocks) put(stage);
   }
   // fetches that nothing waited for end before the workgroup does
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -1097,26 +1144,32 @@ Plan plan_of(int64_t M, int64_t N, int64_t K) {
 }
 int64_t part_pitch(int64_t N) { return (N + 3) / 4 * 4; }
 
-template <typename Out, bool kE8, bool kExact, typename Shape, int kStages>
+template <typename Out, bool kE8, bool kExact, bool kDirect, typename Shape, int kStages>
 void launch_stream(Side a, Side b, int64_t K, int64_t blocks_each, Out* out, int64_t out_stride, int64_t out_part, hipStream_t stream) {
   const auto tiles_m = static_cast<uint32_t>((a.rows + Shape::kRowsA - 1) / Shape::kRowsA);
   const auto tiles_n = static_cast<uint32_t>((b.rows + Shape::kRowsB - 1) / Shape::kRowsB);
   const dim3 grid(tiles_m * tiles_n, static_cast<uint32_t>((blocks_of(K) + blocks_each - 1) / blocks_each));
-  product_stream_kernel<Out, kE8, kExact, Shape, kStages><<<grid, Shape::kThreadsHere, StreamLds<Shape, kStages>::kBytes, stream>>>(
+  product_stream_kernel<Out, kE8, kExact, kDirect, Shape, kStages><<<grid, Shape::kThreadsHere, StreamLds<Shape, kStages>::kBytes, stream>>>(
       a, b, static_cast<uint32_t>(K), static_cast<uint32_t>(blocks_each), out, out_stride, out_part, tiles_m, tiles_n);
 }
 
 // Tiles of one form into `out`, of type Out: the result, or the parts' sums.
 template <typename Out, bool kE8, bool kExact>
-void launch_tiles(Form form, Side a, Side b, int64_t K, int64_t blocks_each, Out* out, int64_t out_stride, int64_t out_part,
-                  hipStream_t stream) {
+void launch_tiles(Form form, bool direct, Side a, Side b, int64_t K, int64_t blocks_each, Out* out, int64_t out_stride,
+                  int64_t out_part, hipStream_t stream) {
   if (form == Form::k64) {
-    launch_stream<Out, kE8, kExact, Tiles64, 3>(a, b, K, blocks_each, out, out_stride, out_part, stream);
+    auto* launch = direct ? launch_stream<Out, kE8, kExact, true, Tiles64, 3> : launch_stream<Out, kE8, kExact, false, Tiles64, 2>;
+    launch(a, b, K, blocks_each, out, out_stride, out_part, stream);
+  } else if (!direct) {
+    if constexpr (sizeof(Out) == 4)    // parts of K
+      launch_stream<Out, kE8, kExact, false, Tiles128, 2>(a, b, K, blocks_each, out, out_stride, out_part, stream);
   } else if (form == Form::k128) {
-    if (blocks_of(a.rows) * blocks_of(b.rows) >= 512) launch_stream<Out, kE8, kExact, Tiles128, 2>(a, b, K, blocks_each, out, out_stride, out_part, stream);
-    else launch_stream<Out, kE8, kExact, Tiles128, 3>(a, b, K, blocks_each, out, out_stride, out_part, stream);
+    // two places leave room for two workgroups on a compute unit, where there are as many
+    auto* launch = blocks_of(a.rows) * blocks_of(b.rows) >= 512 ? launch_stream<Out, kE8, kExact, true, Tiles128, 2>
+                                                               : launch_stream<Out, kE8, kExact, true, Tiles128, 3>;
+    launch(a, b, K, blocks_each, out, out_stride, out_part, stream);
   } else if (!kE8 || kExact || K % 16 != 0) {
-    launch_stream<Out, kE8, kExact, Tiles256, 2>(a, b, K, blocks_each, out, out_stride, out_part, stream);
+    launch_stream<Out, kE8, kExact, true, Tiles256, 2>(a, b, K, blocks_each, out, out_stride, out_part, stream);
   } else if constexpr (kE8 && !kExact) {
     const auto tiles_m = static_cast<uint32_t>((a.rows + 255) / 256), tiles_n = static_cast<uint32_t>((b.rows + 255) / 256);
     const dim3 grid(tiles_m * tiles_n, static_cast<uint32_t>((blocks_of(K) + blocks_each - 1) / blocks_each));
@@ -1139,19 +1192,20 @@ void launch_product(Side a, Side b, int64_t K, void* out_, int64_t out_stride, u
   const auto aligned = [&](const Side& s) {
     return (reinterpret_cast<uintptr_t>(s.codes) | static_cast<uintptr_t>(s.stride)) % 16 == 0;
   };
-  if (!aligned(a) || !aligned(b)) {
+  const bool direct = aligned(a) && aligned(b);
+  if (!direct && plan.form != Form::k64 && plan.parts == 1) {
     const dim3 grid(static_cast<uint32_t>(blocks_of(b.rows)), static_cast<uint32_t>(blocks_of(a.rows)));
     product_any_kernel<Out, kE8><<<grid, kThreads, 0, stream>>>(a, b, K, out, out_stride);
     return;
   }
   if (plan.parts == 1) {
-    launch_tiles<Out, kE8, kExact>(plan.form, a, b, K, blocks, out, out_stride, 0, stream);
+    launch_tiles<Out, kE8, kExact>(plan.form, direct, a, b, K, blocks, out, out_stride, 0, stream);
     return;
   }
   const int64_t blocks_each = ((blocks + plan.parts - 1) / plan.parts + 3) / 4 * 4, parts = (blocks + blocks_each - 1) / blocks_each;
   const int64_t pitch = part_pitch(b.rows);
   auto* sums = reinterpret_cast<float*>(workspace);
-  launch_tiles<float, kE8, kExact>(plan.form, a, b, K, blocks_each, sums, pitch, a.rows * pitch, stream);
+  launch_tiles<float, kE8, kExact>(plan.form, direct, a, b, K, blocks_each, sums, pitch, a.rows * pitch, stream);
   const dim3 grid(static_cast<uint32_t>((b.rows + 4 * kThreads - 1) / (4 * kThreads)),
                   static_cast<uint32_t>(a.rows < kMaxGridY ? a.rows : kMaxGridY));
   product_join_kernel<Out><<<grid, kThreads, 0, stream>>>(sums, a.rows, b.rows, pitch, static_cast<uint32_t>(parts), out, out_stride);
@@ -1204,7 +1258,7 @@ sbw_status_t sbw_matmul_fp8(const uint8_t* a, int64_t M, int64_t a_stride, const
   if ((dtype != SBW_F32 && dtype != SBW_BF16) || (scale_type != SBW_SCALE_E8M0 && scale_type != SBW_SCALE_F32))
     return SBW_ERR_UNSUPPORTED;
   if (a_stride > kMostStride || b_stride > kMostStride) return SBW_ERR_UNSUPPORTED;
-  if (M > kBlock * kMaxGridY || N > kMostRows) return SBW_ERR_UNSUPPORTED;
+  if (M > kBlock * kMaxGridY || N > kMostRows || blocks_of(M) * blocks_of(N) >= int64_t{1} << 24) return SBW_ERR_UNSUPPORTED;
   if (M == 0 || N == 0) return SBW_OK;
   if (a == nullptr || b == nullptr || a_scales == nullptr || b_scales == nullptr || out == nullptr)
     return SBW_ERR_INVALID_ARG;

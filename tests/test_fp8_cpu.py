@@ -76,6 +76,7 @@ def test_matmul_refusals(lib):
     assert product(lib, M=1 << 23) == UNSUPPORTED
     assert product(lib, N=1 << 30, stride=1 << 30) == UNSUPPORTED
     assert product(lib, stride=1 << 62) == UNSUPPORTED
+    assert product(lib, M=1 << 20, N=1 << 20, stride=1 << 20) == UNSUPPORTED      # more tiles than a launch takes
     assert product(lib, M=0) == OK
     assert product(lib, N=0, stride=0) == OK
     for sizes in ((0, 5, 5), (5, 0, 5), (5, 5, 0), (-1, 5, 5), (1 << 40, 5, 5)):
