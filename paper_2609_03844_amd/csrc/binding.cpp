@@ -16,7 +16,9 @@
 #include <c10/core/TensorImpl.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/autograd/function.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/autograd/variable.h>
 
 #include <algorithm>
 #include <exception>
@@ -684,6 +686,28 @@ PyCFunction fast(PyObject* (*f)(PyObject*, PyObject* const*, Py_ssize_t)) {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f));
 }
 
+// (x, ...): whether the current stream is being captured while a live graph of an eager call accumulates into one of the
+// tensors on the default stream.  A captured backward pass would wait on that stream, which a capture forbids, and torch ends
+// the process for it.
+PyObject* capture_meets_eager(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  const c10::DeviceIndex device = c10::hip::current_device();
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(c10::hip::getCurrentHIPStream(device).stream(), &status) != hipSuccess ||
+      status == hipStreamCaptureStatusNone)
+    Py_RETURN_FALSE;
+  const c10::StreamId eager = c10::hip::getDefaultHIPStream(device).id();
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    if (!THPVariable_Check(a[i])) continue;
+    const Tensor& t = THPVariable_Unpack(a[i]);
+    if (!t.requires_grad() || !t.is_leaf()) continue;
+    const auto node = torch::autograd::impl::try_get_grad_accumulator(t);
+    if (node == nullptr) continue;
+    const auto stream = node->stream();
+    if (stream && stream->id() == eager) Py_RETURN_TRUE;
+  }
+  Py_RETURN_FALSE;
+}
+
 PyMethodDef methods[] = {
     {"watermark", fast(watermark), METH_FASTCALL, nullptr},
     {"watermark_candidates", fast(watermark_candidates), METH_FASTCALL, nullptr},
@@ -696,6 +720,7 @@ PyMethodDef methods[] = {
     {"sample_tokens", fast(sample_tokens), METH_FASTCALL, nullptr},
     {"quantize_fp8", fast(quantize_fp8), METH_FASTCALL, nullptr},
     {"matmul_fp8", fast(matmul_fp8), METH_FASTCALL, nullptr},
+    {"capture_meets_eager", fast(capture_meets_eager), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods,

@@ -402,8 +402,9 @@ def sample_tokens(logits: torch.Tensor, seeds: torch.Tensor, inv_temperature=1.0
     that of ``watermark_sample``, and without filters so is the token (with gamma 0).  A row with a NaN or +inf gives the
     first column of its order with NaN, one of -inf alone column 0 with -inf, and a row whose inv_temperature in a tensor
     is not finite and positive -1 with NaN.  ``workspace`` is an int64 scratch tensor of at least
-    sample_tokens_workspace_size(B, V) elements; what is allocated here may share one storage with it.  The log probabilities carry no gradient (token_logprobs' do): logits
-    that require one are refused unless it is off (torch.no_grad()) or the tokens alone are asked for."""
+    sample_tokens_workspace_size(B, V) elements; what is allocated here may share one storage with it.  The log
+    probabilities carry no gradient (token_logprobs' do): logits that require one are refused unless it is off
+    (torch.no_grad()) or the tokens alone are asked for."""
     if stream is None and tokens is None and logprobs is None and workspace is None and with_logprobs:
         got = _native.sample_tokens(logits, seeds, inv_temperature, top_k, top_p, min_p)
         if type(got) is tuple:

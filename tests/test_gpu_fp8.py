@@ -168,7 +168,8 @@ def test_product(sbw, M, N, K, scales):
 
 # many tiles, few tiles with long rows (parts of K), columns that end inside a block, blocks not a multiple of four
 LARGE = [(512, 25700, 272), (513, 25601, 400), (1024, 4096, 8208), (300, 300, 8192), (40, 520, 4096), (64, 30000, 1040),
-         (17, 130, 20000), (1000, 1000, 4112), (16, 70, 20000), (129, 40000, 528), (2, 100, 8320)]
+         (17, 130, 20000), (1000, 1000, 4112), (16, 70, 20000), (129, 40000, 528), (2, 100, 8320), (60, 3000, 1001),
+         (1024, 600, 2003), (20, 30001, 777), (520, 26000, 200)]
 
 
 @pytest.mark.parametrize("scales", ["e8m0", "f32"])
@@ -381,3 +382,97 @@ def test_repeats_are_equal(sbw):
     for dtype in DTYPES.values():
         first = sbw.matmul_fp8(*a, *b, dtype=dtype)
         assert all(torch.equal(sbw.matmul_fp8(*a, *b, dtype=dtype), first) for _ in range(5))
+
+
+@pytest.mark.parametrize("scales", ["e8m0", "f32"])
+def test_scales_that_are_no_number(sbw, scales):
+    """They reach their rows' results and no others, in every form: also where blocks behind the last one are looked at."""
+    rng = np.random.default_rng(2)
+    for M, N, K in ((3, 140, 300), (40, 140, 1300), (70, 300, 650), (520, 26000, 200)):
+        say(f"nan scales {scales} {M}x{N}x{K}")
+        a, sa, *_ = matrices(rng, M, K, 1, scales, False)
+        b, sb, *_ = matrices(rng, N, K, 1, scales, False)
+        sa[M // 2, -1] = float("nan")
+        sb[N // 3, 0] = float("nan")
+        for dtype in DTYPES.values():
+            got = sbw.matmul_fp8(a, sa, b, sb, dtype=dtype).isnan()
+            want = torch.zeros((M, N), dtype=torch.bool, device="cuda")
+            want[M // 2] = True
+            want[:, N // 3] = True
+            assert torch.equal(got, want)
+
+
+def test_graphs_share_a_workspace(sbw):
+    """Two graphs of products in parts of K with one workspace, replayed in turn on one stream."""
+    g = torch.Generator(device="cuda").manual_seed(4)
+    sizes = ((40, 300, 8192), (200, 300, 4096))
+    pairs = [(sbw.quantize_fp8(torch.randn((M, K), generator=g, device="cuda")),
+              sbw.quantize_fp8(torch.randn((N, K), generator=g, device="cuda"), 128)) for M, N, K in sizes]
+    words = max(sbw.matmul_fp8_workspace_size(*s) for s in sizes)
+    assert min(sbw.matmul_fp8_workspace_size(*s) for s in sizes) > 0
+    workspace = torch.empty(words, dtype=torch.int64, device="cuda")
+    want = [sbw.matmul_fp8(*a, *b) for a, b in pairs]
+    outs, graphs = [torch.empty_like(w) for w in want], []
+    torch.cuda.synchronize()
+    for (a, b), out in zip(pairs, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            sbw.matmul_fp8(*a, *b, out=out, workspace=workspace)
+    for turn in (0, 1, 0, 0, 1, 1):
+        outs[turn].fill_(7.0)
+        graphs[turn].replay()
+        workspace.fill_(-1)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[turn], want[turn])
+
+
+def test_layer_in_a_graph(sbw):
+    """Forward and backward captured together and replayed with new inputs between; refused while an eager result lives."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn((70, 384), generator=g, device="cuda").requires_grad_()
+    w = torch.randn((500, 384), generator=g, device="cuda").requires_grad_()
+    dy = torch.randn((70, 500), generator=g, device="cuda")
+
+    def step():
+        y = sbw.linear_fp8(x, w)
+        return [y.detach(), *torch.autograd.grad(y, (x, w), dy)]
+    eager = sbw.linear_fp8(x, w)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    refused = None
+    marker = torch.zeros(8, device="cuda")
+    with torch.cuda.graph(graph):
+        marker.add_(1.0)                     # a graph of something
+        try:
+            sbw.linear_fp8(x, w)
+        except RuntimeError as error:
+            refused = str(error)
+    assert refused is not None and "eager graph" in refused
+    del eager
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for _ in range(4):
+        with torch.no_grad():
+            x.normal_(generator=g), w.normal_(generator=g)
+        dy.normal_(generator=g)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, step()))
+
+
+def test_layer_on_a_side_stream(sbw):
+    """Its backward pass follows it there."""
+    g = torch.Generator(device="cuda").manual_seed(6)
+    x = torch.randn((70, 384), generator=g, device="cuda").to(torch.bfloat16).requires_grad_()
+    w = torch.randn((500, 384), generator=g, device="cuda").requires_grad_()
+    dy = torch.randn((70, 500), generator=g, device="cuda").to(torch.bfloat16)
+    want = torch.autograd.grad(sbw.linear_fp8(x, w), (x, w), dy)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        y = sbw.linear_fp8(x, w)
+        got = torch.autograd.grad(y, (x, w), dy)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))

@@ -210,6 +210,71 @@ def test_graph_replays(sbw):
             assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+def test_graphs_share_a_workspace(sbw):
+    """Two graphs with one workspace, replayed in turn on one stream."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    inputs = [2 * torch.randn((B, V), generator=g, device="cuda") for B, V in ((5, 30011), (40, 20000))]
+    seeds = [torch.randint(0, 1 << 62, (x.shape[0],), generator=g, device="cuda") for x in inputs]
+    words = max(sbw.sample_tokens_workspace_size(*x.shape) for x in inputs)
+    workspace = torch.empty(words, dtype=torch.int64, device="cuda")
+    want = [sbw.sample_tokens(x, s, top_p=0.9) for x, s in zip(inputs, seeds)]
+    outs = [(torch.empty_like(t), torch.empty_like(lp)) for t, lp in want]
+    graphs = []
+    torch.cuda.synchronize()
+    for x, s, (t, lp) in zip(inputs, seeds, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            sbw.sample_tokens(x, s, top_p=0.9, tokens=t, logprobs=lp, workspace=workspace)
+    for turn in (0, 1, 0, 0, 1, 1):
+        outs[turn][0].fill_(-5), outs[turn][1].fill_(7.0)
+        graphs[turn].replay()
+        workspace.fill_(-1)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[turn][0], want[turn][0]) and torch.equal(outs[turn][1], want[turn][1])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_more_rows_than_take_a_turn(sbw, dtype):
+    """Long rows are sampled 512 at a time: parameters, seeds and results of later turns are their own rows'."""
+    rng = np.random.default_rng(12)
+    B, V = 1100, 4999
+    t, exact = placed(special(rng, B, V), dtype, 1, 3)
+    inv_t, top_k, top_p, min_p = requests(rng, B)
+    seeds, device = new_seeds(rng, B)
+    tokens, logprobs = sbw.sample_tokens(t, device, *(torch.from_numpy(v.astype(d)).cuda() for v, d in
+                                         ((inv_t, np.float32), (top_k, np.int32), (top_p, np.float32), (min_p, np.float32))))
+    tokens, logprobs = tokens.cpu().numpy(), logprobs.double().cpu().numpy()
+    for b in [0, 1, 510, 511, 512, 513, 1022, 1023, 1024, 1025, 1099] + [int(b) for b in rng.permutation(B)[:60]]:
+        answers = ref.sample(exact[b], np.uint64(seeds[b]), inv_t[b], top_k[b], top_p[b], min_p[b])
+        assert any(a == tokens[b] and (np.array_equal(lp, logprobs[b], equal_nan=True) or abs(lp - logprobs[b]) <= tol)
+                   for a, lp, tol in answers), (b, tokens[b], logprobs[b], answers)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [130, 5003])
+def test_scores_beyond_the_type(sbw, V, dtype):
+    """Temperatures so low that scores overflow, so high that they vanish, and the smallest min-p."""
+    rng = np.random.default_rng(V)
+    x = rng.standard_normal((6, V)).astype(np.float32)
+    x[1] = -np.abs(x[1]) - 2
+    x[2] *= 1e-30
+    x[3, 5:] = -np.inf
+    x[4] = np.abs(x[4]) + 2
+    x[5] *= 0.2
+    t, exact = placed(x, dtype)
+    seeds, device = new_seeds(rng, 6)
+    for inv_t in (3.4e38, 2e38, 1e-45, 1e-38):
+        for f in (dict(), dict(top_k=3), dict(top_k=400), dict(top_p=0.5), dict(min_p=0.5), dict(min_p=1e-45)):
+            say(f"sample beyond {dtype} {V} {inv_t} {f}")
+            tokens, logprobs = sbw.sample_tokens(t, device, inv_t, f.get("top_k", 0), f.get("top_p", 1.0), f.get("min_p", 0.0))
+            tokens, logprobs = tokens.cpu().numpy(), logprobs.cpu().numpy()
+            for b in range(6):
+                answers = ref.sample(exact[b], np.uint64(seeds[b]), inv_t, **f)
+                with np.errstate(over="ignore"):       # a log probability below all of fp32
+                    assert any(a == tokens[b] and (np.float32(lp) == logprobs[b] or abs(lp - float(logprobs[b])) <= tol)
+                               for a, lp, tol in answers), (b, tokens[b], logprobs[b], answers)
+
+
 @pytest.mark.parametrize("raw", [False, True])
 def test_another_stream(sbw, raw):
     """On a busy stream while the current one allocates and writes."""
