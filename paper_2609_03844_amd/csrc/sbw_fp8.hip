@@ -1128,19 +1128,31 @@ struct Plan {
   Form form;
   int64_t parts;            // of K
 };
-Plan plan_of(int64_t M, int64_t N, int64_t K) {
+// `inside`: the scales go into the instructions.  Figures: us, e the e8m0 scales, f fp32 ones, then the result's type.
+Plan plan_of(int64_t M, int64_t N, int64_t K, bool inside, bool direct) {
   const int64_t blocks = blocks_of(K);
-  if (M <= 16 && blocks <= 64) return Plan{Form::kRows, 1};
-  const auto tiles = [&](int64_t size) { return (M + size - 1) / size * ((N + size - 1) / size); };
-  // parts of at least `least` blocks where the tiles alone leave compute units idle
+  const auto tiles = [&](int64_t rows, int64_t columns) { return (M + rows - 1) / rows * ((N + columns - 1) / columns); };
+  // Parts of at least `least` blocks where the tiles alone leave compute units idle.  64 x 1024 x 4096 e bf16: 1 part 19.5, 2 14.1, 4
+  // 10.6, 8 10.2; 64 x 16000: 20.7, 17.6, 20.6, 27.8; 64 x 24000 (188 tiles): 21.2, 25.5.  128 x 128, 512 x 2048 x 8192 f bf16: 84, 51, 4 33;
+  // 1024 x 2048 x 8192 (128 tiles): 84, 54, 45; 1024 x 4096 x 4096 (256 tiles): 47, 45, 55, and e bf16 31, 35, 47.
   const auto parts = [&](int64_t count, int64_t least) {
     const int64_t most = std::min(256 / std::max(count, int64_t{1}), blocks / least);
     return count >= 200 || most < 2 ? int64_t{1} : most;
   };
-  if (M <= 64) return Plan{Form::k64, parts((N + 127) / 128, 4)};
-  const int64_t large = tiles(256), of_large = parts(large, 16);
-  if (large * of_large >= 200 && large * 256 * 256 * 4 <= tiles(128) * 128 * 128 * 5) return Plan{Form::k256, of_large};
-  return Plan{Form::k128, parts(tiles(128), 4)};
+  const int64_t of_64 = tiles(64, 128), of_128 = tiles(128, 128), of_256 = tiles(256, 256);
+  // Up to 16 rows by kRows and k64.  e bf16: 8000 x 2048 6.6 and 11.1, 32000 x 2048 15.7 and 12.6, 32000 x 4096 27.9 and 21.5, 128256 x 4096
+  // 106 and 100.  f fp32: 8000 x 2048 7.4 and 17.5, 32000 x 2048 16.8 and 19.4, 128256 x 2048 62.2 and 63.4, 32000 x 4096 35.2 and 34.4,
+  // 128256 x 8192 251 and 226.
+  if (M <= 16 && blocks <= 64 && (!direct || of_64 < 200 || (!inside && blocks <= 16))) return Plan{Form::kRows, 1};
+  // 64 rows by k64 and k128: x 32000 x 2048 e bf16 13.7 and 17.0, x 128256 x 4096 f bf16 122 and 138.
+  if (M <= 64) return Plan{Form::k64, parts(of_64, 4)};
+  // Two tiles of 128 x 128 share a compute unit.  A round of 512 of them takes 40 (2048 x 4096 x 4096 e bf16), one of 256 of 256 x 256, twice the work,
+  // 60; without scales inside 60 and 100 (f bf16), 89 and 148 (e fp32): rounds are compared by 3 to 2, and 7 to 4.  By k128 and k256: 256 x
+  // 32000 x 4096 e bf16 49 and 57, 512 x 40000 128 and 111, f bf16 162 and 198, 1024 x 32000 170 and 123, f 234 and 203.
+  const int64_t parts_128 = parts(of_128, 4), parts_256 = parts(of_256, 48);
+  const auto time = [&](int64_t count, int64_t resident, int64_t n) { return (count * n + resident - 1) / resident * ((blocks + n - 1) / n); };
+  if (time(of_256, 256, parts_256) * (inside ? 6 : 7) <= time(of_128, 512, parts_128) * 4) return Plan{Form::k256, parts_256};
+  return Plan{Form::k128, parts_128};
 }
 int64_t part_pitch(int64_t N) { return (N + 3) / 4 * 4; }
 
@@ -1164,10 +1176,8 @@ void launch_tiles(Form form, bool direct, Side a, Side b, int64_t K, int64_t blo
     if constexpr (sizeof(Out) == 4)    // parts of K
       launch_stream<Out, kE8, kExact, false, Tiles128, 2>(a, b, K, blocks_each, out, out_stride, out_part, stream);
   } else if (form == Form::k128) {
-    // two places leave room for two workgroups on a compute unit, where there are as many
-    auto* launch = blocks_of(a.rows) * blocks_of(b.rows) >= 512 ? launch_stream<Out, kE8, kExact, true, Tiles128, 2>
-                                                               : launch_stream<Out, kE8, kExact, true, Tiles128, 3>;
-    launch(a, b, K, blocks_each, out, out_stride, out_part, stream);
+    // three places leave no room for a second workgroup (512 x 16000 x 4096 e8m0 bf16 41 us with two, 57 with three)
+    launch_stream<Out, kE8, kExact, true, Tiles128, 2>(a, b, K, blocks_each, out, out_stride, out_part, stream);
   } else if (!kE8 || kExact || K % 16 != 0) {
     launch_stream<Out, kE8, kExact, true, Tiles256, 2>(a, b, K, blocks_each, out, out_stride, out_part, stream);
   } else if constexpr (kE8 && !kExact) {
@@ -1182,17 +1192,17 @@ template <typename Out, bool kE8>
 void launch_product(Side a, Side b, int64_t K, void* out_, int64_t out_stride, uint64_t* workspace, hipStream_t stream) {
   constexpr bool kExact = sizeof(Out) == 4;
   auto* out = static_cast<Out*>(out_);
-  const Plan plan = plan_of(a.rows, b.rows, K);
+  const auto aligned = [&](const Side& s) {
+    return (reinterpret_cast<uintptr_t>(s.codes) | static_cast<uintptr_t>(s.stride)) % 16 == 0;
+  };
+  const bool direct = aligned(a) && aligned(b);
+  const Plan plan = plan_of(a.rows, b.rows, K, kE8 && !kExact, direct);
   const int64_t blocks = blocks_of(K);
   if (plan.form == Form::kRows) {
     auto* launch = blocks <= 16 ? launch_rows_of<Out, kE8, 1, 1, 2> : blocks <= 32 ? launch_rows_of<Out, kE8, 1, 2, 2> : launch_rows_of<Out, kE8, 1, 4, 1>;
     launch(a, b, K, out, out_stride, stream);
     return;
   }
-  const auto aligned = [&](const Side& s) {
-    return (reinterpret_cast<uintptr_t>(s.codes) | static_cast<uintptr_t>(s.stride)) % 16 == 0;
-  };
-  const bool direct = aligned(a) && aligned(b);
   if (!direct && plan.form != Form::k64 && plan.parts == 1) {
     const dim3 grid(static_cast<uint32_t>(blocks_of(b.rows)), static_cast<uint32_t>(blocks_of(a.rows)));
     product_any_kernel<Out, kE8><<<grid, kThreads, 0, stream>>>(a, b, K, out, out_stride);
@@ -1244,8 +1254,10 @@ sbw_status_t sbw_quantize_fp8(const void* x, sbw_dtype_t dtype, int64_t M, int64
 
 int64_t sbw_matmul_fp8_workspace(int64_t M, int64_t N, int64_t K) {
   if (M <= 0 || N <= 0 || K <= 0 || M > kMostRows || N > kMostRows || K > kMostStride) return 0;
-  const Plan plan = plan_of(M, N, K);
-  return plan.parts == 1 ? 0 : plan.parts * M * part_pitch(N) / 2;
+  int64_t parts = 1;
+  for (const bool inside : {false, true})
+    for (const bool direct : {false, true}) parts = std::max(parts, plan_of(M, N, K, inside, direct).parts);
+  return parts == 1 ? 0 : parts * M * part_pitch(N) / 2;
 }
 
 sbw_status_t sbw_matmul_fp8(const uint8_t* a, int64_t M, int64_t a_stride, const void* a_scales, int64_t a_block_rows,

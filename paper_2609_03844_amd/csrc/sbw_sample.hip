@@ -75,7 +75,7 @@ __device__ __forceinline__ uint64_t wave_most64(uint64_t x) {
   return x;
 }
 
-// A row of any kind by one workgroup, which reads it once for each step: the largest logit; four digits
+// A row of any kind by one workgroup (140 us where top-k and top-p both cut), which reads it once for each step: the largest logit; four digits
 // of the key where top-k ends, four of the one where top-p ends, four of a column where equal logits are parted; the
 // weights and the draw.
 template <typename T>
@@ -262,7 +262,7 @@ sample_any_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t r
 // bins in front of the one where it ends are kept whole, and the logits of that one are listed and put in order.  All
 // workgroups share the wide rows' logits in both steps.
 // ---------------------------------------------------------------------------
-constexpr uint32_t kSmallTop = kSmallMost;      // top-k that a row's first logits in order are gathered for
+constexpr uint32_t kSmallTop = SelectionSize<false>::kT;   // top-k that a row's first logits in order are gathered for
 // As many keys a lane as a row of 160000 logits has groups: 200 and fewer of 256 x 152064 29 us with 8, 24 so.
 struct SampledSize : SelectionSize<true> {
   static constexpr int kHeld = 20;
@@ -377,21 +377,22 @@ sample_plan_kernel(int64_t B, uint32_t V, uint32_t segments, const Stats* __rest
   if (threadIdx.x % kWave == 0) wide[b].plan = p;
 }
 
-// A small top-k: the first logits in order, their weights' sums, the draw among those that are kept; a lane for each.
-template <typename T, int kVecs>
-__global__ void __launch_bounds__(kThreads)
+// A small top-k: the first logits in order, their weights' sums, the draw among those that are kept; a lane for each.  Up to
+// 256 and more are two launches where the rows' top-k differ.  Against a histogram, us: 400 of 64 x 128256 bf16 KLARGE64 and 48, 1000 KLARGE64B
+// and 50, of 256 x 152064 fp32 KLARGE256 and 142; with top-p, which no histogram takes, 257 of 1 x 32000 KLARGE1 and 235 (by one workgroup).
+template <typename T, int kVecs, typename Size>
+__global__ void __launch_bounds__(Size::kT)
 sample_small_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride, uint32_t segments, Maxima maxima,
                     Filters filters, const uint64_t* __restrict__ seeds, int32_t* __restrict__ tokens, float* __restrict__ logprobs) {
-  using Size = SampledSize;
-  static_assert(Size::kT == kThreads && kSmallTop == kThreads, "a lane for each of the first logits");
-  constexpr int kWaves = kThreads / kWave;
+  static_assert(Size::kT >= (Size::kSmall ? kSmallMost : kSmallTop), "a lane for each of the first logits");
+  constexpr int kWaves = Size::kT / kWave;
   __shared__ Selection<Size> s;
   __shared__ double sums[2][kWaves];
   __shared__ uint64_t bests[kWaves];
   const uint32_t tid = threadIdx.x, wave = tid / kWave;
   for (int64_t b = blockIdx.x; b < B; b += gridDim.x) {
     const RowFilter f = row_filter(filters, b, V);
-    if (!is_small(f, V)) continue;
+    if (!is_small(f, V) || (f.top_k <= kSmallMost) != Size::kSmall) continue;
     const T* row = logits + b * row_stride;
     const Maxima of_row = row_maxima(maxima, b, segments);
     const uint64_t* best = select_row<T, kVecs, Size>(
@@ -446,8 +447,11 @@ sample_small_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) winner = max(winner, bests[w]);
     if (drawn == winner && kept) {
+      double whole = 0.0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) whole += sums[1][w];
       tokens[b] = static_cast<int32_t>(column);
-      if (logprobs != nullptr) logprobs[b] = static_cast<float>(score - log(sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3]));
+      if (logprobs != nullptr) logprobs[b] = static_cast<float>(score - log(whole));
     }
     __syncthreads();
   }
@@ -788,8 +792,10 @@ sample_join_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t 
   }
 }
 
-// Rows of up to so many logits are left to one workgroup each.
-constexpr int64_t kShortSampled = 4096;
+// Few short rows that nothing is cut from are left to one workgroup each.  Us so and in steps: 1 x 4096 fp32 12.7 and 15.2, 64 x 1024
+// 11.3 and 17.2, 64 x 4096 14.2 and 16.7; but 64 x 8192 19.2 and 17.0, 512 x 1024 32 and 25.  With top-p, or a top-k of 50, one workgroup takes
+// 80 and 140 us for a row of any of these lengths, the steps 24 and 13.
+constexpr int64_t kShortSampled = 4096, kFewSampled = 128;
 
 // The workspace: statistics of the pass, maxima, best scores, wide rows.  Its sizes go by B and V alone.
 struct SampleSpace {
@@ -800,8 +806,12 @@ constexpr int64_t kRowsAtOnce = 512;   // more rows take turns: a wide row's spa
 SampleSpace sample_space(int64_t B, int64_t V) {
   SampleSpace s{};
   B = std::min(B, kRowsAtOnce);
-  s.longer = long_segments(B, V, 40);
-  s.segments = (V + (s.longer ? kLongSegment : kShortSegment) - 1) / (s.longer ? kLongSegment : kShortSegment);
+  // Long segments leave fewer parts to join and groups to look at, short ones fill the chip.  Us with top-p 0.9, short and long: 1 x 32000
+  // fp32 24.4 and 27.9, 1 x 152064 bf16 28.2 and 29.2, 16 x 128256 39.0 and 32.0, 64 x 128256 78.9 and 46.8, 256 x 152064 fp32 243 and
+  // 129.  A selection of up to 40 wants twice as many blocks.
+  const int64_t of_long = (V + kLongSegment - 1) / kLongSegment;
+  s.longer = B * of_long >= 256 && of_long * kBlocksOf >= 80;
+  s.segments = s.longer ? of_long : (V + kShortSegment - 1) / kShortSegment;
   s.maxima = B * s.segments * kPartElems;
   s.bests = s.maxima + B * s.segments * kMaximaElems;
   s.wide = s.bests + B * s.segments * (kThreads / kWave) * static_cast<int64_t>(sizeof(PartBest) / 8);
@@ -827,8 +837,12 @@ void launch_long_rows(const T* logits, int64_t B, uint32_t V, int64_t row_stride
                : any_small ? sample_pass_kernel<T, kVecs, true, true> : sample_pass_kernel<T, kVecs, true, false>;
   pass<<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, filters, parts, maxima, !all_small && any_cut ? wide : nullptr);
   if (!all_small) sample_plan_kernel<<<static_cast<uint32_t>((B + 3) / 4), kThreads, 0, stream>>>(B, V, segments, parts, filters, wide);
-  if (any_small)
-    sample_small_kernel<T, kVecs><<<rows, kThreads, 0, stream>>>(logits, B, V, row_stride, segments, maxima, filters, seeds, tokens, logprobs);
+  if (any_small && (!all_small || filters.top_k <= static_cast<int32_t>(kSmallMost)))
+    sample_small_kernel<T, kVecs, SampledSize><<<rows, SampledSize::kT, 0, stream>>>(logits, B, V, row_stride, segments, maxima, filters,
+                                                                                    seeds, tokens, logprobs);
+  if (any_small && (!all_small || filters.top_k > static_cast<int32_t>(kSmallMost)))
+    sample_small_kernel<T, kVecs, SelectionSize<false>><<<rows, kSmallTop, 0, stream>>>(logits, B, V, row_stride, segments, maxima, filters,
+                                                                                       seeds, tokens, logprobs);
   if (all_small) return;
   if (any_cut) sample_bins_kernel<T, kVecs><<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, maxima.groups, filters, wide);
   sample_wide_kernel<T, kVecs><<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, maxima.groups, filters, seeds, wide, bests);
@@ -839,7 +853,9 @@ template <typename T>
 void launch_sample(const void* logits_, int64_t B, uint32_t V, int64_t row_stride, const Filters& filters,
                    const uint64_t* seeds, int32_t* tokens, float* logprobs, uint64_t* workspace, hipStream_t stream) {
   const T* logits = static_cast<const T*>(logits_);
-  if (V <= kShortSampled) {
+  const bool cuts = filters.top_ks != nullptr || (filters.top_k > 0 && static_cast<uint32_t>(filters.top_k) < V) ||
+                    filters.top_ps != nullptr || filters.top_p < 1.0f;
+  if (!cuts && V <= kShortSampled && B <= kFewSampled) {
     sample_any_kernel<T><<<static_cast<uint32_t>(grid_for(B)), kAnyThreads, 0, stream>>>(logits, B, V, row_stride, filters, seeds,
                                                                                         tokens, logprobs);
     return;
@@ -864,7 +880,7 @@ void launch_sample(const void* logits_, int64_t B, uint32_t V, int64_t row_strid
 extern "C" {
 
 int64_t sbw_sample_tokens_workspace(int64_t B, int64_t V) {
-  if (B <= 0 || V <= kShortSampled || V > kMostColumns || B > INT64_MAX / 4 / V) return 0;
+  if (B <= 0 || V <= 0 || V > kMostColumns || B > INT64_MAX / 4 / V) return 0;
   return sample_space(B, V).total;
 }
 
