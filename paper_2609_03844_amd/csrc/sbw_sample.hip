@@ -263,6 +263,7 @@ sample_any_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t r
 // workgroups share the wide rows' logits in both steps.
 // ---------------------------------------------------------------------------
 constexpr uint32_t kSmallTop = SelectionSize<false>::kT;   // top-k that a row's first logits in order are gathered for
+constexpr uint32_t kQuarterTop = 64;            // of them by 256 lanes, the others by 1024 (sample_small_kernel)
 // As many keys a lane as a row of 160000 logits has groups: 200 and fewer of 256 x 152064 29 us with 8, 24 so.
 struct SampledSize : SelectionSize<true> {
   static constexpr int kHeld = 20;
@@ -319,7 +320,7 @@ __device__ __forceinline__ uint32_t bin_of(const WidePlan& p, float x) {
 }
 __device__ __forceinline__ float weight_of(const WidePlan& p, float x) { return __builtin_amdgcn_exp2f((x - p.m) * p.c); }
 
-// The pass.  Workgroups and groups as in row_pass_kernel.
+// The pass.  Workgroups and groups as in row_pass_kernel.  Bound by memory: 256 x 152064 fp32 25 us, 6.1 TB/s.
 template <typename T, int kVecs, bool kStats, bool kTop>
 __global__ void __launch_bounds__(kThreads)
 sample_pass_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride, Filters filters,
@@ -377,14 +378,16 @@ sample_plan_kernel(int64_t B, uint32_t V, uint32_t segments, const Stats* __rest
   if (threadIdx.x % kWave == 0) wide[b].plan = p;
 }
 
-// A small top-k: the first logits in order, their weights' sums, the draw among those that are kept; a lane for each.  Up to
-// 256 and more are two launches where the rows' top-k differ.  Against a histogram, us: 400 of 64 x 128256 bf16 KLARGE64 and 48, 1000 KLARGE64B
-// and 50, of 256 x 152064 fp32 KLARGE256 and 142; with top-p, which no histogram takes, 257 of 1 x 32000 KLARGE1 and 235 (by one workgroup).
+// A small top-k: the first logits in order, their weights' sums, the draw among those that are kept; a lane for each.  Bound by
+// dependent trips to memory, like any selection.  Us of a call with top-p, by 256 lanes and by 1024: 50 of 1 x 32000 fp32 13.3 and 14.2, of
+// 64 x 128256 bf16 16.4 and 17.4; 100 17.1 and 15.9, 21.3 and 19.0; 256 22.7 and 16.4, 29.3 and 20.5.  Where rows differ both are launched.  Up to
+// 1024 lanes' worth beats a histogram: 400 of 64 x 128256 21.6 and 48, 1000 28.5 and 50, of 256 x 152064 fp32 60 and 142; with top-p behind
+// it no histogram serves, and one workgroup a row takes 235 for 1 x 32000, 650 for 64 x 128256.
 template <typename T, int kVecs, typename Size>
 __global__ void __launch_bounds__(Size::kT)
 sample_small_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride, uint32_t segments, Maxima maxima,
                     Filters filters, const uint64_t* __restrict__ seeds, int32_t* __restrict__ tokens, float* __restrict__ logprobs) {
-  static_assert(Size::kT >= (Size::kSmall ? kSmallMost : kSmallTop), "a lane for each of the first logits");
+  static_assert(Size::kT >= (Size::kSmall ? kQuarterTop : kSmallTop), "a lane for each of the first logits");
   constexpr int kWaves = Size::kT / kWave;
   __shared__ Selection<Size> s;
   __shared__ double sums[2][kWaves];
@@ -392,7 +395,7 @@ sample_small_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t
   const uint32_t tid = threadIdx.x, wave = tid / kWave;
   for (int64_t b = blockIdx.x; b < B; b += gridDim.x) {
     const RowFilter f = row_filter(filters, b, V);
-    if (!is_small(f, V) || (f.top_k <= kSmallMost) != Size::kSmall) continue;
+    if (!is_small(f, V) || (f.top_k <= kQuarterTop) != Size::kSmall) continue;
     const T* row = logits + b * row_stride;
     const Maxima of_row = row_maxima(maxima, b, segments);
     const uint64_t* best = select_row<T, kVecs, Size>(
@@ -473,7 +476,8 @@ __device__ __forceinline__ uint32_t list_groups(bool some, uint16_t* list, uint3
   return total;
 }
 
-// The histogram of a wide row with top-p or a large top-k.
+// The histogram of a wide row with top-p or a large top-k.  Groups whose largest logit lies behind all bins are not read.  Bound by the
+// atomics in LDS of neighbouring weights: 64 x 128256 bf16 11 us, 32 of 256 x 152064 fp32 among others 20.
 template <typename T, int kVecs>
 __global__ void __launch_bounds__(kThreads)
 sample_bins_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride, const uint32_t* __restrict__ groups,
@@ -679,7 +683,8 @@ sample_wide_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t 
   }
 }
 
-// The parts of a wide row joined, with the listed logits' share; rows that no other step took.
+// The parts of a wide row joined, with the listed logits' share; rows that no other step took.  One workgroup a row: a chain of
+// the bins' sums, the list's order and two sums over the lanes, 17 us whatever the number of rows.
 template <typename T>
 __global__ void __launch_bounds__(kAnyThreads)
 sample_join_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride, uint32_t segments,
@@ -837,10 +842,10 @@ void launch_long_rows(const T* logits, int64_t B, uint32_t V, int64_t row_stride
                : any_small ? sample_pass_kernel<T, kVecs, true, true> : sample_pass_kernel<T, kVecs, true, false>;
   pass<<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, filters, parts, maxima, !all_small && any_cut ? wide : nullptr);
   if (!all_small) sample_plan_kernel<<<static_cast<uint32_t>((B + 3) / 4), kThreads, 0, stream>>>(B, V, segments, parts, filters, wide);
-  if (any_small && (!all_small || filters.top_k <= static_cast<int32_t>(kSmallMost)))
+  if (any_small && (!all_small || filters.top_k <= static_cast<int32_t>(kQuarterTop)))
     sample_small_kernel<T, kVecs, SampledSize><<<rows, SampledSize::kT, 0, stream>>>(logits, B, V, row_stride, segments, maxima, filters,
                                                                                     seeds, tokens, logprobs);
-  if (any_small && (!all_small || filters.top_k > static_cast<int32_t>(kSmallMost)))
+  if (any_small && (!all_small || filters.top_k > static_cast<int32_t>(kQuarterTop)))
     sample_small_kernel<T, kVecs, SelectionSize<false>><<<rows, kSmallTop, 0, stream>>>(logits, B, V, row_stride, segments, maxima, filters,
                                                                                        seeds, tokens, logprobs);
   if (all_small) return;
