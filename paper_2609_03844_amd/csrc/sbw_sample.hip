@@ -264,7 +264,7 @@ sample_any_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t r
 // ---------------------------------------------------------------------------
 constexpr uint32_t kSmallTop = SelectionSize<false>::kT;   // top-k that a row's first logits in order are gathered for
 constexpr uint32_t kQuarterTop = 64;            // of them by 256 lanes, the others by 1024 (sample_small_kernel)
-// As many keys a lane as a row of 160000 logits has groups: 200 and fewer of 256 x 152064 29 us with 8, 24 so.
+// As many keys a lane as a row of 160000 logits has groups (200 of 256 x 152064 29 us with 8, 24 so).
 struct SampledSize : SelectionSize<true> {
   static constexpr int kHeld = 20;
 };
@@ -380,8 +380,8 @@ sample_plan_kernel(int64_t B, uint32_t V, uint32_t segments, const Stats* __rest
 
 // A small top-k: the first logits in order, their weights' sums, the draw among those that are kept; a lane for each.  Bound by
 // dependent trips to memory, like any selection.  Us of a call with top-p, by 256 lanes and by 1024: 50 of 1 x 32000 fp32 13.3 and 14.2, of
-// 64 x 128256 bf16 16.4 and 17.4; 100 17.1 and 15.9, 21.3 and 19.0; 256 22.7 and 16.4, 29.3 and 20.5.  Where rows differ both are launched.  Up to
-// 1024 lanes' worth beats a histogram: 400 of 64 x 128256 21.6 and 48, 1000 28.5 and 50, of 256 x 152064 fp32 60 and 142; with top-p behind
+// 64 x 128256 bf16 16.4 and 17.4; 100 17.1 and 15.9, 21.3 and 19.0; 256 22.7 and 16.4, 29.3 and 20.5; where rows differ 1024 take all
+// (both, one after the other, 30 us of 256 requests).  Up to 1024 lanes' worth beats a histogram: 400 of 64 x 128256 21.6 and 48, 1000 28.5 and 50, of 256 x 152064 fp32 60 and 142; with top-p behind
 // it no histogram serves, and one workgroup a row takes 235 for 1 x 32000, 650 for 64 x 128256.
 template <typename T, int kVecs, typename Size>
 __global__ void __launch_bounds__(Size::kT)
@@ -395,7 +395,7 @@ sample_small_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t
   const uint32_t tid = threadIdx.x, wave = tid / kWave;
   for (int64_t b = blockIdx.x; b < B; b += gridDim.x) {
     const RowFilter f = row_filter(filters, b, V);
-    if (!is_small(f, V) || (f.top_k <= kQuarterTop) != Size::kSmall) continue;
+    if (!is_small(f, V)) continue;
     const T* row = logits + b * row_stride;
     const Maxima of_row = row_maxima(maxima, b, segments);
     const uint64_t* best = select_row<T, kVecs, Size>(
@@ -842,12 +842,12 @@ void launch_long_rows(const T* logits, int64_t B, uint32_t V, int64_t row_stride
                : any_small ? sample_pass_kernel<T, kVecs, true, true> : sample_pass_kernel<T, kVecs, true, false>;
   pass<<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, filters, parts, maxima, !all_small && any_cut ? wide : nullptr);
   if (!all_small) sample_plan_kernel<<<static_cast<uint32_t>((B + 3) / 4), kThreads, 0, stream>>>(B, V, segments, parts, filters, wide);
-  if (any_small && (!all_small || filters.top_k <= static_cast<int32_t>(kQuarterTop)))
-    sample_small_kernel<T, kVecs, SampledSize><<<rows, SampledSize::kT, 0, stream>>>(logits, B, V, row_stride, segments, maxima, filters,
-                                                                                    seeds, tokens, logprobs);
-  if (any_small && (!all_small || filters.top_k > static_cast<int32_t>(kQuarterTop)))
-    sample_small_kernel<T, kVecs, SelectionSize<false>><<<rows, kSmallTop, 0, stream>>>(logits, B, V, row_stride, segments, maxima, filters,
-                                                                                       seeds, tokens, logprobs);
+  if (any_small) {
+    const bool quarter = all_small && filters.top_k <= static_cast<int32_t>(kQuarterTop);
+    auto* small = quarter ? sample_small_kernel<T, kVecs, SampledSize> : sample_small_kernel<T, kVecs, SelectionSize<false>>;
+    small<<<rows, quarter ? SampledSize::kT : kSmallTop, 0, stream>>>(logits, B, V, row_stride, segments, maxima, filters, seeds, tokens,
+                                                                      logprobs);
+  }
   if (all_small) return;
   if (any_cut) sample_bins_kernel<T, kVecs><<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, maxima.groups, filters, wide);
   sample_wide_kernel<T, kVecs><<<grid, kThreads, 0, stream>>>(logits, B, V, row_stride, maxima.groups, filters, seeds, wide, bests);
