@@ -5,6 +5,7 @@ import torch
 
 import oracle
 import sample_reference as ref
+from test_gpu_fp8 import layer_reference
 from test_gpu_step import DTYPES, logits, placed, special
 
 pytestmark = pytest.mark.gpu
@@ -317,3 +318,39 @@ def test_in_a_decode_step(sbw):
     # the filters only raise the probability of what they keep
     _, lp = sbw.sample_tokens(marked, seeds, 1.25, 50, 0.95)
     assert (lp >= answer.logprobs - 1e-4).all()
+
+
+def test_example_of_requests_and_an_8_bit_head(sbw):
+    """The example's steps: tokens within what the filters keep, gradients against the layer's definition."""
+    import importlib.util
+    import pathlib
+    path = pathlib.Path(__file__).resolve().parents[1] / "examples" / "decode_step.py"
+    spec = importlib.util.spec_from_file_location("decode_step", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    B, V, K = 12, 5003, 256
+    hidden = torch.randn((B, K), generator=g, device="cuda").to(torch.bfloat16)
+    weight = torch.randn((V, K), generator=g, device="cuda") * 3 / 16
+    window = torch.randint(0, V, (B, 4), generator=g, device="cuda", dtype=torch.int32)
+    seeds = torch.randint(0, 1 << 62, (B,), generator=g, device="cuda")
+    full = lambda v: torch.full((B,), v, device="cuda")  # noqa: E731
+    head = sbw.quantize_fp8(weight, 128)
+    top_ks = torch.full((B,), 5, device="cuda", dtype=torch.int32)
+    tokens, logprobs = example.requests_step(hidden, head, window, seeds, full(1.0), top_ks, full(0.9), full(0.0))
+    logits = sbw.matmul_fp8(*sbw.quantize_fp8(hidden), *head)
+    sbw.watermark(logits, window, example.KEY, example.GAMMA, example.DELTA)
+    five = sbw.top_candidates(logits, 5)[0]
+    assert (five == tokens[:, None]).any(1).all() and (logprobs <= 0).all()
+    loss, of_hidden, of_weight = example.head_training_step(hidden, weight, tokens)
+    # the layer's definition on the gradient of the log probabilities of its own logits, of type bf16
+    z = sbw.linear_fp8(hidden, weight).double()
+    p = torch.softmax(z, 1)
+    p[torch.arange(B), tokens.long()] -= 1
+    dy = (p / B).to(torch.bfloat16).float().cpu().numpy()
+    want = layer_reference(hidden.float().cpu().numpy(), weight.cpu().numpy(), dy)
+    # The kernel's gradient is within 2^-18 of this one, so one value in 2^8 at most rounds to another bf16, and its code moves by a
+    # step of 2^-3 of it at most: sqrt(2^-8) 2^-3 = 2^-7 of the whole.  The results' own rounding is 2^-9.
+    for got, name in ((of_hidden, "dx"), (of_weight, "dw")):
+        exact, _ = want(name == "dx")[name]
+        assert np.linalg.norm(got.double().cpu().numpy() - exact) < 2.0 ** -6 * np.linalg.norm(exact), name
