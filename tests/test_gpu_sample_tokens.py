@@ -252,6 +252,23 @@ def test_more_rows_than_take_a_turn(sbw, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [1, 5, 1025, 1100, 5003, 40001])
+def test_top_k_of_every_size(sbw, V, dtype):
+    """Around the sizes where another step takes over, of each row and of all."""
+    rng = np.random.default_rng(V)
+    sizes = np.array([0, 1, 2, 63, 64, 65, 255, 256, 257, 1023, 1024, 1025, V - 1, V, V + 1])
+    x = 3 * rng.standard_normal((sizes.size, V)).astype(np.float32)
+    x[1::3] = np.round(x[1::3])
+    t, exact = placed(x, dtype, 1, 1)
+    for f in (dict(), dict(top_p=0.95), dict(min_p=0.01)):
+        say(f"sample top-k {dtype} {V} {f}")
+        check(sbw, t, exact, rng, top_k=sizes, **f)
+    for k in (64, 65, 1024, 1025):
+        say(f"sample top-k {dtype} {V} {k}")
+        check(sbw, t[:6], exact[:6], rng, top_k=k, top_p=0.9)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("V", [130, 5003])
 def test_scores_beyond_the_type(sbw, V, dtype):
     """Temperatures so low that scores overflow, so high that they vanish, and the smallest min-p."""
