@@ -147,7 +147,8 @@ sbw_status_t sbw_head_logits(const void *hidden, int64_t B, int64_t K, int64_t h
  * The token is the one of the largest logits_v * inv_temperature + G_v (rounded in fp32 twice, the lower column of equal
  * ones), G_v the noise of sbw_watermark_sample for column v under the row's seed: without filters it is that
  * call's token with gamma = 0.  Sums of weights are made in one order, or of whole numbers: the same call gives the same
- * answer.  They hold as many bits as fp32 at least, which decides for a logit that ends just where top-p does.
+ * answer.  Weights and their sums hold as many bits as fp32 at least, tails of small weights among them, which decides for a
+ * logit that ends just where top-p does.
  * A row with a NaN or +inf gives the first column of the order and NaN; one of -inf alone column 0 and -inf.
  *
  *   seeds            device, [B] uint64.

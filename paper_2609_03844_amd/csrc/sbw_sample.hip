@@ -2,9 +2,12 @@
 //
 // What the filters keep is a beginning of the row's order (larger first, equal ones by column): top-k by count, top-p by
 // the sum of weights before a logit, min-p by its own weight.  Weights are e_v = exp((x_v - m) / T) relative to the row's
-// largest logit m, held as whole numbers of 2^-F, so that their sums are exact in any order.  Of the kept ones
-// the token is the first with the largest x_v / T + G_v, G_v the sampler's Gumbel noise of column v under the
-// row's seed.
+// largest logit m.  Of the kept ones the token is the first with the largest x_v / T + G_v, G_v the sampler's Gumbel noise of
+// column v under the row's seed.
+//
+// Where top-p ends goes by sums of weights.  A small top-k sums doubles, in the lanes' order.  One workgroup a row sums whole
+// numbers of 2^-F, exact in any order.  The steps for wide rows hold a weight in fp32, and a row's sum like that of the log
+// probabilities; the sums in front of a bin are of whole numbers of 2^-61 of it, exact in any order, and doubles within a bin.
 #include "sbw_step.h"
 
 #include <algorithm>
@@ -270,7 +273,6 @@ struct SampledSize : SelectionSize<true> {
 };
 constexpr uint32_t kBins = 2048;
 constexpr uint32_t kListed = SelectionSize<false>::kList;
-constexpr int kWeightBits = 30;                 // of a weight in the histogram
 
 struct PartBest {
   uint64_t best;                                // score's key << 32 | ~column, of the kept ones of a part
@@ -282,8 +284,12 @@ struct WidePlan {
   bool small, plain;          // a small top-k; a row with a distribution
   bool by_count, cut, slow;   // the histogram counts; there is one; the row is left to one workgroup
   float m, c, scale, least;   // largest logit, score factor, bins per logit, min-p's floor
+  float unit;                 // whole numbers of a weight of 1 in the histogram
   double S, target;           // sum of weights; of the histogram's units in front of where the filter ends
 };
+// The power of two that takes a sum to between 2^61 and 2^62.  A weight loses less than one of its whole numbers, so V of them
+// less than V 2^-61 of the sum (whole numbers of 2^-30 of the largest weight lost V 2^-31 of that, far more than fp32 where a tail lies below).
+__device__ __forceinline__ float unit_of(float S) { return __uint_as_float((127u + 61u + 127u - (__float_as_uint(S) >> 23)) << 23); }
 __device__ __forceinline__ bool is_small(const RowFilter& f, uint32_t V) { return f.top_k <= kSmallTop && f.top_k < V; }
 __device__ __forceinline__ WidePlan wide_plan(const RowFilter& f, uint32_t V, Stats r) {
   WidePlan p{};
@@ -292,6 +298,7 @@ __device__ __forceinline__ WidePlan wide_plan(const RowFilter& f, uint32_t V, St
   p.m = r.m;
   p.c = score_factor(f.inv_t);
   p.S = r.S;
+  p.unit = unit_of(r.S);
   p.by_count = f.top_k < V;
   p.cut = p.by_count || f.top_p < 1.0f;
   p.slow = (p.by_count && f.top_p < 1.0f) || !(fabsf(r.m * f.inv_t) < INFINITY);
@@ -302,7 +309,7 @@ __device__ __forceinline__ WidePlan wide_plan(const RowFilter& f, uint32_t V, St
                                   : fmaxf((1.0f - f.top_p) * r.S / static_cast<float>(V) * 0.999f, 1e-12f);
     p.scale = static_cast<float>(kBins) * f.inv_t / -logf(fminf(left, 0.5f));
     p.target = p.by_count ? static_cast<double>(f.top_k)
-                          : ceil(static_cast<double>(f.top_p) * p.S * static_cast<double>(1u << kWeightBits));
+                          : ceil(static_cast<double>(f.top_p) * p.S * static_cast<double>(p.unit));
     if (!(p.scale > 1e-30f) || !(p.scale < 1e30f)) p.slow = true;
   }
   return p;
@@ -507,8 +514,8 @@ sample_bins_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t 
         const float v = elem(x, e);
         const uint32_t bin = bin_of(p, v);
         if (bin >= kBins || j * kPer + e >= V) continue;
-        const uint32_t w = p.by_count ? 1u : static_cast<uint32_t>(__builtin_fmaf(weight_of(p, v), static_cast<float>(1u << kWeightBits), 0.5f));
-        atomicAdd(reinterpret_cast<unsigned long long*>(&bins[bin]), static_cast<unsigned long long>(w));
+        const auto w = p.by_count ? 1ull : static_cast<unsigned long long>(weight_of(p, v) * p.unit);
+        atomicAdd(reinterpret_cast<unsigned long long*>(&bins[bin]), w);
       }
     }
     __syncthreads();
@@ -737,8 +744,7 @@ sample_join_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t 
     }
     double own = 0.0;                    // of the listed logits that are kept
     if (p.cut) {
-      const double unit = static_cast<double>(1u << kWeightBits);
-      const double before = p.by_count ? 0.0 : static_cast<double>(cut.before) / unit, target = p.by_count ? 0.0 : static_cast<double>(f.top_p) * p.S;
+      const double before = p.by_count ? 0.0 : static_cast<double>(cut.before) / static_cast<double>(p.unit), target = p.by_count ? 0.0 : static_cast<double>(f.top_p) * p.S;
       const uint32_t still = p.by_count ? f.top_k - static_cast<uint32_t>(cut.before) : listed;
       for (uint32_t i = tid; i < listed; i += kAnyThreads) s.list.list[i] = wide[b].list[i];
       __syncthreads();
