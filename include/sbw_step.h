@@ -156,8 +156,8 @@ sbw_status_t sbw_head_logits(const void *hidden, int64_t B, int64_t K, int64_t h
  *                    SBW_ERR_INVALID_ARG; a row whose own is not gives token -1 and NaN).
  *   top_ks           device, [B] int32, or NULL: top_k for all rows.  0 and less, V and more keep all.
  *   top_ps, min_ps   device, [B] float each, or NULL: top_p and min_p for all rows (not NaN, else
- *                    SBW_ERR_INVALID_ARG).  top_p keeps all from 1 on (or NaN), min_p up to 0 (or NaN); a min_p beyond 1
- *                    is 1.
+ *                    SBW_ERR_INVALID_ARG).  top_p keeps all from 1 on (or NaN) and the first alone up to 0, min_p all up
+ *                    to 0 (or NaN); a min_p beyond 1 is 1.
  *   tokens           device, [B] int32, written.
  *   logprobs         device, [B] float, written (may be NULL): the token's log probability among the kept.
  *   workspace        device, sbw_sample_tokens_workspace(B, V) uint64 elements, caller-owned; contents on entry do

@@ -31,7 +31,7 @@ __device__ __forceinline__ RowFilter row_filter(const Filters& f, int64_t b, uin
               f.min_ps != nullptr ? f.min_ps[b] : f.min_p, 0u};
   const int32_t k = f.top_ks != nullptr ? f.top_ks[b] : f.top_k;
   r.top_k = k > 0 && static_cast<uint32_t>(k) < V ? static_cast<uint32_t>(k) : V;
-  if (!(r.top_p < 1.0f)) r.top_p = 1.0f;
+  r.top_p = r.top_p < 1.0f ? fmaxf(r.top_p, 0.0f) : 1.0f;   // its share of a sum is taken as a whole number without a sign
   r.min_p = r.min_p > 0.0f ? fminf(r.min_p, 1.0f) : 0.0f;
   return r;
 }

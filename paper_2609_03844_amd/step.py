@@ -395,8 +395,8 @@ def sample_tokens(logits: torch.Tensor, seeds: torch.Tensor, inv_temperature=1.0
 
     In the order of logits (larger first, equal ones by their id) top_k keeps the first k, top_p of those the ones before
     which less than top_p of their probability lies (the first at least), min_p of those the ones with at least min_p times
-    the largest probability.  0, 1 and 0 keep all.  Each parameter is a number, or a tensor with one for every row:
-    float32 [B], top_k int32 [B].
+    the largest probability.  0, 1 and 0 keep all, a top_p of 0 and less the first alone.  Each parameter is a number, or a
+    tensor with one for every row: float32 [B], top_k int32 [B].
 
     logits: [B, V] float32 or bfloat16, for instance as ``watermark()`` left them.  seeds: int64 [B], random; the noise is
     that of ``watermark_sample``, and without filters so is the token (with gamma 0).  A row with a NaN or +inf gives the
