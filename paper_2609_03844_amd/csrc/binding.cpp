@@ -552,7 +552,8 @@ PyObject* sample_tokens(PyObject*, PyObject* const* a, Py_ssize_t count) {
     const Tensor* seeds = packed_of(a[1], at::kLong, c.device);
     if (seeds == nullptr || seeds->dim() != 1 || seeds->size(0) != c.rows || !of_rows(a[2], at::kFloat, c, &inv_ts, &inv_t) ||
         !(integer(a[3], &top_k) || (THPVariable_CheckExact(a[3]) && of_rows(a[3], at::kInt, c, &top_ks, &unused))) ||
-        !of_rows(a[4], at::kFloat, c, &top_ps, &top_p) || !of_rows(a[5], at::kFloat, c, &min_ps, &min_p))
+        !of_rows(a[4], at::kFloat, c, &top_ps, &top_p) || !of_rows(a[5], at::kFloat, c, &min_ps, &min_p) ||
+        (inv_ts != nullptr && followed(THPVariable_Unpack(a[2]))))
       Py_RETURN_NONE;
     Block block(sbw_sample_tokens_workspace(c.rows, c.columns), 2 * c.rows, c);
     Tensor tokens = block.take(at::kInt, {c.rows}), logprobs = block.take(at::kFloat, {c.rows});

@@ -403,8 +403,8 @@ def sample_tokens(logits: torch.Tensor, seeds: torch.Tensor, inv_temperature=1.0
     first column of its order with NaN, one of -inf alone column 0 with -inf, and a row whose inv_temperature in a tensor
     is not finite and positive -1 with NaN.  ``workspace`` is an int64 scratch tensor of at least
     sample_tokens_workspace_size(B, V) elements; what is allocated here may share one storage with it.  The log
-    probabilities carry no gradient (token_logprobs' do): logits that require one are refused unless it is off
-    (torch.no_grad()) or the tokens alone are asked for."""
+    probabilities carry no gradient (token_logprobs' do): logits or inv_temperature that require one are refused unless it is
+    off (torch.no_grad()) or the tokens alone are asked for."""
     if stream is None and tokens is None and logprobs is None and workspace is None and with_logprobs:
         got = _native.sample_tokens(logits, seeds, inv_temperature, top_k, top_p, min_p)
         if type(got) is tuple:
@@ -412,7 +412,8 @@ def sample_tokens(logits: torch.Tensor, seeds: torch.Tensor, inv_temperature=1.0
         if got is not None:
             _check(got)
     if with_logprobs or logprobs is not None:
-        _no_gradient("the log probabilities of sample_tokens", logits=logits)
+        of_temperature = {"inv_temperature": inv_temperature} if isinstance(inv_temperature, torch.Tensor) else {}
+        _no_gradient("the log probabilities of sample_tokens", logits=logits, **of_temperature)
     dtype, B, V, row_stride = _matrix(logits, "logits")
     dev = logits.device
     side = _side(stream, dev)
