@@ -227,8 +227,8 @@ def linear_fp8(x: torch.Tensor, weight: torch.Tensor, dtype: Optional[torch.dtyp
 
     (the blocks lie along what is summed over).  ``dtype`` of y: that of x when not given.  The gradients have the
     types of x and weight, which may change after the call: the backward pass has codes of its own.  K >= 1.  On the current
-    stream.  A call that is captured into a graph is refused while the result of an eager one on the default stream, with the
-    same leaf, is alive."""
+    stream.  A call with a gradient that is captured into a graph is refused while the result of an eager one on the default
+    stream, with the same leaf, is alive."""
     x_dtype, M, K, _ = _matrix(x, "x")
     _, N, columns, _ = _matrix(weight, "weight")
     if columns != K or K == 0:
@@ -238,6 +238,10 @@ def linear_fp8(x: torch.Tensor, weight: torch.Tensor, dtype: Optional[torch.dtyp
     if dtype not in (torch.float32, torch.bfloat16):
         raise TypeError("dtype must be float32 or bfloat16")
     _on_device(x=x, weight=weight)
+    if not (torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad)):
+        x8, _ = _quantized(x, 1, torch.float8_e8m0fnu, True, None)
+        w8, _ = _quantized(weight, BLOCK, torch.float8_e8m0fnu, True, None)
+        return matmul_fp8(*x8, *w8, dtype=dtype)
     if _native.capture_meets_eager(x, weight):
         raise RuntimeError("linear_fp8 cannot be captured while an eager graph of x or weight is alive: delete its results first")
     return _Linear.apply(x, weight, dtype)
