@@ -546,7 +546,8 @@ __device__ __forceinline__ TileAt tile_at(uint32_t id, uint32_t tiles_m, uint32_
 // read of LDS.  `arrived` waits for all but the newest `kNewer` fetches, and for the wave's own reads.
 //
 // A vector instruction may have written the scalar registers of a fetch just before (readfirstlane makes them), which takes five wait
-// states until an access to memory may read them; m0 takes one.  The compiler does not look into the statement, so it waits itself.
+// states until an access to memory may read them; m0, where the place in LDS stands, takes one.  The compiler does not look into the
+// statement, so it waits itself; m0 is an operand, so that the compiler knows who writes it.
 typedef uint32_t Buffer __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ Buffer buffer_of(const void* p) {
   const uint64_t at = reinterpret_cast<uint64_t>(p);
@@ -557,19 +558,19 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return __builtin_amdgcn_readfirstlane(static_cast<int>(reinterpret_cast<uintptr_t>((SBW_LDS const void*)p)));
 }
 __device__ __forceinline__ void fetch_to_lds(Buffer from, uint32_t at, uint32_t base, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-               :: "s"(to), "v"(at), "s"(from), "s"(base) : "memory");
+  asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+               :: "{m0}"(to), "v"(at), "s"(from), "s"(base) : "memory");
 }
 __device__ __forceinline__ void fetch_word_to_lds(Buffer from, uint32_t at, uint32_t base, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, %3 offen lds"
-               :: "s"(to), "v"(at), "s"(from), "s"(base) : "memory");
+  asm volatile("s_nop 4\n\tbuffer_load_dword %1, %2, %3 offen lds"
+               :: "{m0}"(to), "v"(at), "s"(from), "s"(base) : "memory");
 }
 // A word a lane; of scales of one byte that byte.
 template <bool kByte>
 __device__ __forceinline__ void fetch_scale_to_lds(Buffer from, uint32_t at, uint32_t base, uint32_t to) {
   if constexpr (kByte)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_ubyte %1, %2, %3 offen lds"
-                 :: "s"(to), "v"(at), "s"(from), "s"(base) : "memory");
+    asm volatile("s_nop 4\n\tbuffer_load_ubyte %1, %2, %3 offen lds"
+                 :: "{m0}"(to), "v"(at), "s"(from), "s"(base) : "memory");
   else
     fetch_word_to_lds(from, at, base, to);
 }

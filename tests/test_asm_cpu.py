@@ -27,3 +27,15 @@ def test_accesses_wait_for_their_scalar_registers():
             nop = re.match(r"s_nop (\d+)", instruction)
             states += int(nop[1]) + 1 if nop else 1
     assert accesses >= 3
+
+
+def test_m0_is_written_by_the_compiler():
+    """It may keep a value of its own there across a statement that does not say otherwise."""
+    fetches = 0
+    for name, code, operands in statements():
+        for instruction in code:
+            assert not re.match(r"s_\w+ m0\b", instruction), (name, code)
+            if re.match(r"buffer_load.* lds$", instruction):
+                fetches += 1
+                assert '"{m0}"(' in operands, (name, code)
+    assert fetches >= 3
