@@ -789,20 +789,20 @@ product_tiles_kernel(Side a, Side b, uint32_t K, uint32_t blocks_each, Out* __re
   }
 }
 
-// Few rows of a (up to kMt * 16): the rows of b stream past them once.  The waves of a workgroup share the columns, kSteps
+// Up to 16 rows of a: the rows of b stream past them once.  The waves of a workgroup share the columns, kSteps
 // blocks each, and keep their part of a in registers; a wave's part of 16 * kTn rows of b goes from memory into registers and
 // into the instructions (a's rows as rows, b's as columns).  The waves' sums meet in LDS.  Any alignment.  Bound by memory, with a barrier
 // and the waves' sums for every tile: 1 x 32000 x 2048 15.6 us, 4.2 TB/s.
-template <typename Out, bool kE8, int kMt, int kSteps, int kTn>
+template <typename Out, bool kE8, int kSteps, int kTn>
 __global__ void __launch_bounds__(1024)
 product_rows_kernel(Side a, Side b, uint32_t K, Out* __restrict__ out, int64_t out_stride, uint32_t waves) {
   constexpr bool kExact = sizeof(Out) == 4, kInside = kE8 && !kExact;
-  constexpr uint32_t kSums = kTn * kMt * 256;               // of a wave
+  constexpr uint32_t kSums = kTn * 256;                     // of a wave
   // sixteen sums of a row side by side, rows 4 apart (of the wave's four quarters) in other banks
   const auto place_of_sum = [](uint32_t row, uint32_t c) { return row / 4 * 64 + ((row ^ row / 4) % 4) * 16 + c; };
   extern __shared__ float shared[];
   float* const sums[2] = {shared, shared + waves * kSums};
-  float* const row_scales = shared + 2 * waves * kSums;     // [wave][step][kMt * 16]
+  float* const row_scales = shared + 2 * waves * kSums;     // [wave][step][16]
   const uint32_t tid = threadIdx.x, lane = tid % kWave, r16 = lane % 16, quarter = lane / 16, threads = waves * kWave;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const uint32_t blocks = (K + kBlock - 1) / kBlock, first = wave * kSteps;
@@ -833,69 +833,58 @@ product_rows_kernel(Side a, Side b, uint32_t K, Out* __restrict__ out, int64_t o
   const auto next_of = [&](int64_t tile) { return tile + gridDim.x < tiles ? tile + gridDim.x : tile; };
   load(blockIdx.x);
 
-  Codes x[kMt][kSteps];
-  uint32_t sx[kMt][kSteps];
+  Codes x[kSteps];
+  uint32_t sx[kSteps];
 #pragma unroll
-  for (int i = 0; i < kMt; ++i)
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      const int64_t m = i * 16 + r16;
-      const uint8_t* row = a.codes + min(m, a.rows - 1) * a.stride;
-      x[i][s] = Codes{load_codes(row, column(s, 0), K), load_codes(row, column(s, 1), K)};
-      sx[i][s] = load_scale<kE8, kInside>(a, m, min(first + s, blocks - 1), blocks);
-      if (!kInside && quarter == 0) row_scales[(wave * kSteps + s) * (kMt * 16) + m] = __uint_as_float(sx[i][s]);
-    }
+  for (int s = 0; s < kSteps; ++s) {
+    const int64_t m = r16;
+    const uint8_t* row = a.codes + min(m, a.rows - 1) * a.stride;
+    x[s] = Codes{load_codes(row, column(s, 0), K), load_codes(row, column(s, 1), K)};
+    sx[s] = load_scale<kE8, kInside>(a, m, min(first + s, blocks - 1), blocks);
+    if (!kInside && quarter == 0) row_scales[(wave * kSteps + s) * 16 + m] = __uint_as_float(sx[s]);
+  }
   __syncthreads();
 
   uint32_t turn = 0;
   for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
 #pragma unroll
     for (int t = 0; t < kTn; ++t) {
-      f32x4 total[kMt] = {};
+      f32x4 total = {};
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
         if constexpr (kInside) {
-#pragma unroll
-          for (int i = 0; i < kMt; ++i)
-            total[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(as_operand(x[i][s]), as_operand(words[t][s]), total[i], 0, 0,
-                                                                        0, sx[i][s], 0, scale[t][s]);
+          total = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(as_operand(x[s]), as_operand(words[t][s]), total, 0, 0, 0, sx[s], 0,
+                                                                   scale[t][s]);
         } else {
           const float sb = kE8 ? power_of(scale[t][s]) : __uint_as_float(scale[t][s]);
-          Widened wide;
-          if constexpr (kExact) wide = widened(words[t][s]);
+          f32x4 part = {};
+          if constexpr (kExact) {
+            const Widened wide = widened(words[t][s]);
+            Codes c = x[s];
+            if (kSteps > 2) asm volatile("" : "+v"(c.lo), "+v"(c.hi));   // widened each time: there is no room to keep them
+            const Widened wx = widened(c);
 #pragma unroll
-          for (int i = 0; i < kMt; ++i) {
-            f32x4 part = {};
-            if constexpr (kExact) {
-              Codes c = x[i][s];
-              if (kMt * kSteps > 2) asm volatile("" : "+v"(c.lo), "+v"(c.hi));   // widened each time: there is no room to keep them
-              const Widened wx = widened(c);
-#pragma unroll
-              for (int h = 0; h < 4; ++h) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wx.part[h], wide.part[h], part, 0, 0, 0);
-            } else {
-              part = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(as_operand(x[i][s]), as_operand(words[t][s]), part, 0, 0, 0,
-                                                                      0x7F7F7F7F, 0, 0x7F7F7F7F);
-            }
-            const f32x4 sa = *reinterpret_cast<const f32x4*>(&row_scales[(wave * kSteps + s) * (kMt * 16) + i * 16 + quarter * 4]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) total[i][e] = __builtin_fmaf(part[e], sa[e] * sb, total[i][e]);
+            for (int h = 0; h < 4; ++h) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wx.part[h], wide.part[h], part, 0, 0, 0);
+          } else {
+            part = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(as_operand(x[s]), as_operand(words[t][s]), part, 0, 0, 0,
+                                                                    0x7F7F7F7F, 0, 0x7F7F7F7F);
           }
+          const f32x4 sa = *reinterpret_cast<const f32x4*>(&row_scales[(wave * kSteps + s) * 16 + quarter * 4]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) total[e] = __builtin_fmaf(part[e], sa[e] * sb, total[e]);
         }
       }
 #pragma unroll
-      for (int i = 0; i < kMt; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          sums[turn][wave * kSums + place_of_sum((t * kMt + i) * 16 + quarter * 4 + e, r16)] = total[i][e];
+      for (int e = 0; e < 4; ++e) sums[turn][wave * kSums + place_of_sum(t * 16 + quarter * 4 + e, r16)] = total[e];
     }
     __builtin_amdgcn_sched_barrier(0);
     load(next_of(tile));
     __builtin_amdgcn_sched_barrier(0);
     // the waves' reads of these sums are done when they meet here again, one tile later
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    for (uint32_t i = tid; i < kTn * kMt * 256; i += threads) {
+    for (uint32_t i = tid; i < kSums; i += threads) {
       const uint32_t row = i / 16, c = i % 16;               // row: a tile of 16 rows of b, a row of a
-      const int64_t m = row % (kMt * 16), n = tile * (16 * kTn) + row / (kMt * 16) * 16 + c;
+      const int64_t m = row % 16, n = tile * (16 * kTn) + row / 16 * 16 + c;
       if (m >= a.rows || n >= b.rows) continue;
       float sum = sums[turn][place_of_sum(row, c)];
       for (uint32_t w = 1; w < waves; ++w) sum += sums[turn][w * kSums + place_of_sum(row, c)];
@@ -905,13 +894,13 @@ product_rows_kernel(Side a, Side b, uint32_t K, Out* __restrict__ out, int64_t o
   }
 }
 
-template <typename Out, bool kE8, int kMt, int kSteps, int kTn>
+template <typename Out, bool kE8, int kSteps, int kTn>
 void launch_rows_of(Side a, Side b, int64_t K, void* out, int64_t out_stride, hipStream_t stream) {
   const auto waves = static_cast<uint32_t>((blocks_of(K) + kSteps - 1) / kSteps);
   const int64_t tiles = (b.rows + 16 * kTn - 1) / (16 * kTn);
   const int64_t resident = 256 * (16 / waves);
-  const uint32_t lds = (2 * waves * kTn * kMt * 256 + waves * kSteps * kMt * 16) * sizeof(float);
-  product_rows_kernel<Out, kE8, kMt, kSteps, kTn><<<static_cast<uint32_t>(tiles < resident ? tiles : resident), waves * kWave, lds, stream>>>(
+  const uint32_t lds = (2 * waves * kTn * 256 + waves * kSteps * 16) * sizeof(float);
+  product_rows_kernel<Out, kE8, kSteps, kTn><<<static_cast<uint32_t>(tiles < resident ? tiles : resident), waves * kWave, lds, stream>>>(
       a, b, static_cast<uint32_t>(K), static_cast<Out*>(out), out_stride, waves);
 }
 
@@ -1208,7 +1197,7 @@ void launch_product(Side a, Side b, int64_t K, void* out_, int64_t out_stride, u
   const Plan plan = plan_of(a.rows, b.rows, K, kE8 && !kExact, direct);
   const int64_t blocks = blocks_of(K);
   if (plan.form == Form::kRows) {
-    auto* launch = blocks <= 16 ? launch_rows_of<Out, kE8, 1, 1, 2> : blocks <= 32 ? launch_rows_of<Out, kE8, 1, 2, 2> : launch_rows_of<Out, kE8, 1, 4, 1>;
+    auto* launch = blocks <= 16 ? launch_rows_of<Out, kE8, 1, 2> : blocks <= 32 ? launch_rows_of<Out, kE8, 2, 2> : launch_rows_of<Out, kE8, 4, 1>;
     launch(a, b, K, out, out_stride, stream);
     return;
   }

@@ -62,7 +62,7 @@ __device__ __forceinline__ float float_from(double x) {
 constexpr int kAnyThreads = 1024;
 constexpr uint32_t kDigits = 256;
 struct AnyRow {
-  uint64_t mass[kDigits], best[kAnyThreads / kWave], sums[kAnyThreads / kWave];
+  uint64_t mass[kDigits], sums[kAnyThreads / kWave];
   uint32_t count[kDigits], digit;
   uint64_t above;          // counts or masses of larger digits
 };
