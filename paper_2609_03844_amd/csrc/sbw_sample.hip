@@ -78,7 +78,7 @@ __device__ __forceinline__ uint64_t wave_most64(uint64_t x) {
   return x;
 }
 
-// A row of any kind by one workgroup (140 us where top-k and top-p both cut), which reads it once for each step: the largest logit; four digits
+// A row of any kind by one workgroup (1 x 32000 fp32 of a spread of 3: 330 us where a top-k of 1025 and top-p both cut), which reads it once for each step: the largest logit; four digits
 // of the key where top-k ends, four of the one where top-p ends, four of a column where equal logits are parted; the
 // weights and the draw.
 template <typename T>
@@ -484,7 +484,7 @@ __device__ __forceinline__ uint32_t list_groups(bool some, uint16_t* list, uint3
 }
 
 // The histogram of a wide row with top-p or a large top-k.  Groups whose largest logit lies behind all bins are not read.  Bound by the
-// atomics in LDS of neighbouring weights: 64 x 128256 bf16 11 us, 32 of 256 x 152064 fp32 among others 20.
+// atomics in LDS of neighbouring weights: 64 x 128256 bf16 12.6 us, 32 of 256 x 152064 fp32 among others 20.
 template <typename T, int kVecs>
 __global__ void __launch_bounds__(kThreads)
 sample_bins_kernel(const T* __restrict__ logits, int64_t B, uint32_t V, int64_t row_stride, const uint32_t* __restrict__ groups,

@@ -148,9 +148,12 @@ def matmul_fp8(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scale
     128 columns of a row, or of 128 rows, by their shape.  K >= 1.  Rows of codes have unit stride and may be padded; those
     that start at multiples of 16 bytes are fetched faster.
 
-    dtype (of the product): float32 or bfloat16, rounded once from sums in float32.  The product carries no
-    gradient (linear_fp8() does): scales that require one are refused unless it is off.  ``workspace`` is an int64
-    scratch tensor of at least matmul_fp8_workspace_size(M, N, K) elements (allocated here when not given)."""
+    dtype (of the product): float32 or bfloat16, rounded once from sums in float32.  A float32 product is of exact terms; for a
+    bfloat16 one each term may be cut off 13 bits below the power of two of the largest of its eight neighbours on its way into the
+    sum.  The product of two blocks' scales is to lie in float32's range, outside of which results are 0, infinite or NaN where
+    the sums need not be.  The product carries no gradient (linear_fp8() does): scales that require one are refused unless it is
+    off.  ``workspace`` is an int64 scratch tensor of at least matmul_fp8_workspace_size(M, N, K) elements (allocated here when not
+    given)."""
     if stream is None and out is None and workspace is None and (dtype is torch.float32 or dtype is torch.bfloat16):
         got = _native.matmul_fp8(a, a_scales, b, b_scales, dtype is torch.bfloat16)
         if type(got) is torch.Tensor:
@@ -225,7 +228,8 @@ def linear_fp8(x: torch.Tensor, weight: torch.Tensor, dtype: Optional[torch.dtyp
 
         y = Q1(x) Q128(weight)^T,   dx = Q1(dy) Q128(weight),   dw = Q1(dy^T) Q1(x^T)^T
 
-    (the blocks lie along what is summed over).  ``dtype`` of y: that of x when not given.  The gradients have the
+    (the blocks lie along what is summed over; products as matmul_fp8()'s, so blocks whose largest values multiply to less than
+    about 1e-32 or more than about 1e43 are out of range).  ``dtype`` of y: that of x when not given.  The gradients have the
     types of x and weight, which may change after the call: the backward pass has codes of its own.  K >= 1.  On the current
     stream.  A call with a gradient that is captured into a graph is refused while the result of an eager one on the default
     stream, with the same leaf, is alive."""
