@@ -687,9 +687,9 @@ PyCFunction fast(PyObject* (*f)(PyObject*, PyObject* const*, Py_ssize_t)) {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f));
 }
 
-// (x, ...): whether the current stream is being captured while a live graph of an eager call accumulates into one of the
-// tensors on the default stream.  A captured backward pass would wait on that stream, which a capture forbids, and torch ends
-// the process for it.
+// (x, ...): whether the current stream is being captured while one of the tensors has its gradient taken on the default
+// stream: by a live graph of an eager call that accumulates into it there, or by the eager call there that it comes from.  A
+// captured backward pass would wait on that stream, which a capture forbids, and torch ends the process for it.
 PyObject* capture_meets_eager(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const c10::DeviceIndex device = c10::hip::current_device();
   hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
@@ -700,8 +700,8 @@ PyObject* capture_meets_eager(PyObject*, PyObject* const* a, Py_ssize_t n) {
   for (Py_ssize_t i = 0; i < n; ++i) {
     if (!THPVariable_Check(a[i])) continue;
     const Tensor& t = THPVariable_Unpack(a[i]);
-    if (!t.requires_grad() || !t.is_leaf()) continue;
-    const auto node = torch::autograd::impl::try_get_grad_accumulator(t);
+    if (!t.requires_grad()) continue;
+    const auto node = t.is_leaf() ? torch::autograd::impl::try_get_grad_accumulator(t) : t.grad_fn();
     if (node == nullptr) continue;
     const auto stream = node->stream();
     if (stream && stream->id() == eager) Py_RETURN_TRUE;

@@ -232,7 +232,7 @@ def linear_fp8(x: torch.Tensor, weight: torch.Tensor, dtype: Optional[torch.dtyp
     about 1e-32 or more than about 1e43 are out of range).  ``dtype`` of y: that of x when not given.  The gradients have the
     types of x and weight, which may change after the call: the backward pass has codes of its own.  K >= 1.  On the current
     stream.  A call with a gradient that is captured into a graph is refused while the result of an eager one on the default
-    stream, with the same leaf, is alive."""
+    stream, with the same leaf, is alive, and where x or weight itself comes from an eager call there: detach() it."""
     x_dtype, M, K, _ = _matrix(x, "x")
     _, N, columns, _ = _matrix(weight, "weight")
     if columns != K or K == 0:
@@ -247,5 +247,6 @@ def linear_fp8(x: torch.Tensor, weight: torch.Tensor, dtype: Optional[torch.dtyp
         w8, _ = _quantized(weight, BLOCK, torch.float8_e8m0fnu, True, None)
         return matmul_fp8(*x8, *w8, dtype=dtype)
     if _native.capture_meets_eager(x, weight):
-        raise RuntimeError("linear_fp8 cannot be captured while an eager graph of x or weight is alive: delete its results first")
+        raise RuntimeError("linear_fp8 cannot be captured while an eager graph of x or weight is alive: delete its results first, "
+                           "or detach() what comes from it")
     return _Linear.apply(x, weight, dtype)
